@@ -4,7 +4,10 @@ The product is the HIP library behind ``include/mosaic.h``; ``binding`` marshals
 tensors to it, ``workloads`` draws the seeded synthetic inputs, ``build`` compiles the library.
 """
 from . import binding, workloads  # noqa: F401
-from .binding import (MaskOnlyLogits, MosaicError, MosaicPlan, mosaic_compact_scratch_bytes,  # noqa: F401
+from .binding import (MaskOnlyLogits, MosaicError, MosaicPlan, Q8Rows, mosaic_checkpoint_load,  # noqa: F401
+                      mosaic_checkpoint_store, mosaic_compact_scratch_bytes, mosaic_gated_ffn_backward,
+                      mosaic_gated_ffn_backward_workspace_bytes, mosaic_gated_ffn_forward,
                       mosaic_mask_compact, mosaic_masked_logits_reduce, mosaic_masked_logits_sample,
-                      mosaic_plan_workspace, mosaic_sample_workspace_bytes,
+                      mosaic_plan_workspace, mosaic_rmsnorm_backward, mosaic_rmsnorm_backward_workspace_bytes,
+                      mosaic_rmsnorm_forward, mosaic_sample_workspace_bytes,
                       mosaic_shift_indices, mosaic_unmask_topn)

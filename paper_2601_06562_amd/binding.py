@@ -38,6 +38,16 @@ EXPORTS = (
     "mosaic_vmm_reserved_bytes", "mosaic_vmm_granularity", "mosaic_vmm_kept_contents", "mosaic_vmm_last_error",
     "mosaic_vmm_destroy",
 )
+LAYER_EXPORTS = (   # include/mosaic_layer.h
+    "mosaic_checkpoint_store", "mosaic_checkpoint_load", "mosaic_rmsnorm_forward",
+    "mosaic_rmsnorm_backward_workspace_bytes", "mosaic_rmsnorm_backward", "mosaic_gated_ffn_forward",
+    "mosaic_gated_ffn_backward_workspace_bytes", "mosaic_gated_ffn_backward",
+)
+BF16, F32 = 0, 1                     # mosaic_type
+INT8, E4M3 = 0, 1                    # mosaic_q8_format
+ACT_SILU, ACT_GELU_TANH = 0, 1       # mosaic_activation
+MAX_NORM_ROW = 16384
+MAX_ROW = 1 << 17
 GRAPH_EXPORTS = (
     "mosaic_graph_create", "mosaic_graph_destroy", "mosaic_graph_add_dim", "mosaic_graph_add_chunk_param",
     "mosaic_graph_add_tensor", "mosaic_graph_add_op", "mosaic_graph_add_alias", "mosaic_graph_add_barrier",
@@ -70,6 +80,11 @@ class MosaicPlan(ctypes.Structure):
         return ("MosaicPlan(workspace_bytes=%d, num_chunks=%d, rows_per_chunk=%d, vocab_splits=%d, tile_panel=%d, "
                 "grid=%d)" % (self.workspace_bytes, self.num_chunks, self.rows_per_chunk, self.vocab_splits,
                               self.tile_panel, self.grid))
+
+
+class MosaicQ8Rows(ctypes.Structure):
+    _fields_ = [("values", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("ld_values", ctypes.c_int64),
+                ("ld_scales", ctypes.c_int64), ("format", ctypes.c_int32), ("group", ctypes.c_int32)]
 
 
 class MosaicError(RuntimeError):
@@ -156,6 +171,25 @@ def lib():
         L.mosaic_graph_plan.argtypes = [p, p, ctypes.c_int, p, ctypes.c_int, p, i64, ctypes.POINTER(MosaicPlanSummary)]
         L.mosaic_graph_search.restype = ctypes.c_int
         L.mosaic_graph_search.argtypes = [p, p, ctypes.c_int, i64, p, ctypes.c_int, ctypes.POINTER(MosaicPlanSummary), p]
+        q8, f32 = ctypes.POINTER(MosaicQ8Rows), ctypes.c_float
+        L.mosaic_checkpoint_store.restype = ctypes.c_int
+        L.mosaic_checkpoint_store.argtypes = [p, i32, i64, i64, i32, q8, p]
+        L.mosaic_checkpoint_load.restype = ctypes.c_int
+        L.mosaic_checkpoint_load.argtypes = [q8, i64, i32, p, i32, i64, p]
+        L.mosaic_rmsnorm_forward.restype = ctypes.c_int
+        L.mosaic_rmsnorm_forward.argtypes = [p, i64, p, i32, i64, p, i32, f32, i64, i32, p, p, i64, p, i64, p, i64, q8, p]
+        L.mosaic_rmsnorm_backward_workspace_bytes.restype = i64
+        L.mosaic_rmsnorm_backward_workspace_bytes.argtypes = [i64, i32]
+        L.mosaic_rmsnorm_backward.restype = ctypes.c_int
+        L.mosaic_rmsnorm_backward.argtypes = [p, i64, p, i64, q8, i32, p, i32, f32, i64, i32, p, i64, p, i64, p, i32, p, i64,
+                                              p]
+        L.mosaic_gated_ffn_forward.restype = ctypes.c_int
+        L.mosaic_gated_ffn_forward.argtypes = [p, i64, p, p, i64, i64, i32, i32, i32, p, i64, p]
+        L.mosaic_gated_ffn_backward_workspace_bytes.restype = i64
+        L.mosaic_gated_ffn_backward_workspace_bytes.argtypes = [i64, i32, i32, i32]
+        L.mosaic_gated_ffn_backward.restype = ctypes.c_int
+        L.mosaic_gated_ffn_backward.argtypes = [p, i64, p, i64, q8, p, p, i64, i64, i32, i32, i32, p, i64, p, i64, p, p, i32,
+                                                i64, i32, p, i64, p]
         _lib = L
     return _lib
 
@@ -317,6 +351,189 @@ def mosaic_mfma_probe(operands, sink, iters, num_wgs, stream=None) -> int:
     _check(lib().mosaic_mfma_probe(_dev_ptr(operands, "operands", torch.bfloat16), _dev_ptr(sink, "sink", torch.float32),
                                    int(iters), int(num_wgs), _stream_ptr(stream)), "mosaic_mfma_probe")
     return int(lib().mosaic_mfma_probe_flops(int(iters), int(num_wgs)))
+
+
+# ---- the layer work on either side of the pass (include/mosaic_layer.h)
+
+_TYPES = {torch.bfloat16: BF16, torch.float32: F32}
+_FORMATS = {torch.int8: INT8, torch.float8_e4m3fn: E4M3}
+
+
+def _type_of(t, name):
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{name} must be torch.bfloat16 or torch.float32, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _rows(t, name, T, cols, dtype=None):
+    """(pointer, row stride) of a [T, cols] device matrix with dense rows; (0, 0) for None."""
+    if t is None:
+        return 0, 0
+    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != cols:
+        raise ValueError(f"{name} must be [{T}, {cols}], got {list(t.shape)}")
+    ld = t.stride(0) if T > 1 else cols
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"the rows of {name} must be dense")
+    return _dev_ptr(t, name, dtype), ld
+
+
+def _vector(t, name, n, dtype=None):
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must hold {n} dense elements")
+    return _dev_ptr(t, name, dtype)
+
+
+class Q8Rows:
+    """Rows in 8 bits: `values` int8 or float8_e4m3fn [T, d] and `scales` float32 [T, ceil(d / group)], device tensors
+    that the caller owns (the object keeps them alive)."""
+
+    def __init__(self, values, scales, group=128):
+        if values.dtype not in _FORMATS:
+            raise TypeError(f"values must be torch.int8 or torch.float8_e4m3fn, got {values.dtype}")
+        T, d = values.shape
+        p_values, ld_values = _rows(values, "values", T, d)
+        p_scales, ld_scales = _rows(scales, "scales", T, -(-d // int(group)), torch.float32)
+        self.values, self.scales, self.group = values, scales, int(group)
+        self.shape = (T, d)
+        self._c = MosaicQ8Rows(p_values, p_scales, ld_values, ld_scales, _FORMATS[values.dtype], self.group)
+        self._ref = ctypes.byref(self._c)
+
+    @classmethod
+    def empty(cls, T, d, dtype=torch.int8, group=128, device="cuda"):
+        return cls(torch.empty((T, d), dtype=dtype, device=device),
+                   torch.empty((T, -(-d // group)), dtype=torch.float32, device=device), group)
+
+
+def mosaic_checkpoint_store(x, q8, stream=None):
+    """Rows of x (bf16 or float32 [T, d]) into 8 bits."""
+    T, d = q8.shape
+    ptr, ld = _rows(x, "x", T, d)
+    _check(lib().mosaic_checkpoint_store(ptr, _type_of(x, "x"), ld, T, d, q8._ref, _stream_ptr(stream)),
+           "mosaic_checkpoint_store")
+
+
+def mosaic_checkpoint_load(q8, out, stream=None):
+    """What 8-bit rows stand for, into out (bf16 or float32 [T, d])."""
+    T, d = q8.shape
+    ptr, ld = _rows(out, "out", T, d)
+    _check(lib().mosaic_checkpoint_load(q8._ref, T, d, ptr, _type_of(out, "out"), ld, _stream_ptr(stream)),
+           "mosaic_checkpoint_load")
+
+
+def mosaic_rmsnorm_forward(x, residual, gamma, eps, y, sum=None, q8=None, idx=None, count=None, max_rows=None, stream=None):
+    """sum = x + residual, y = sum / rms(sum) * gamma, and y in 8 bits, over all rows or the listed ones.  x bf16 [T, d] or
+    None, residual bf16 or float32 or None; sum (of the residual's type), y (bf16) and q8 are outputs, None where not
+    wanted.  idx, count: int32 device tensors as mosaic_mask_compact makes them; max_rows bounds the count (default:
+    the entries that idx has room for, at most T)."""
+    first = x if x is not None else residual
+    if first is None:
+        raise ValueError("x or residual is needed")
+    T, d = first.shape
+    stream_type = _type_of(residual, "residual") if residual is not None else (_type_of(sum, "sum") if sum is not None else BF16)
+    if residual is not None and sum is not None and sum.dtype != residual.dtype:
+        raise TypeError("sum must have the residual's type")
+    if q8 is not None and q8.shape != (T, d):
+        raise ValueError("q8 must have the shape of the rows")
+    p_x, ld_x = _rows(x, "x", T, d, torch.bfloat16)
+    p_r, ld_r = _rows(residual, "residual", T, d)
+    p_s, ld_s = _rows(sum, "sum", T, d)
+    p_y, ld_y = _rows(y, "y", T, d, torch.bfloat16)
+    if max_rows is None:
+        max_rows = min(T, idx.numel()) if idx is not None else 0
+    elif idx is not None and idx.numel() < max_rows:
+        raise ValueError("idx holds fewer than max_rows entries")
+    _check(lib().mosaic_rmsnorm_forward(
+        p_x, ld_x, p_r, stream_type, ld_r, _vector(gamma, "gamma", d), _type_of(gamma, "gamma"), float(eps), T, d,
+        _dev_ptr(idx, "idx", torch.int32), _dev_ptr(count, "count", torch.int32), max_rows, p_s, ld_s, p_y, ld_y,
+        q8._ref if q8 is not None else None, _stream_ptr(stream)), "mosaic_rmsnorm_forward")
+
+
+def mosaic_rmsnorm_backward_workspace_bytes(T, d) -> int:
+    return int(lib().mosaic_rmsnorm_backward_workspace_bytes(T, d))
+
+
+def mosaic_rmsnorm_backward(dy, h, gamma, eps, dsum, dgamma, workspace, dsum_in=None, accumulate=False, stream=None):
+    """Gradient of the norm at h (the kept sum: bf16 or float32 [T, d], or Q8Rows): dsum (plus dsum_in) and dgamma
+    (float32 [d]; added to what it holds if accumulate); either may be None."""
+    T, d = dy.shape
+    q8 = h if isinstance(h, Q8Rows) else None
+    if q8 is not None and q8.shape != (T, d):
+        raise ValueError("h must have the shape of dy")
+    p_dy, ld_dy = _rows(dy, "dy", T, d, torch.bfloat16)
+    p_h, ld_h = _rows(None if q8 is not None else h, "h", T, d)
+    types = {t.dtype for t in (None if q8 is not None else h, dsum_in, dsum) if t is not None}
+    if len(types) > 1:
+        raise TypeError("h, dsum_in and dsum must have one type")
+    stream_type = BF16
+    for t in types:
+        if t not in _TYPES:
+            raise TypeError(f"h, dsum_in and dsum must be torch.bfloat16 or torch.float32, got {t}")
+        stream_type = _TYPES[t]
+    p_in, ld_in = _rows(dsum_in, "dsum_in", T, d)
+    p_out, ld_out = _rows(dsum, "dsum", T, d)
+    _check(lib().mosaic_rmsnorm_backward(
+        p_dy, ld_dy, p_h, ld_h, q8._ref if q8 is not None else None, stream_type, _vector(gamma, "gamma", d),
+        _type_of(gamma, "gamma"), float(eps), T, d, p_in, ld_in, p_out, ld_out,
+        _vector(dgamma, "dgamma", d, torch.float32) if dgamma is not None else 0, int(bool(accumulate)),
+        *_workspace_args(workspace), _stream_ptr(stream)), "mosaic_rmsnorm_backward")
+
+
+def _weights(w_gate, w_up, dtype=torch.bfloat16, names=("w_gate", "w_up")):
+    """(pointers, row stride) of two [F, d] matrices with one stride."""
+    F, d = w_gate.shape
+    p_g, ld_g = _rows(w_gate, names[0], F, d, dtype)
+    p_u, ld_u = _rows(w_up, names[1], F, d, dtype)
+    if ld_g != ld_u:
+        raise ValueError(f"{names[0]} and {names[1]} must have the same row stride")
+    return p_g, p_u, ld_g
+
+
+def mosaic_gated_ffn_forward(x, w_gate, w_up, out, activation=ACT_SILU, stream=None):
+    """out = act(x w_gate^T) * (x w_up^T): x bf16 [T, d], w_gate and w_up bf16 [F, d], out bf16 [T, F]."""
+    T, d = x.shape
+    F = w_gate.shape[0]
+    if w_gate.shape[1] != d:
+        raise ValueError("x and w_gate disagree on d")
+    p_x, ld_x = _rows(x, "x", T, d, torch.bfloat16)
+    p_g, p_u, ld_w = _weights(w_gate, w_up)
+    p_o, ld_o = _rows(out, "out", T, F, torch.bfloat16)
+    _check(lib().mosaic_gated_ffn_forward(p_x, ld_x, p_g, p_u, ld_w, T, d, F, int(activation), p_o, ld_o,
+                                          _stream_ptr(stream)), "mosaic_gated_ffn_forward")
+
+
+def mosaic_gated_ffn_backward_workspace_bytes(T, d, F, q8_input=False) -> int:
+    return int(lib().mosaic_gated_ffn_backward_workspace_bytes(T, d, F, int(bool(q8_input))))
+
+
+def mosaic_gated_ffn_backward(dout, x, w_gate, w_up, dx, dw_gate, dw_up, workspace, activation=ACT_SILU, out=None,
+                              accumulate=False, stream=None):
+    """Gradients of mosaic_gated_ffn_forward from dout (bf16 [T, F]) and the block's input x (bf16 [T, d], or Q8Rows):
+    dx bf16, dw_gate and dw_up bf16 or float32 (added to what they hold if accumulate; float32 only), and the block's
+    output again into `out`; each of dx, the pair and out may be None."""
+    T, F = dout.shape
+    d = w_gate.shape[1]
+    if w_gate.shape[0] != F:
+        raise ValueError("dout and w_gate disagree on F")
+    q8 = x if isinstance(x, Q8Rows) else None
+    if q8 is not None and q8.shape != (T, d):
+        raise ValueError("x must be [T, d]")
+    p_x, ld_x = _rows(None if q8 is not None else x, "x", T, d, torch.bfloat16)
+    p_do, ld_do = _rows(dout, "dout", T, F, torch.bfloat16)
+    p_g, p_u, ld_w = _weights(w_gate, w_up)
+    p_o, ld_o = _rows(out, "out", T, F, torch.bfloat16)
+    p_dx, ld_dx = _rows(dx, "dx", T, d, torch.bfloat16)
+    p_dg = p_du = ld_dw = dw_type = 0
+    if (dw_gate is None) != (dw_up is None):
+        raise ValueError("dw_gate and dw_up go together")
+    if dw_gate is not None:
+        dw_type = _type_of(dw_gate, "dw_gate")
+        if tuple(dw_gate.shape) != (F, d):
+            raise ValueError(f"dw_gate must be [{F}, {d}], got {list(dw_gate.shape)}")
+        p_dg, p_du, ld_dw = _weights(dw_gate, dw_up, dw_gate.dtype, ("dw_gate", "dw_up"))
+    _check(lib().mosaic_gated_ffn_backward(
+        p_do, ld_do, p_x, ld_x, q8._ref if q8 is not None else None, p_g, p_u, ld_w, T, d, F, int(activation), p_o, ld_o,
+        p_dx, ld_dx, p_dg, p_du, dw_type, ld_dw, int(bool(accumulate)), *_workspace_args(workspace), _stream_ptr(stream)),
+        "mosaic_gated_ffn_backward")
 
 
 class VmmWorkspace:

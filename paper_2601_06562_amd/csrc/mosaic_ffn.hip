@@ -1,0 +1,421 @@
+// Gated feed-forward block, act(x Wg^T) * (x Wu^T), and its gradients, on the matrix cores.
+//
+// All products run through one tile: 256 "P" rows by 64 QB "Q" rows, K in steps of 64.  P is the operand whose rows are the
+// output's contiguous columns (the accumulator layout gives a lane four consecutive P rows of one Q row, so results are
+// stored eight bytes a lane), Q the one whose rows are the output's rows:
+//   forward, and the projections again in the backward pass:  P = 128 rows of Wg and the same 128 of Wu, Q = x; the two
+//     projections of an element meet in one lane, so the activation and the product need no exchange
+//   dx:  P = columns of Wg, then of Wu (K = 2 F), Q = dg | du
+//   dw:  P = columns of x (K = T), Q = columns of dg | du
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "mosaic_layer_internal.h"
+
+namespace mosaic {
+namespace {
+
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef __attribute__((address_space(3))) bf16x4_t* lds_bf16x4_ptr_t;
+
+constexpr int kThreads = 512;        // 8 waves: 2 along P (128 rows each) x 4 along Q (16 QB rows each)
+constexpr int kStepK = 64;
+constexpr int kTileP = 256;
+constexpr int kBytesP = kTileP * kStepK * 2;
+constexpr uint32_t kOutside = 0x80000000u;   // a buffer offset past every range here: such a lane's copy brings zeros
+
+constexpr int kXcds = 8;
+
+enum { kForward, kRecompute, kDx, kDw };
+
+struct GemmArgs {
+  const char* p0;      // P: weights (gate / its columns), or x
+  const char* p1;      // up
+  const char* q;       // x, or dg | du
+  int64_t ld_p, ld_q;  // bytes
+  int64_t rows_q;      // Q rows of the output
+  int32_t rows_p;      // P rows of the output: F, d
+  int64_t depth;       // K: of a segment, where there are two (kDx: gate, up)
+  int32_t tiles_p, tiles_q;
+  int32_t splits;      // kDx: parts of K
+  int32_t F, f32, accumulate;
+  const char* dout;
+  int64_t ld_dout;     // bytes, as the strides below
+  char* out0;          // forward: out; kRecompute: out or nullptr; kDx: dx or the partial sums; kDw: dw_gate
+  char* out1;          // kRecompute: dg | du; kDw: dw_up
+  int64_t ld_out0, ld_out1;
+};
+
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896340736f));
+}
+
+// The activation of g and its slope.  GELU in its tanh form is g sigmoid(2 z); beyond |g| = 16 the sigmoid is 0 or 1 to the
+// last bit, and the clamp keeps z and its slope finite (a NaN passes it).
+template <int ACT>
+__device__ __forceinline__ void activate(float g, float& a, float& slope) {
+  if constexpr (ACT == MOSAIC_SILU) {
+    const float s = sigmoid(g);
+    a = g * s;
+    slope = s * (1.0f + g * (1.0f - s));
+  } else {
+    const float c = g > 16.0f ? 16.0f : g < -16.0f ? -16.0f : g;
+    constexpr float k2 = 1.59576912160573081f;   // 2 sqrt(2 / pi)
+    const float s = sigmoid(k2 * c * (1.0f + 0.044715f * c * c));
+    a = g * s;
+    slope = s * (1.0f + c * (1.0f - s) * k2 * (1.0f + 0.134145f * c * c));
+  }
+}
+
+// Copies of one operand's K-step into LDS, 16 bytes a lane, through a buffer descriptor whose base moves with the step.
+// Along K (rows of 64 consecutive k, 128 bytes): the eight 16-byte pieces of a row lie at piece ^ (row / 2 % 8), so that the
+// 16 rows of a fragment read spread over the banks.
+// Across K (KROW; rows of one k, ROWS consecutive columns): the 32-byte pieces (16 columns) of a row lie at piece ^ turn(k)
+// for the transposing reads, of which 32 lanes take 8 k at once.
+template <int ROWS, bool KROW>
+struct Copier {
+  static constexpr int kCopies = ROWS * 128 / (kThreads * 16);
+  uint32_t offset[kCopies];   // of this lane's piece within the step, or kOutside for a row or column past the end
+  int at[kCopies];            // its k
+
+  static __device__ __forceinline__ int turn(int k) {
+    if (ROWS >= 128) return (k & 3) | (k >> 3 & 1) << 2;
+    return (k >> 1 & 1) | (k >> 3 & 1) << 1;   // rows of 128 bytes: two of them span the banks
+  }
+
+  __device__ __forceinline__ void place(int wave, int lane, int64_t ld, int64_t valid) {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int byte = (wave * kCopies + i) * 1024 + lane * 16;
+      if constexpr (KROW) {
+        const int k = byte / (ROWS * 2), piece = byte % (ROWS * 2) / 16;
+        const int col = ((piece >> 1) ^ turn(k)) * 16 + (piece & 1) * 8;
+        at[i] = k;
+        offset[i] = col < valid ? (uint32_t)(k * (uint32_t)ld + col * 2) : kOutside;
+      } else {
+        const int row = byte / 128, piece = byte % 128 / 16;
+        const int k = (piece ^ (row >> 1 & 7)) * 8;
+        at[i] = k;
+        offset[i] = row < valid ? (uint32_t)(row * (uint32_t)ld + k * 2) : kOutside;
+      }
+    }
+  }
+
+  // `left`: k from this step on; pieces at or past it become zeros.
+  __device__ __forceinline__ void issue(const char* base, char* lds, int wave, int left) const {
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass has no buffer descriptors: it would drop the kernels' stubs
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, kOutside, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(lds + (wave * kCopies + i) * 1024), 16,
+                                               at[i] < left ? offset[i] : kOutside, 0, 0, 0);
+#endif
+  }
+};
+
+// Fragment of 16 rows, k = 32 kk + 8 (lane / 16) .. + 7, rows from `row` on.
+template <int ROWS, bool KROW>
+__device__ __forceinline__ bf16x8_t fragment(const char* lds, int row, int kk, int lane) {
+  if constexpr (KROW) {
+    const int g = lane >> 4, i = lane & 15;
+    const int k = 32 * kk + 8 * g + (i >> 2);
+    const int piece = (row >> 4) ^ Copier<ROWS, true>::turn(8 * g + (i >> 2));
+    const char* at = lds + k * (ROWS * 2) + piece * 32 + (i & 3) * 8;
+    const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)at);
+    const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(at + 4 * ROWS * 2));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  } else {
+    const int i = lane & 15;
+    const char* at = lds + (row + i) * 128 + (((4 * kk + (lane >> 4)) ^ (i >> 1)) * 16);
+    return *reinterpret_cast<const bf16x8_t*>(at);
+  }
+}
+
+template <int MODE, int QB, int ACT>
+__global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
+  constexpr bool kGated = MODE == kForward || MODE == kRecompute;
+  constexpr bool kRowP = !kGated, kRowQ = MODE == kDw;
+  constexpr int kTileQ = 64 * QB, kBytesQ = kTileQ * kStepK * 2, kSlot = kBytesP + kBytesQ;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * kSlot];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wp = wave >> 2, wq = wave & 3;
+
+  // Workgroup b runs on XCD b % 8; every XCD gets a run of tiles, and within it panels of 8 Q tiles, so that what is in
+  // flight behind one L2 shares both operands.
+  const int n = a.tiles_p * a.tiles_q * a.splits;
+  const int b = (int)blockIdx.x, x = b % kXcds;
+  const int id = x * (n / kXcds) + (x < n % kXcds ? x : n % kXcds) + b / kXcds;
+  const int split = id / (a.tiles_p * a.tiles_q), tile = id % (a.tiles_p * a.tiles_q);
+  constexpr int kPanel = 8;
+  const int panel = tile / (kPanel * a.tiles_p);
+  const int deep = a.tiles_q - panel * kPanel < kPanel ? a.tiles_q - panel * kPanel : kPanel;
+  const int in_panel = tile - panel * kPanel * a.tiles_p;
+  const int tp = in_panel / deep;
+  const int64_t tq = panel * kPanel + in_panel % deep;
+
+  const int p_row = tp * (kGated ? kTileP / 2 : kTileP);   // first P row; gated: first feature
+  const int64_t q_row = tq * kTileQ;
+  const char* p_base[2];
+  const char* q_base;
+  Copier<kTileP, kRowP> cp;
+  Copier<kTileQ, kRowQ> cq;
+  if constexpr (kGated) {   // waves 0..3 copy gate rows (LDS rows 0..127), waves 4..7 the up rows
+    p_base[0] = (wp == 0 ? a.p0 : a.p1) + p_row * a.ld_p;
+    p_base[1] = p_base[0];
+    cp.place(wave & 3, lane, a.ld_p, a.rows_p - p_row);
+  } else {
+    p_base[0] = a.p0 + (int64_t)p_row * 2;
+    p_base[1] = MODE == kDx ? a.p1 + (int64_t)p_row * 2 : p_base[0];
+    cp.place(wave, lane, a.ld_p, a.rows_p - p_row);
+  }
+  q_base = kRowQ ? a.q + q_row * 2 : a.q + q_row * a.ld_q;
+  cq.place(wave, lane, a.ld_q, a.rows_q - q_row);
+
+  const int seg_steps = (int)((a.depth + kStepK - 1) / kStepK);
+  const int all_steps = MODE == kDx ? 2 * seg_steps : seg_steps;
+  const int step0 = (int)((int64_t)all_steps * split / a.splits);
+  const int step1 = (int)((int64_t)all_steps * (split + 1) / a.splits);
+
+  auto copy = [&](int step) {
+    char* slot = smem + ((step - step0) & 1) * kSlot;
+    const int seg = MODE == kDx && step >= seg_steps ? 1 : 0;
+    const int64_t k = (int64_t)(step - seg * seg_steps) * kStepK;
+    const int left = a.depth - k < kStepK ? (int)(a.depth - k) : kStepK;
+    if constexpr (kGated) cp.issue(p_base[0] + k * 2, slot + wp * (kBytesP / 2), wave & 3, left);
+    else cp.issue(p_base[seg] + k * a.ld_p, slot, wave, left);
+    cq.issue(q_base + (kRowQ ? k * a.ld_q : (k + (int64_t)seg * a.depth) * 2), slot + kBytesP, wave, left);
+  };
+
+  f32x4_t acc[8][QB];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+#pragma unroll
+    for (int j = 0; j < QB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  // LDS row of this wave's P block i: gated, four gate blocks and the up blocks of the same features.
+  auto p_block = [&](int i) { return kGated ? (i >> 2) * 128 + wp * 64 + (i & 3) * 16 : wp * 128 + i * 16; };
+
+  if (step0 < step1) copy(step0);
+  for (int step = step0; step < step1; ++step) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();   // this step has arrived, and nobody reads the other slot any more
+    if (step + 1 < step1) copy(step + 1);
+    const char* slot = smem + ((step - step0) & 1) * kSlot;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      bf16x8_t fp[8], fq[QB];
+#pragma unroll
+      for (int j = 0; j < QB; ++j) fq[j] = fragment<kTileQ, kRowQ>(slot + kBytesP, wq * 16 * QB + j * 16, kk, lane);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) fp[i] = fragment<kTileP, kRowP>(slot, p_block(i), kk, lane);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int j = 0; j < QB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
+      }
+    }
+  }
+
+  // Accumulator register r of a lane: P row 4 (lane / 16) + r, Q row lane % 16 of the block.
+  const int sub = 4 * (lane >> 4);
+#pragma unroll
+  for (int j = 0; j < QB; ++j) {
+    const int64_t q = q_row + wq * 16 * QB + j * 16 + (lane & 15);
+    if (q >= a.rows_q) continue;
+    if constexpr (kGated) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int f = p_row + wp * 64 + i * 16 + sub;
+        if (f >= a.rows_p) continue;
+        bf16x4_t o;
+        if constexpr (MODE == kForward) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float act, slope;
+            activate<ACT>(acc[i][j][r], act, slope);
+            o[r] = (__bf16)(act * acc[i + 4][j][r]);
+          }
+          *reinterpret_cast<bf16x4_t*>(a.out0 + q * a.ld_out0 + (int64_t)f * 2) = o;
+        } else {
+          const bf16x4_t d = *reinterpret_cast<const bf16x4_t*>(a.dout + q * a.ld_dout + (int64_t)f * 2);
+          bf16x4_t dg, du;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float act, slope;
+            const float u = acc[i + 4][j][r], dr = (float)d[r];
+            activate<ACT>(acc[i][j][r], act, slope);
+            o[r] = (__bf16)(act * u);
+            dg[r] = (__bf16)(dr * u * slope);
+            du[r] = (__bf16)(dr * act);
+          }
+          if (a.out0 != nullptr) *reinterpret_cast<bf16x4_t*>(a.out0 + q * a.ld_out0 + (int64_t)f * 2) = o;
+          *reinterpret_cast<bf16x4_t*>(a.out1 + q * a.ld_out1 + (int64_t)f * 2) = dg;
+          *reinterpret_cast<bf16x4_t*>(a.out1 + q * a.ld_out1 + ((int64_t)a.F + f) * 2) = du;
+        }
+      }
+    } else {
+      char* row;
+      if constexpr (MODE == kDx) row = a.out0 + ((int64_t)split * a.rows_q + q) * a.ld_out0;
+      else row = q < a.F ? a.out0 + q * a.ld_out0 : a.out1 + (q - a.F) * a.ld_out0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = p_row + wp * 128 + i * 16 + sub;
+        if (c >= a.rows_p) continue;
+        if (a.f32) {
+          f32x4_t* to = reinterpret_cast<f32x4_t*>(row + (int64_t)c * 4);
+          *to = a.accumulate ? *to + acc[i][j] : acc[i][j];
+        } else {
+          bf16x4_t o;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[r] = (__bf16)acc[i][j][r];
+          *reinterpret_cast<bf16x4_t*>(row + (int64_t)c * 2) = o;
+        }
+      }
+    }
+  }
+}
+
+// Adds the parts of dx in their order and rounds once.
+__global__ __launch_bounds__(256) void ffn_join_kernel(const float* __restrict__ partials, int splits, int64_t T, int d,
+                                                       __bf16* __restrict__ dx, int64_t ld) {
+  const int per_row = d / 8;
+  const int64_t all = T * per_row;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
+    const int64_t t = e / per_row;
+    const int c = (int)(e - t * per_row) * 8;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < splits; ++k) {
+      float v[8];
+      load8(partials + ((int64_t)k * T + t) * d + c, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] += v[i];
+    }
+    store8(dx + t * ld + c, s);
+  }
+}
+
+int64_t tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
+
+// Rows of one launch: at most 2^12 row tiles by 2^10 column tiles of 512 threads stay under 2^32 threads.
+constexpr int64_t kLaunchRows = (int64_t)1 << 20;
+static_assert((kLaunchRows / 256) * (MOSAIC_MAX_ROW / 128) * kThreads < (int64_t)1 << 32, "threads of a launch");
+
+template <int MODE, int ACT>
+int launch_gemm(GemmArgs a, hipStream_t stream) {
+  a.tiles_p = (int32_t)tiles(a.rows_p, MODE == kForward || MODE == kRecompute ? kTileP / 2 : kTileP);
+  // Few rows take a narrow tile.
+  const int qb = a.rows_q <= 64 ? 1 : a.rows_q <= 128 ? 2 : 4;
+  const int64_t tiles_q = tiles(a.rows_q, 64 * qb);
+  a.tiles_q = (int32_t)tiles_q;
+  const dim3 grid((unsigned)(tiles_q * a.tiles_p * a.splits));
+  if (qb == 1) return launch_kernel(ffn_gemm_kernel<MODE, 1, ACT>, grid, dim3(kThreads), stream, a);
+  if (qb == 2) return launch_kernel(ffn_gemm_kernel<MODE, 2, ACT>, grid, dim3(kThreads), stream, a);
+  return launch_kernel(ffn_gemm_kernel<MODE, 4, ACT>, grid, dim3(kThreads), stream, a);
+}
+
+template <int MODE>
+int launch_gated(const GemmArgs& a, int activation, hipStream_t stream) {
+  return activation == MOSAIC_SILU ? launch_gemm<MODE, MOSAIC_SILU>(a, stream)
+                                   : launch_gemm<MODE, MOSAIC_GELU_TANH>(a, stream);
+}
+
+}  // namespace
+
+int32_t ffn_dx_splits(int64_t T, int32_t d, int32_t F) {
+  const int64_t units = tiles(T, 256) * tiles(d, kTileP);
+  const int64_t steps = 2 * tiles(F, kStepK);
+  if (T == 0 || units >= 192) return 1;
+  const int64_t s = 256 / units;
+  const int64_t most = steps / 8 < 1 ? 1 : steps / 8;
+  return (int32_t)(s > most ? most : s);
+}
+
+int launch_gated_ffn_forward(const FfnForwardArgs& f, hipStream_t stream) {
+  GemmArgs a = {};
+  a.p0 = static_cast<const char*>(f.w_gate);
+  a.p1 = static_cast<const char*>(f.w_up);
+  a.ld_p = f.ld_w * 2;
+  a.ld_q = f.ld_x * 2;
+  a.rows_p = f.F;
+  a.depth = f.d;
+  a.splits = 1;
+  a.F = f.F;
+  a.ld_out0 = f.ld_out * 2;
+  for (int64_t t = 0; t < f.T; t += kLaunchRows) {
+    a.rows_q = f.T - t < kLaunchRows ? f.T - t : kLaunchRows;
+    a.q = static_cast<const char*>(f.x) + t * a.ld_q;
+    a.out0 = static_cast<char*>(f.out) + t * a.ld_out0;
+    if (launch_gated<kForward>(a, f.activation, stream) != 0) return -1;
+  }
+  return 0;
+}
+
+int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
+  const int64_t ld_grads = (int64_t)f.F * 4;
+  for (int64_t t = 0; t < f.T; t += kLaunchRows) {
+    GemmArgs a = {};
+    a.p0 = static_cast<const char*>(f.w_gate);
+    a.p1 = static_cast<const char*>(f.w_up);
+    a.ld_p = f.ld_w * 2;
+    a.ld_q = f.ld_x * 2;
+    a.rows_q = f.T - t < kLaunchRows ? f.T - t : kLaunchRows;
+    a.q = static_cast<const char*>(f.x) + t * a.ld_q;
+    a.rows_p = f.F;
+    a.depth = f.d;
+    a.splits = 1;
+      a.F = f.F;
+    a.ld_dout = f.ld_dout * 2;
+    a.dout = static_cast<const char*>(f.dout) + t * a.ld_dout;
+    a.ld_out0 = f.ld_out * 2;
+    a.out0 = f.out == nullptr ? nullptr : static_cast<char*>(f.out) + t * a.ld_out0;
+    a.ld_out1 = ld_grads;
+    a.out1 = static_cast<char*>(f.grads) + t * ld_grads;
+    if (launch_gated<kRecompute>(a, f.activation, stream) != 0) return -1;
+  }
+  const int32_t splits = ffn_dx_splits(f.T, f.d, f.F);
+  for (int64_t t = 0; f.dx != nullptr && t < f.T; t += kLaunchRows) {
+    GemmArgs a = {};
+    a.p0 = static_cast<const char*>(f.w_gate);
+    a.p1 = static_cast<const char*>(f.w_up);
+    a.ld_p = f.ld_w * 2;
+    a.ld_q = ld_grads;
+    a.rows_q = f.T - t < kLaunchRows ? f.T - t : kLaunchRows;
+    a.q = static_cast<const char*>(f.grads) + t * ld_grads;
+    a.rows_p = f.d;
+    a.depth = f.F;
+    a.splits = splits;
+    a.f32 = splits > 1;      // then all rows are in one launch
+    a.ld_out0 = a.f32 ? (int64_t)f.d * 4 : f.ld_dx * 2;
+    a.out0 = a.f32 ? reinterpret_cast<char*>(f.partials) : static_cast<char*>(f.dx) + t * a.ld_out0;
+    if (launch_gemm<kDx, 0>(a, stream) != 0) return -1;
+  }
+  if (f.dx != nullptr && splits > 1) {
+    const int64_t blocks = tiles(f.T * (f.d / 8), 256);
+    if (launch_kernel(ffn_join_kernel, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), stream, f.partials,
+                      (int)splits, f.T, f.d, static_cast<__bf16*>(f.dx), f.ld_dx) != 0)
+      return -1;
+  }
+  if (f.dw_gate != nullptr) {
+    GemmArgs a = {};
+    a.p0 = static_cast<const char*>(f.x);
+    a.p1 = a.p0;
+    a.q = static_cast<const char*>(f.grads);
+    a.ld_p = f.ld_x * 2;
+    a.ld_q = (int64_t)f.F * 4;
+    a.rows_q = 2 * (int64_t)f.F;
+    a.rows_p = f.d;
+    a.depth = f.T;
+    a.splits = 1;
+    a.F = f.F;
+    a.f32 = f.dw_f32;
+    a.accumulate = f.accumulate;
+    a.out0 = static_cast<char*>(f.dw_gate);
+    a.out1 = static_cast<char*>(f.dw_up);
+    a.ld_out0 = f.ld_dw * (f.dw_f32 ? 4 : 2);
+    if (launch_gemm<kDw, 0>(a, stream) != 0) return -1;
+  }
+  return 0;
+}
+
+}  // namespace mosaic

@@ -1,0 +1,401 @@
+// Root-mean-square norm with the residual's addition and an 8-bit output, its backward pass, and activations stored
+// in 8 bits.  All of it is bound by memory: every element is read once and written once, a row stays in registers between
+// the sum of its squares and its use.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "mosaic_layer_internal.h"
+
+namespace mosaic {
+namespace {
+
+// ---- 8 bits: a lane holds 8 consecutive columns, so a group is 4, 8 or 16 neighbouring lanes.
+
+constexpr float kTiny = 0x1p-112f;   // below it top / a could overflow, and scales would lie among the denormals
+
+// Largest magnitude over the lanes of a group, as bits: the order of non-negative floats is that of their bits, and every
+// NaN and infinity stays at or above 0x7f800000.
+__device__ __forceinline__ uint32_t group_max_bits(const float (&v)[8], int lanes) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
+    m = b > m ? b : m;
+  }
+  for (int x = 1; x < lanes; x <<= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)m, x, 64);
+    m = o > m ? o : m;
+  }
+  return m;
+}
+
+// Eight values of a group whose largest magnitude has the bits `m`, as bytes; *scale is what restores them.
+__device__ __forceinline__ uint2 to_q8(const float (&v)[8], uint32_t m, int format, float* scale) {
+  const float top = format == MOSAIC_INT8 ? 127.0f : 448.0f;
+  const float a = __uint_as_float(m);
+  const bool finite = m < 0x7f800000u, stored = finite && a >= kTiny;
+  *scale = finite ? (stored ? a / top : 0.0f) : __builtin_nanf("");
+  if (!stored) return uint2{0u, 0u};
+  const float up = top / a;
+  uint2 w;
+  if (format == MOSAIC_INT8) {
+    uint32_t b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = (uint32_t)(int)__builtin_rintf(v[i] * up) & 0xffu;
+    w.x = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+    w.y = b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24;
+  } else {
+    int lo = 0, hi = 0;   // to nearest, ties to even; |v * up| <= 448 (1 + 2^-23), which rounds to 448
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * up, v[1] * up, lo, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * up, v[3] * up, lo, true);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * up, v[5] * up, hi, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * up, v[7] * up, hi, true);
+    w.x = (uint32_t)lo;
+    w.y = (uint32_t)hi;
+  }
+  return w;
+}
+
+// What eight stored bytes stand for: value * scale, rounded to bf16 (so that a backward pass on the matrix cores and one
+// in 32 bits see the same numbers).
+__device__ __forceinline__ void from_q8(uint2 w, float scale, int format, float (&v)[8]) {
+  if (format == MOSAIC_INT8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = (float)(int8_t)(w.x >> (8 * i));
+      v[i + 4] = (float)(int8_t)(w.y >> (8 * i));
+    }
+  } else {
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.x, true);
+    const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.y, false), e = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.y, true);
+    v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1];
+    v[4] = c[0]; v[5] = c[1]; v[6] = e[0]; v[7] = e[1];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)(__bf16)(v[i] * scale);
+}
+
+__device__ __forceinline__ void store_q8(const mosaic_q8_rows& q, int group_shift, int64_t row, int c, bool in,
+                                         const float (&v)[8]) {
+  const int lanes = 1 << (group_shift - 3);
+  const uint32_t m = group_max_bits(v, lanes);
+  float scale;
+  const uint2 w = to_q8(v, m, q.format, &scale);
+  if (!in) return;
+  *reinterpret_cast<uint2*>(static_cast<uint8_t*>(q.values) + row * q.ld_values + c) = w;
+  if ((c & ((1 << group_shift) - 1)) == 0) q.scales[row * q.ld_scales + (c >> group_shift)] = scale;
+}
+
+__device__ __forceinline__ int group_shift_of(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
+
+__device__ __forceinline__ void load_q8(const mosaic_q8_rows& q, int group_shift, int64_t row, int c, float (&v)[8]) {
+  const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(q.values) + row * q.ld_values + c);
+  from_q8(w, q.scales[row * q.ld_scales + (c >> group_shift)], q.format, v);
+}
+
+__device__ __forceinline__ void load_gamma(const void* gamma, int f32, int c, float (&v)[8]) {
+  if (f32) load8(static_cast<const float*>(gamma) + c, v);
+  else load8(static_cast<const __bf16*>(gamma) + c, v);
+}
+
+// Sum over the R lanes of a row.  R > 64: over the block's waves through `lds`, whose half `turn` is this call's (the
+// barrier of the next call stands between a half's use and its next).
+template <int R, int N>
+__device__ __forceinline__ void row_sum(float (&s)[N], float* lds, int turn) {
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] += __shfl_xor(s[i], x, 64);
+  }
+  if constexpr (R > 64) {
+    constexpr int W = R / 64;
+    float* at = lds + turn * (W * N);
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) at[i * W + (threadIdx.x >> 6)] = s[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) t += at[i * W + w];
+      s[i] = t;
+    }
+  }
+}
+
+// R lanes hold a row (a wave, or a block of four), NV vectors of 8 columns each.
+constexpr int kThreads = 256;
+
+template <typename S, int R, int NV>
+__global__ __launch_bounds__(kThreads) void rmsnorm_forward_kernel(const NormForwardArgs p) {
+  constexpr int kRows = kThreads / R;
+  __shared__ float lds[2 * (R > 64 ? R / 64 : 1)];
+  const int lane = threadIdx.x % R;
+  int64_t n = p.T;
+  if (p.idx != nullptr) {
+    n = *p.count;
+    if (n > p.max_rows) n = p.max_rows;
+  }
+  const int shift = group_shift_of(p.q8.group);
+  int turn = 0;
+  for (int64_t j = (int64_t)blockIdx.x * kRows + threadIdx.x / R; j < n; j += (int64_t)gridDim.x * kRows) {
+    int64_t t = j;
+    if (p.idx != nullptr) {
+      t = p.idx[j];
+      if (t < 0 || t >= p.T) continue;   // the same for all lanes of a row, and so, R > 64, for the block
+    }
+    float h[NV][8];
+    float ss[1] = {0.f};
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * R + lane) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[v][i] = 0.f;
+      if (c < p.d && p.residual != nullptr) load8(static_cast<const S*>(p.residual) + t * p.ld_residual + c, h[v]);
+    }
+    if (p.x != nullptr) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int c = (v * R + lane) * 8;
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (c < p.d) load8(static_cast<const __bf16*>(p.x) + t * p.ld_x + c, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[v][i] += x[i];
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * R + lane) * 8;
+      if (c < p.d && p.sum != nullptr) store8(static_cast<S*>(p.sum) + t * p.ld_sum + c, h[v]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss[0] = __builtin_fmaf(h[v][i], h[v][i], ss[0]);
+    }
+    row_sum<R>(ss, lds, turn);
+    turn ^= 1;
+    const float rstd = 1.0f / __builtin_sqrtf(ss[0] / (float)p.d + p.eps);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * R + lane) * 8;
+      const bool in = c < p.d;
+      float g[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (in) load_gamma(p.gamma, p.gamma_f32, c, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[v][i] = in ? h[v][i] * rstd * g[i] : 0.f;
+      if (in && p.y != nullptr) store8(static_cast<__bf16*>(p.y) + t * p.ld_y + c, h[v]);
+      if (p.q8.values != nullptr) store_q8(p.q8, shift, t, c, in, h[v]);
+    }
+  }
+}
+
+enum { kFromBf16 = 0, kFromF32 = 1, kFromQ8 = 2 };
+
+// The rows are dealt to gridDim.x * kRows groups of R lanes, each of which sums its rows' dy * n per column in registers
+// and leaves one partial sum; norm_gamma_kernel adds those up.  Rows in turn, not in blocks: the same sums on every call.
+template <int FROM, typename S, int R, int NV>
+__global__ __launch_bounds__(kThreads) void rmsnorm_backward_kernel(const NormBackwardArgs p) {
+  constexpr int kRows = kThreads / R;
+  __shared__ float lds[4 * (R > 64 ? R / 64 : 1)];
+  const int lane = threadIdx.x % R;
+  const int64_t first = (int64_t)blockIdx.x * kRows + threadIdx.x / R;
+  const int shift = FROM == kFromQ8 ? group_shift_of(p.q8.group) : 0;
+  float dgamma[NV][8];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dgamma[v][i] = 0.f;
+  }
+  int turn = 0;
+  for (int64_t t = first; t < p.T; t += (int64_t)gridDim.x * kRows) {
+    float h[NV][8], dy[NV][8];
+    float s[2] = {0.f, 0.f};   // sums of h^2 and of gamma dy h
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * R + lane) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { h[v][i] = 0.f; dy[v][i] = 0.f; }
+      if (c < p.d) {
+        load8(static_cast<const __bf16*>(p.dy) + t * p.ld_dy + c, dy[v]);
+        if constexpr (FROM == kFromBf16) load8(static_cast<const __bf16*>(p.h) + t * p.ld_h + c, h[v]);
+        if constexpr (FROM == kFromF32) load8(static_cast<const float*>(p.h) + t * p.ld_h + c, h[v]);
+        if constexpr (FROM == kFromQ8) load_q8(p.q8, shift, t, c, h[v]);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * R + lane) * 8;
+      float g[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (c < p.d) load_gamma(p.gamma, p.gamma_f32, c, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        s[0] = __builtin_fmaf(h[v][i], h[v][i], s[0]);
+        s[1] = __builtin_fmaf(g[i] * dy[v][i], h[v][i], s[1]);
+      }
+    }
+    row_sum<R>(s, lds, turn);
+    turn ^= 1;
+    const float rstd = 1.0f / __builtin_sqrtf(s[0] / (float)p.d + p.eps);
+    const float along = s[1] / (float)p.d * rstd;   // mean of c n
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * R + lane) * 8;
+      if (c >= p.d) continue;
+      float g[8], out[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      load_gamma(p.gamma, p.gamma_f32, c, g);
+      if (p.dsum_in != nullptr) load8(static_cast<const S*>(p.dsum_in) + t * p.ld_dsum_in + c, out);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float n = h[v][i] * rstd;
+        out[i] = __builtin_fmaf(rstd, __builtin_fmaf(-n, along, g[i] * dy[v][i]), out[i]);
+        dgamma[v][i] = __builtin_fmaf(dy[v][i], n, dgamma[v][i]);
+      }
+      if (p.dsum != nullptr) store8(static_cast<S*>(p.dsum) + t * p.ld_dsum + c, out);
+    }
+  }
+  if (p.dgamma == nullptr) return;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (v * R + lane) * 8;
+    if (c < p.d) store8(p.partials + first * p.d + c, dgamma[v]);
+  }
+}
+
+// Adds `n` partial rows: 16 lanes of four columns, 16 strips of rows, joined in LDS.
+__global__ __launch_bounds__(256) void norm_gamma_kernel(const float* __restrict__ partials, int n, int d, int accumulate,
+                                                         float* __restrict__ dgamma) {
+  __shared__ f32x4_t strip[16][16];
+  const int q = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+  const int c = ((int)blockIdx.x * 16 + q) * 4;
+  f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+  if (c < d) {
+#pragma unroll 4
+    for (int r = r0; r < n; r += 16) s += *reinterpret_cast<const f32x4_t*>(partials + (int64_t)r * d + c);
+  }
+  strip[r0][q] = s;
+  __syncthreads();
+  if (r0 == 0 && c < d) {
+    for (int k = 1; k < 16; ++k) s += strip[k][q];
+    f32x4_t* out = reinterpret_cast<f32x4_t*>(dgamma + c);
+    *out = accumulate ? *out + s : s;
+  }
+}
+
+// A wave per row and turn; `padded` columns so that the lanes of a group all take part in its maximum.
+template <typename S>
+__global__ __launch_bounds__(256) void checkpoint_store_kernel(const S* __restrict__ x, int64_t ld_x, int64_t T, int d,
+                                                               const mosaic_q8_rows q8) {
+  const int shift = group_shift_of(q8.group);
+  const int padded = (d + q8.group - 1) >> shift << shift;
+  for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < T; t += (int64_t)gridDim.x * 4) {
+#pragma unroll 4
+    for (int c = (threadIdx.x & 63) * 8; c < padded; c += 512) {
+      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (c < d) load8(x + t * ld_x + c, v);
+      store_q8(q8, shift, t, c, c < d, v);
+    }
+  }
+}
+
+template <typename S>
+__global__ __launch_bounds__(256) void checkpoint_load_kernel(const mosaic_q8_rows q8, int64_t T, int d, S* __restrict__ out,
+                                                              int64_t ld_out) {
+  const int shift = group_shift_of(q8.group);
+  for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < T; t += (int64_t)gridDim.x * 4) {
+#pragma unroll 4
+    for (int c = (threadIdx.x & 63) * 8; c < d; c += 512) {
+      float v[8];
+      load_q8(q8, shift, t, c, v);
+      store8(out + t * ld_out + c, v);
+    }
+  }
+}
+
+constexpr int64_t kMostBlocks = 1 << 20;   // beyond it the blocks take further rows (a launch has under 2^32 threads)
+unsigned blocks_for(int64_t rows, int rows_per_block) {
+  const int64_t b = (rows + rows_per_block - 1) / rows_per_block;
+  return (unsigned)(b > kMostBlocks ? kMostBlocks : b);
+}
+
+// Lanes a row.
+int lanes_for(int32_t d) { return d <= 1024 ? 64 : 256; }
+
+template <typename S, int R, int NV>
+int forward_as(const NormForwardArgs& a, int64_t rows, hipStream_t stream) {
+  return launch_kernel(rmsnorm_forward_kernel<S, R, NV>, dim3(blocks_for(rows, kThreads / R)),
+                       dim3(kThreads), stream, a);
+}
+
+template <typename S>
+int forward_of(const NormForwardArgs& a, hipStream_t stream) {
+  const int64_t rows = a.idx != nullptr ? a.max_rows : a.T;
+  const int32_t d = a.d;
+  if (d <= 512) return forward_as<S, 64, 1>(a, rows, stream);
+  if (d <= 1024) return forward_as<S, 64, 2>(a, rows, stream);
+  if (d <= 2048) return forward_as<S, 256, 1>(a, rows, stream);
+  if (d <= 4096) return forward_as<S, 256, 2>(a, rows, stream);
+  if (d <= 8192) return forward_as<S, 256, 4>(a, rows, stream);
+  return forward_as<S, 256, 8>(a, rows, stream);
+}
+
+template <int FROM, typename S, int R, int NV>
+int backward_as(const NormBackwardArgs& a, int64_t partials, hipStream_t stream) {
+  constexpr int kRows = kThreads / R;
+  return launch_kernel(rmsnorm_backward_kernel<FROM, S, R, NV>, dim3((unsigned)(partials / kRows)), dim3(kThreads),
+                       stream, a);
+}
+
+template <int FROM, typename S>
+int backward_of(const NormBackwardArgs& a, int64_t partials, hipStream_t stream) {
+  const int32_t d = a.d;
+  if (d <= 512) return backward_as<FROM, S, 64, 1>(a, partials, stream);
+  if (d <= 1024) return backward_as<FROM, S, 64, 2>(a, partials, stream);
+  if (d <= 2048) return backward_as<FROM, S, 256, 1>(a, partials, stream);
+  if (d <= 4096) return backward_as<FROM, S, 256, 2>(a, partials, stream);
+  if (d <= 8192) return backward_as<FROM, S, 256, 4>(a, partials, stream);
+  return backward_as<FROM, S, 256, 8>(a, partials, stream);
+}
+
+}  // namespace
+
+int launch_rmsnorm_forward(const NormForwardArgs& a, bool stream_f32, hipStream_t stream) {
+  return stream_f32 ? forward_of<float>(a, stream) : forward_of<__bf16>(a, stream);
+}
+
+// Partial sums of dgamma: at least four rows each, so that they cost a fraction of the rows themselves.
+int64_t norm_backward_partials(int64_t T, int32_t d) {
+  const int64_t rows = kThreads / lanes_for(d);
+  int64_t n = (T + 3) / 4;
+  n = n > 1024 ? 1024 : n;
+  return (n + rows - 1) / rows * rows;
+}
+
+int launch_rmsnorm_backward(const NormBackwardArgs& a, bool stream_f32, hipStream_t stream) {
+  const int64_t partials = norm_backward_partials(a.T, a.d);
+  int rc = 0;
+  if (a.T > 0) {
+    if (a.h == nullptr) rc = stream_f32 ? backward_of<kFromQ8, float>(a, partials, stream) : backward_of<kFromQ8, __bf16>(a, partials, stream);
+    else if (stream_f32) rc = backward_of<kFromF32, float>(a, partials, stream);
+    else rc = backward_of<kFromBf16, __bf16>(a, partials, stream);
+  }
+  if (rc != 0 || a.dgamma == nullptr) return rc;
+  return launch_kernel(norm_gamma_kernel, dim3((unsigned)((a.d + 63) / 64)), dim3(256), stream, a.partials, (int)partials,
+                       a.d, a.accumulate, a.dgamma);
+}
+
+int launch_checkpoint_store(const void* x, bool f32, int64_t ld_x, int64_t T, int32_t d, const mosaic_q8_rows& q8,
+                            hipStream_t stream) {
+  const dim3 grid(blocks_for(T, 4)), block(256);
+  return f32 ? launch_kernel(checkpoint_store_kernel<float>, grid, block, stream, static_cast<const float*>(x), ld_x, T, d, q8)
+             : launch_kernel(checkpoint_store_kernel<__bf16>, grid, block, stream, static_cast<const __bf16*>(x), ld_x, T, d, q8);
+}
+
+int launch_checkpoint_load(const mosaic_q8_rows& q8, int64_t T, int32_t d, void* out, bool f32, int64_t ld_out,
+                           hipStream_t stream) {
+  const dim3 grid(blocks_for(T, 4)), block(256);
+  return f32 ? launch_kernel(checkpoint_load_kernel<float>, grid, block, stream, q8, T, d, static_cast<float*>(out), ld_out)
+             : launch_kernel(checkpoint_load_kernel<__bf16>, grid, block, stream, q8, T, d, static_cast<__bf16*>(out), ld_out);
+}
+
+}  // namespace mosaic
