@@ -171,25 +171,6 @@ def lib():
         L.mosaic_graph_plan.argtypes = [p, p, ctypes.c_int, p, ctypes.c_int, p, i64, ctypes.POINTER(MosaicPlanSummary)]
         L.mosaic_graph_search.restype = ctypes.c_int
         L.mosaic_graph_search.argtypes = [p, p, ctypes.c_int, i64, p, ctypes.c_int, ctypes.POINTER(MosaicPlanSummary), p]
-        q8, f32 = ctypes.POINTER(MosaicQ8Rows), ctypes.c_float
-        L.mosaic_checkpoint_store.restype = ctypes.c_int
-        L.mosaic_checkpoint_store.argtypes = [p, i32, i64, i64, i32, q8, p]
-        L.mosaic_checkpoint_load.restype = ctypes.c_int
-        L.mosaic_checkpoint_load.argtypes = [q8, i64, i32, p, i32, i64, p]
-        L.mosaic_rmsnorm_forward.restype = ctypes.c_int
-        L.mosaic_rmsnorm_forward.argtypes = [p, i64, p, i32, i64, p, i32, f32, i64, i32, p, p, i64, p, i64, p, i64, q8, p]
-        L.mosaic_rmsnorm_backward_workspace_bytes.restype = i64
-        L.mosaic_rmsnorm_backward_workspace_bytes.argtypes = [i64, i32]
-        L.mosaic_rmsnorm_backward.restype = ctypes.c_int
-        L.mosaic_rmsnorm_backward.argtypes = [p, i64, p, i64, q8, i32, p, i32, f32, i64, i32, p, i64, p, i64, p, i32, p, i64,
-                                              p]
-        L.mosaic_gated_ffn_forward.restype = ctypes.c_int
-        L.mosaic_gated_ffn_forward.argtypes = [p, i64, p, p, i64, i64, i32, i32, i32, p, i64, p]
-        L.mosaic_gated_ffn_backward_workspace_bytes.restype = i64
-        L.mosaic_gated_ffn_backward_workspace_bytes.argtypes = [i64, i32, i32, i32]
-        L.mosaic_gated_ffn_backward.restype = ctypes.c_int
-        L.mosaic_gated_ffn_backward.argtypes = [p, i64, p, i64, q8, p, p, i64, i64, i32, i32, i32, p, i64, p, i64, p, p, i32,
-                                                i64, i32, p, i64, p]
         _lib = L
     return _lib
 
@@ -355,6 +336,38 @@ def mosaic_mfma_probe(operands, sink, iters, num_wgs, stream=None) -> int:
 
 # ---- the layer work on either side of the pass (include/mosaic_layer.h)
 
+_layer_lib = None
+
+
+def _layer():
+    """lib(), with the prototypes of include/mosaic_layer.h."""
+    global _layer_lib
+    if _layer_lib is None:
+        L = lib()
+        p, i64, i32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
+        q8, f32 = ctypes.POINTER(MosaicQ8Rows), ctypes.c_float
+        L.mosaic_checkpoint_store.restype = ctypes.c_int
+        L.mosaic_checkpoint_store.argtypes = [p, i32, i64, i64, i32, q8, p]
+        L.mosaic_checkpoint_load.restype = ctypes.c_int
+        L.mosaic_checkpoint_load.argtypes = [q8, i64, i32, p, i32, i64, p]
+        L.mosaic_rmsnorm_forward.restype = ctypes.c_int
+        L.mosaic_rmsnorm_forward.argtypes = [p, i64, p, i32, i64, p, i32, f32, i64, i32, p, p, i64, p, i64, p, i64, q8, p]
+        L.mosaic_rmsnorm_backward_workspace_bytes.restype = i64
+        L.mosaic_rmsnorm_backward_workspace_bytes.argtypes = [i64, i32]
+        L.mosaic_rmsnorm_backward.restype = ctypes.c_int
+        L.mosaic_rmsnorm_backward.argtypes = [p, i64, p, i64, q8, i32, p, i32, f32, i64, i32, p, i64, p, i64, p, i32, p, i64,
+                                              p]
+        L.mosaic_gated_ffn_forward.restype = ctypes.c_int
+        L.mosaic_gated_ffn_forward.argtypes = [p, i64, p, p, i64, i64, i32, i32, i32, p, i64, p]
+        L.mosaic_gated_ffn_backward_workspace_bytes.restype = i64
+        L.mosaic_gated_ffn_backward_workspace_bytes.argtypes = [i64, i32, i32, i32]
+        L.mosaic_gated_ffn_backward.restype = ctypes.c_int
+        L.mosaic_gated_ffn_backward.argtypes = [p, i64, p, i64, q8, p, p, i64, i64, i32, i32, i32, p, i64, p, i64, p, p, i32,
+                                                i64, i32, p, i64, p]
+        _layer_lib = L
+    return _layer_lib
+
+
 _TYPES = {torch.bfloat16: BF16, torch.float32: F32}
 _FORMATS = {torch.int8: INT8, torch.float8_e4m3fn: E4M3}
 
@@ -408,7 +421,7 @@ def mosaic_checkpoint_store(x, q8, stream=None):
     """Rows of x (bf16 or float32 [T, d]) into 8 bits."""
     T, d = q8.shape
     ptr, ld = _rows(x, "x", T, d)
-    _check(lib().mosaic_checkpoint_store(ptr, _type_of(x, "x"), ld, T, d, q8._ref, _stream_ptr(stream)),
+    _check(_layer().mosaic_checkpoint_store(ptr, _type_of(x, "x"), ld, T, d, q8._ref, _stream_ptr(stream)),
            "mosaic_checkpoint_store")
 
 
@@ -416,7 +429,7 @@ def mosaic_checkpoint_load(q8, out, stream=None):
     """What 8-bit rows stand for, into out (bf16 or float32 [T, d])."""
     T, d = q8.shape
     ptr, ld = _rows(out, "out", T, d)
-    _check(lib().mosaic_checkpoint_load(q8._ref, T, d, ptr, _type_of(out, "out"), ld, _stream_ptr(stream)),
+    _check(_layer().mosaic_checkpoint_load(q8._ref, T, d, ptr, _type_of(out, "out"), ld, _stream_ptr(stream)),
            "mosaic_checkpoint_load")
 
 
@@ -442,14 +455,14 @@ def mosaic_rmsnorm_forward(x, residual, gamma, eps, y, sum=None, q8=None, idx=No
         max_rows = min(T, idx.numel()) if idx is not None else 0
     elif idx is not None and idx.numel() < max_rows:
         raise ValueError("idx holds fewer than max_rows entries")
-    _check(lib().mosaic_rmsnorm_forward(
+    _check(_layer().mosaic_rmsnorm_forward(
         p_x, ld_x, p_r, stream_type, ld_r, _vector(gamma, "gamma", d), _type_of(gamma, "gamma"), float(eps), T, d,
         _dev_ptr(idx, "idx", torch.int32), _dev_ptr(count, "count", torch.int32), max_rows, p_s, ld_s, p_y, ld_y,
         q8._ref if q8 is not None else None, _stream_ptr(stream)), "mosaic_rmsnorm_forward")
 
 
 def mosaic_rmsnorm_backward_workspace_bytes(T, d) -> int:
-    return int(lib().mosaic_rmsnorm_backward_workspace_bytes(T, d))
+    return int(_layer().mosaic_rmsnorm_backward_workspace_bytes(T, d))
 
 
 def mosaic_rmsnorm_backward(dy, h, gamma, eps, dsum, dgamma, workspace, dsum_in=None, accumulate=False, stream=None):
@@ -471,7 +484,7 @@ def mosaic_rmsnorm_backward(dy, h, gamma, eps, dsum, dgamma, workspace, dsum_in=
         stream_type = _TYPES[t]
     p_in, ld_in = _rows(dsum_in, "dsum_in", T, d)
     p_out, ld_out = _rows(dsum, "dsum", T, d)
-    _check(lib().mosaic_rmsnorm_backward(
+    _check(_layer().mosaic_rmsnorm_backward(
         p_dy, ld_dy, p_h, ld_h, q8._ref if q8 is not None else None, stream_type, _vector(gamma, "gamma", d),
         _type_of(gamma, "gamma"), float(eps), T, d, p_in, ld_in, p_out, ld_out,
         _vector(dgamma, "dgamma", d, torch.float32) if dgamma is not None else 0, int(bool(accumulate)),
@@ -497,12 +510,12 @@ def mosaic_gated_ffn_forward(x, w_gate, w_up, out, activation=ACT_SILU, stream=N
     p_x, ld_x = _rows(x, "x", T, d, torch.bfloat16)
     p_g, p_u, ld_w = _weights(w_gate, w_up)
     p_o, ld_o = _rows(out, "out", T, F, torch.bfloat16)
-    _check(lib().mosaic_gated_ffn_forward(p_x, ld_x, p_g, p_u, ld_w, T, d, F, int(activation), p_o, ld_o,
+    _check(_layer().mosaic_gated_ffn_forward(p_x, ld_x, p_g, p_u, ld_w, T, d, F, int(activation), p_o, ld_o,
                                           _stream_ptr(stream)), "mosaic_gated_ffn_forward")
 
 
 def mosaic_gated_ffn_backward_workspace_bytes(T, d, F, q8_input=False) -> int:
-    return int(lib().mosaic_gated_ffn_backward_workspace_bytes(T, d, F, int(bool(q8_input))))
+    return int(_layer().mosaic_gated_ffn_backward_workspace_bytes(T, d, F, int(bool(q8_input))))
 
 
 def mosaic_gated_ffn_backward(dout, x, w_gate, w_up, dx, dw_gate, dw_up, workspace, activation=ACT_SILU, out=None,
@@ -530,7 +543,7 @@ def mosaic_gated_ffn_backward(dout, x, w_gate, w_up, dx, dw_gate, dw_up, workspa
         if tuple(dw_gate.shape) != (F, d):
             raise ValueError(f"dw_gate must be [{F}, {d}], got {list(dw_gate.shape)}")
         p_dg, p_du, ld_dw = _weights(dw_gate, dw_up, dw_gate.dtype, ("dw_gate", "dw_up"))
-    _check(lib().mosaic_gated_ffn_backward(
+    _check(_layer().mosaic_gated_ffn_backward(
         p_do, ld_do, p_x, ld_x, q8._ref if q8 is not None else None, p_g, p_u, ld_w, T, d, F, int(activation), p_o, ld_o,
         p_dx, ld_dx, p_dg, p_du, dw_type, ld_dw, int(bool(accumulate)), *_workspace_args(workspace), _stream_ptr(stream)),
         "mosaic_gated_ffn_backward")

@@ -25,7 +25,7 @@ def test_the_header_is_exported_and_bound():
     names = re.findall(r"\b(mosaic_\w+)\s*\(", text)
     assert sorted(names) == sorted(b.LAYER_EXPORTS)
     for n in names:
-        assert getattr(b.lib(), n).argtypes
+        assert getattr(b._layer(), n).argtypes
     assert f"#define MOSAIC_MAX_NORM_ROW {b.MAX_NORM_ROW}" in header() and "#define MOSAIC_MAX_ROW (1 << 17)" in header()
     assert b.MAX_ROW == 1 << 17
 
@@ -65,32 +65,32 @@ def with_defaults(call, defaults):
 
 
 def store(**c):
-    return with_defaults(b.lib().mosaic_checkpoint_store, dict(x=P, type=0, ld=512, T=4, d=512, q8=q8(), stream=None))(**c)
+    return with_defaults(b._layer().mosaic_checkpoint_store, dict(x=P, type=0, ld=512, T=4, d=512, q8=q8(), stream=None))(**c)
 
 
 def load(**c):
-    return with_defaults(b.lib().mosaic_checkpoint_load, dict(q8=q8(), T=4, d=512, out=P, type=0, ld=512, stream=None))(**c)
+    return with_defaults(b._layer().mosaic_checkpoint_load, dict(q8=q8(), T=4, d=512, out=P, type=0, ld=512, stream=None))(**c)
 
 
 def norm(**c):
-    return with_defaults(b.lib().mosaic_rmsnorm_forward, dict(
+    return with_defaults(b._layer().mosaic_rmsnorm_forward, dict(
         x=P, ld_x=512, residual=P, type=0, ld_r=512, gamma=P, gamma_type=1, eps=1e-5, T=4, d=512, idx=None, count=None,
         max_rows=0, sum=P, ld_sum=512, y=P, ld_y=512, q8=None, stream=None))(**c)
 
 
 def norm_backward(**c):
-    return with_defaults(b.lib().mosaic_rmsnorm_backward, dict(
+    return with_defaults(b._layer().mosaic_rmsnorm_backward, dict(
         dy=P, ld_dy=512, h=P, ld_h=512, q8=None, type=0, gamma=P, gamma_type=1, eps=1e-5, T=4, d=512, dsum_in=P,
         ld_in=512, dsum=P, ld_dsum=512, dgamma=P, accumulate=0, ws=P, bytes=1 << 30, stream=None))(**c)
 
 
 def ffn(**c):
-    return with_defaults(b.lib().mosaic_gated_ffn_forward, dict(
+    return with_defaults(b._layer().mosaic_gated_ffn_forward, dict(
         x=P, ld_x=512, wg=P, wu=P, ld_w=512, T=4, d=512, F=1024, act=0, out=P, ld_out=1024, stream=None))(**c)
 
 
 def ffn_backward(**c):
-    return with_defaults(b.lib().mosaic_gated_ffn_backward, dict(
+    return with_defaults(b._layer().mosaic_gated_ffn_backward, dict(
         dout=P, ld_dout=1024, x=P, ld_x=512, q8=None, wg=P, wu=P, ld_w=512, T=4, d=512, F=1024, act=0, out=P, ld_out=1024,
         dx=P, ld_dx=512, dwg=P, dwu=P, dw_type=0, ld_dw=512, accumulate=0, ws=P, bytes=1 << 40, stream=None))(**c)
 
