@@ -17,6 +17,8 @@ namespace {
 
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 typedef __attribute__((address_space(3))) bf16x4_t* lds_bf16x4_ptr_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+typedef const __attribute__((address_space(3))) bf16x8_t* lds_bf16x8_ptr_t;
 
 constexpr int kThreads = 512;        // 8 waves: 2 along P (128 rows each) x 4 along Q (16 QB rows each)
 constexpr int kStepK = 64;
@@ -101,36 +103,54 @@ struct Copier {
     }
   }
 
-  // `left`: k from this step on; pieces at or past it become zeros.
-  __device__ __forceinline__ void issue(const char* base, char* lds, int wave, int left) const {
-#ifdef __HIP_DEVICE_COMPILE__   // the host pass has no buffer descriptors: it would drop the kernels' stubs
-    const __amdgpu_buffer_rsrc_t r =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, kOutside, 0x00020000);
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(lds + (wave * kCopies + i) * 1024), 16,
-                                               at[i] < left ? offset[i] : kOutside, 0, 0, 0);
-#endif
+  // Copy i of the step that `r` begins at, to the operand's LDS address `to`.  `left`: k from this step on; pieces at or past
+  // it become zeros.  Written as a statement because the compiler, which cannot tell the slots apart, puts a wait for all
+  // copies under way ahead of every transposing read that follows a copy it knows of.
+  __device__ __forceinline__ void one(int i, u32x4_t r, uint32_t to, int wave, int left) const {
+    const uint32_t from = at[i] < left ? offset[i] : kOutside;
+    const uint32_t m0 = to + (wave * kCopies + i) * 1024;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m0), "v"(from), "s"(r));   // nothing else here uses M0
   }
 };
 
-// Fragment of 16 rows, k = 32 kk + 8 (lane / 16) .. + 7, rows from `row` on.
-template <int ROWS, bool KROW>
-__device__ __forceinline__ bf16x8_t fragment(const char* lds, int row, int kk, int lane) {
-  if constexpr (KROW) {
-    const int g = lane >> 4, i = lane & 15;
-    const int k = 32 * kk + 8 * g + (i >> 2);
-    const int piece = (row >> 4) ^ Copier<ROWS, true>::turn(8 * g + (i >> 2));
-    const char* at = lds + k * (ROWS * 2) + piece * 32 + (i & 3) * 8;
-    const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)at);
-    const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(at + 4 * ROWS * 2));
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-  } else {
-    const int i = lane & 15;
-    const char* at = lds + (row + i) * 128 + (((4 * kk + (lane >> 4)) ^ (i >> 1)) * 16);
-    return *reinterpret_cast<const bf16x8_t*>(at);
-  }
+// Descriptor of the bytes from `base` on: offsets up to kOutside.
+__device__ __forceinline__ u32x4_t buffer_from(const char* base) {
+  const uint64_t b = reinterpret_cast<uint64_t>(base);
+  return u32x4_t{(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, kOutside, 0x00020000u};
 }
+
+// Reads of an operand's fragments: 16 rows, k = 32 kk + 8 (lane / 16) .. + 7.  A lane's addresses differ between blocks, halves
+// and the two reads of a transposed fragment by constants that go into the instruction (and, across K, by one xor a block).
+template <int ROWS, bool KROW>
+struct Reader {
+  uint32_t at[KROW ? 1 : 2];   // LDS address of block 0; along K: of each half
+
+  __device__ __forceinline__ void place(uint32_t lds, int row, int lane) {   // row: a multiple of 16, across K of 128 or ROWS / 4
+    const int g = lane >> 4, i = lane & 15;
+    if constexpr (KROW) {
+      const int k = 8 * g + (i >> 2);
+      at[0] = lds + k * (ROWS * 2) + ((row >> 4) ^ Copier<ROWS, true>::turn(k)) * 32 + (i & 3) * 8;
+    } else {
+      at[0] = lds + (row + i) * 128 + ((g ^ (i >> 1)) * 16);
+      at[1] = lds + (row + i) * 128 + (((4 + g) ^ (i >> 1)) * 16);
+    }
+  }
+  __device__ __forceinline__ void move(int bytes) {   // to the other slot, a multiple of 1024 bytes on or back
+    at[0] += bytes;
+    if constexpr (!KROW) at[1] += bytes;
+  }
+  // Block `block` rows of 16 on; across K it is below the power of two that the first row is a multiple of.
+  __device__ __forceinline__ bf16x8_t get(int block, int kk) const {
+    if constexpr (KROW) {
+      const uint32_t from = (at[0] ^ (block * 32)) + kk * 32 * (ROWS * 2);
+      const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(uintptr_t)from);
+      const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(uintptr_t)(from + 4 * ROWS * 2));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      return *(lds_bf16x8_ptr_t)(uintptr_t)(at[kk] + block * 2048);
+    }
+  }
+};
 
 template <int MODE, int QB, int ACT>
 __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
@@ -177,14 +197,21 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
   const int step0 = (int)((int64_t)all_steps * split / a.splits);
   const int step1 = (int)((int64_t)all_steps * (split + 1) / a.splits);
 
-  auto copy = [&](int step) {
-    char* slot = smem + ((step - step0) & 1) * kSlot;
+  // The copies of a step, 4 of P and QB of Q for every wave.  Steps past the end are copied as zeros, from nowhere, so that
+  // the loop has no branch.
+  struct Source { u32x4_t p, q; int left; };
+  auto source = [&](int step) {
     const int seg = MODE == kDx && step >= seg_steps ? 1 : 0;
     const int64_t k = (int64_t)(step - seg * seg_steps) * kStepK;
-    const int left = a.depth - k < kStepK ? (int)(a.depth - k) : kStepK;
-    if constexpr (kGated) cp.issue(p_base[0] + k * 2, slot + wp * (kBytesP / 2), wave & 3, left);
-    else cp.issue(p_base[seg] + k * a.ld_p, slot, wave, left);
-    cq.issue(q_base + (kRowQ ? k * a.ld_q : (k + (int64_t)seg * a.depth) * 2), slot + kBytesP, wave, left);
+    Source s;
+    s.left = step >= step1 ? 0 : a.depth - k < kStepK ? (int)(a.depth - k) : kStepK;
+    s.p = buffer_from(p_base[seg] + (kGated ? k * 2 : k * a.ld_p));
+    s.q = buffer_from(q_base + (kRowQ ? k * a.ld_q : (k + (int64_t)seg * a.depth) * 2));
+    return s;
+  };
+  auto copy = [&](const Source& s, uint32_t slot, int c) {
+    if (c < 4) cp.one(c, s.p, kGated ? slot + wp * (kBytesP / 2) : slot, kGated ? wave & 3 : wave, s.left);
+    else cq.one(c - 4, s.q, slot + kBytesP, wave, s.left);
   };
 
   f32x4_t acc[8][QB];
@@ -193,29 +220,61 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
 #pragma unroll
     for (int j = 0; j < QB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  // LDS row of this wave's P block i: gated, four gate blocks and the up blocks of the same features.
-  auto p_block = [&](int i) { return kGated ? (i >> 2) * 128 + wp * 64 + (i & 3) * 16 : wp * 128 + i * 16; };
-
-  if (step0 < step1) copy(step0);
-  for (int step = step0; step < step1; ++step) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();   // this step has arrived, and nobody reads the other slot any more
-    if (step + 1 < step1) copy(step + 1);
-    const char* slot = smem + ((step - step0) & 1) * kSlot;
+  // This wave's P blocks: gated, four gate blocks and the up blocks of the same features.
+  Reader<kTileP, kRowP> rp;
+  Reader<kTileQ, kRowQ> rq;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
+  rp.place(lds0, wp * (kGated ? 64 : 128), lane);
+  rq.place(lds0 + kBytesP, wq * 16 * QB, lane);
+  struct Half { bf16x8_t p[8], q[QB]; };   // the fragments of half a step, 32 k
+  auto read = [&](Half& h, int kk, int c) {   // fragment c of them, Q first
+    if (c < QB) h.q[c] = rq.get(c, kk);
+    else h.p[c - QB] = rp.get(kGated ? ((c - QB) >> 2) * 8 + ((c - QB) & 3) : c - QB, kk);
+  };
+  // Half a step: 8 groups of QB products, with the other half's reads and a step's copies dealt out between them.  Products
+  // come first, so that what they wait for was asked for half a step ago.
+  auto half_step = [&](const Half& use, Half& fill, int kk, const Source* s, uint32_t to) {
+    constexpr int kReads = 8 + QB, kCopies = 4 + QB;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      bf16x8_t fp[8], fq[QB];
+    for (int i = 0; i < 8; ++i) {
 #pragma unroll
-      for (int j = 0; j < QB; ++j) fq[j] = fragment<kTileQ, kRowQ>(slot + kBytesP, wq * 16 * QB + j * 16, kk, lane);
+      for (int j = 0; j < QB; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(use.p[i], use.q[j], acc[i][j], 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) fp[i] = fragment<kTileP, kRowP>(slot, p_block(i), kk, lane);
+      for (int c = kReads * i / 7; c < kReads * (i + 1) / 7 && c < kReads; ++c) read(fill, kk, c);
+      if (s != nullptr) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-#pragma unroll
-        for (int j = 0; j < QB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
+        for (int c = kCopies * i / 8; c < kCopies * (i + 1) / 8; ++c) copy(*s, to, c);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
+  };
+
+  Half h0, h1;
+  {
+    const Source s0 = source(step0), s1 = source(step0 + 1);
+#pragma unroll
+    for (int c = 0; c < 4 + QB; ++c) copy(s0, lds0, c);
+#pragma unroll
+    for (int c = 0; c < 4 + QB; ++c) copy(s1, lds0 + kSlot, c);
   }
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(4 + QB) : "memory");
+#pragma unroll
+  for (int c = 0; c < 8 + QB; ++c) read(h0, 0, c);
+  uint32_t slot = lds0;
+  int to_other = kSlot;
+  for (int step = step0; step < step1; ++step) {
+    half_step(h0, h1, 1, nullptr, 0);
+    // This slot has been read by this wave, and its copies to the other one have arrived; so, then, for all waves.
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    rp.move(to_other);
+    rq.move(to_other);
+    const Source s = source(step + 2);
+    half_step(h1, h0, 0, &s, slot);
+    slot += to_other;
+    to_other = -to_other;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
   // Accumulator register r of a lane: P row 4 (lane / 16) + r, Q row lane % 16 of the block.
   const int sub = 4 * (lane >> 4);
