@@ -22,8 +22,6 @@ typedef const __attribute__((address_space(3))) bf16x8_t* lds_bf16x8_ptr_t;
 
 constexpr int kThreads = 512;        // 8 waves: 2 along P (128 rows each) x 4 along Q (16 QB rows each)
 constexpr int kStepK = 64;
-constexpr int kTileP = 256;
-constexpr int kBytesP = kTileP * kStepK * 2;
 constexpr uint32_t kOutside = 0x80000000u;   // a buffer offset past every range here: such a lane's copy brings zeros
 
 constexpr int kXcds = 8;
@@ -152,12 +150,14 @@ struct Reader {
   }
 };
 
-template <int MODE, int QB, int ACT>
+template <int MODE, int TP, int QB, int SLOTS, int ACT>
 __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
   constexpr bool kGated = MODE == kForward || MODE == kRecompute;
   constexpr bool kRowP = !kGated, kRowQ = MODE == kDw;
-  constexpr int kTileQ = 64 * QB, kBytesQ = kTileQ * kStepK * 2, kSlot = kBytesP + kBytesQ;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * kSlot];
+  constexpr int kTileP = TP, kTileQ = 64 * QB, kBlocksP = TP / 32;   // P blocks of a wave
+  constexpr int kBytesP = kTileP * kStepK * 2, kBytesQ = kTileQ * kStepK * 2, kSlot = kBytesP + kBytesQ;
+  constexpr int kCopiesP = TP / 64, kCopies = kCopiesP + QB;   // of a step, by every wave
+  __shared__ __attribute__((aligned(1024))) char smem[SLOTS * kSlot];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wp = wave >> 2, wq = wave & 3;
 
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
   const char* q_base;
   Copier<kTileP, kRowP> cp;
   Copier<kTileQ, kRowQ> cq;
-  if constexpr (kGated) {   // waves 0..3 copy gate rows (LDS rows 0..127), waves 4..7 the up rows
+  if constexpr (kGated) {   // waves 0..3 copy gate rows, waves 4..7 the up rows behind them
     p_base[0] = (wp == 0 ? a.p0 : a.p1) + p_row * a.ld_p;
     p_base[1] = p_base[0];
     cp.place(wave & 3, lane, a.ld_p, a.rows_p - p_row);
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
   const int step0 = (int)((int64_t)all_steps * split / a.splits);
   const int step1 = (int)((int64_t)all_steps * (split + 1) / a.splits);
 
-  // The copies of a step, 4 of P and QB of Q for every wave.  Steps past the end are copied as zeros, from nowhere, so that
+  // Steps past the end are copied as zeros, from nowhere, so that
   // the loop has no branch.
   struct Source { u32x4_t p, q; int left; };
   auto source = [&](int step) {
@@ -210,69 +210,69 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
     return s;
   };
   auto copy = [&](const Source& s, uint32_t slot, int c) {
-    if (c < 4) cp.one(c, s.p, kGated ? slot + wp * (kBytesP / 2) : slot, kGated ? wave & 3 : wave, s.left);
-    else cq.one(c - 4, s.q, slot + kBytesP, wave, s.left);
+    if (c < kCopiesP) cp.one(c, s.p, kGated ? slot + wp * (kBytesP / 2) : slot, kGated ? wave & 3 : wave, s.left);
+    else cq.one(c - kCopiesP, s.q, slot + kBytesP, wave, s.left);
   };
 
-  f32x4_t acc[8][QB];
+  f32x4_t acc[kBlocksP][QB];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < kBlocksP; ++i) {
 #pragma unroll
     for (int j = 0; j < QB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  // This wave's P blocks: gated, four gate blocks and the up blocks of the same features.
+  // This wave's P blocks: gated, half of them gate blocks, then the up blocks of the same features.
   Reader<kTileP, kRowP> rp;
   Reader<kTileQ, kRowQ> rq;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
-  rp.place(lds0, wp * (kGated ? 64 : 128), lane);
+  rp.place(lds0, wp * (kGated ? kTileP / 4 : kTileP / 2), lane);
   rq.place(lds0 + kBytesP, wq * 16 * QB, lane);
-  struct Half { bf16x8_t p[8], q[QB]; };   // the fragments of half a step, 32 k
+  struct Half { bf16x8_t p[kBlocksP], q[QB]; };   // the fragments of half a step, 32 k
+  constexpr int kReads = kBlocksP + QB;
   auto read = [&](Half& h, int kk, int c) {   // fragment c of them, Q first
+    const int i = c - QB;
     if (c < QB) h.q[c] = rq.get(c, kk);
-    else h.p[c - QB] = rp.get(kGated ? ((c - QB) >> 2) * 8 + ((c - QB) & 3) : c - QB, kk);
+    else h.p[i] = rp.get(kGated && i >= kBlocksP / 2 ? i + kBlocksP / 2 : i, kk);
   };
-  // Half a step: 8 groups of QB products, with the other half's reads and a step's copies dealt out between them.  Products
-  // come first, so that what they wait for was asked for half a step ago.
+  // Half a step: kBlocksP groups of QB products, with the other half's reads and a step's copies dealt out between them.
+  // Products come first, so that what they wait for was asked for half a step ago.
   auto half_step = [&](const Half& use, Half& fill, int kk, const Source* s, uint32_t to) {
-    constexpr int kReads = 8 + QB, kCopies = 4 + QB;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < kBlocksP; ++i) {
 #pragma unroll
       for (int j = 0; j < QB; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(use.p[i], use.q[j], acc[i][j], 0, 0, 0);
 #pragma unroll
-      for (int c = kReads * i / 7; c < kReads * (i + 1) / 7 && c < kReads; ++c) read(fill, kk, c);
+      for (int c = kReads * i / (kBlocksP - 1); c < kReads * (i + 1) / (kBlocksP - 1) && c < kReads; ++c) read(fill, kk, c);
       if (s != nullptr) {
 #pragma unroll
-        for (int c = kCopies * i / 8; c < kCopies * (i + 1) / 8; ++c) copy(*s, to, c);
+        for (int c = kCopies * i / kBlocksP; c < kCopies * (i + 1) / kBlocksP; ++c) copy(*s, to, c);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
 
+  // A ring of slots, all but one of them under way.
   Half h0, h1;
-  {
-    const Source s0 = source(step0), s1 = source(step0 + 1);
 #pragma unroll
-    for (int c = 0; c < 4 + QB; ++c) copy(s0, lds0, c);
+  for (int n = 0; n < SLOTS; ++n) {
+    const Source s = source(step0 + n);
 #pragma unroll
-    for (int c = 0; c < 4 + QB; ++c) copy(s1, lds0 + kSlot, c);
+    for (int c = 0; c < kCopies; ++c) copy(s, lds0 + n * kSlot, c);
   }
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(4 + QB) : "memory");
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((SLOTS - 1) * kCopies) : "memory");
 #pragma unroll
-  for (int c = 0; c < 8 + QB; ++c) read(h0, 0, c);
+  for (int c = 0; c < kReads; ++c) read(h0, 0, c);
   uint32_t slot = lds0;
-  int to_other = kSlot;
   for (int step = step0; step < step1; ++step) {
     half_step(h0, h1, 1, nullptr, 0);
-    // This slot has been read by this wave, and its copies to the other one have arrived; so, then, for all waves.
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    rp.move(to_other);
-    rq.move(to_other);
-    const Source s = source(step + 2);
+    // This slot has been read by this wave, and its copies to the next one have arrived; so, then, for all waves.
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((SLOTS - 2) * kCopies) : "memory");
+    const int move = slot == lds0 + (SLOTS - 1) * kSlot ? -(SLOTS - 1) * kSlot : kSlot;
+    rp.move(move);
+    rq.move(move);
+    const Source s = source(step + SLOTS);
     half_step(h1, h0, 0, &s, slot);
-    slot += to_other;
-    to_other = -to_other;
+    slot += move;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
@@ -284,8 +284,8 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
     if (q >= a.rows_q) continue;
     if constexpr (kGated) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int f = p_row + wp * 64 + i * 16 + sub;
+      for (int i = 0; i < kBlocksP / 2; ++i) {
+        const int f = p_row + wp * (kTileP / 4) + i * 16 + sub;
         if (f >= a.rows_p) continue;
         bf16x4_t o;
         if constexpr (MODE == kForward) {
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
           for (int r = 0; r < 4; ++r) {
             float act, slope;
             activate<ACT>(acc[i][j][r], act, slope);
-            o[r] = (__bf16)(act * acc[i + 4][j][r]);
+            o[r] = (__bf16)(act * acc[i + kBlocksP / 2][j][r]);
           }
           *reinterpret_cast<bf16x4_t*>(a.out0 + q * a.ld_out0 + (int64_t)f * 2) = o;
         } else {
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             float act, slope;
-            const float u = acc[i + 4][j][r], dr = (float)d[r];
+            const float u = acc[i + kBlocksP / 2][j][r], dr = (float)d[r];
             activate<ACT>(acc[i][j][r], act, slope);
             o[r] = (__bf16)(act * u);
             dg[r] = (__bf16)(dr * u * slope);
@@ -318,8 +318,8 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
       if constexpr (MODE == kDx) row = a.out0 + ((int64_t)split * a.rows_q + q) * a.ld_out0;
       else row = q < a.F ? a.out0 + q * a.ld_out0 : a.out1 + (q - a.F) * a.ld_out0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int c = p_row + wp * 128 + i * 16 + sub;
+      for (int i = 0; i < kBlocksP; ++i) {
+        const int c = p_row + wp * (kTileP / 2) + i * 16 + sub;
         if (c >= a.rows_p) continue;
         if (a.f32) {
           f32x4_t* to = reinterpret_cast<f32x4_t*>(row + (int64_t)c * 4);
@@ -333,6 +333,89 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
       }
     }
   }
+}
+
+#ifdef __HIP_DEVICE_COMPILE__
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const char* base) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, kOutside, 0x00020000);
+}
+__device__ __forceinline__ bf16x8_t load_at(__amdgpu_buffer_rsrc_t r, uint32_t offset, int from) {
+  return __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(r, offset, from, 0));
+}
+#endif
+
+// Up to 16 rows: the weights are read once, and that is all the time goes to.  A block takes 16 features of both
+// projections; its four waves take the 64 k pieces of their rows in turn, straight into registers, so that 512 consecutive
+// bytes of a row are asked for at once and no wave waits for another before the sums meet in LDS.
+// 1 row of 12288 x 4096: 37 us, the weights at 5.4 TB/s (a tile of 128 x 64: 43 us); 16 rows 40 us, where the tile takes
+// 43; from 17 rows on it would be 45 and more, for every block reads all of x.
+constexpr int kFewRows = 16, kFewThreads = 256;
+
+template <int ACT>
+__global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(const GemmArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__
+  constexpr int kDeep = 4;   // pieces under way
+  __shared__ f32x4_t sums[4][2][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int f0 = (int)blockIdx.x * 16;
+  const int row = lane & 15, part = (lane >> 4) * 8;
+  // A lane's fragments of a piece: k = 32 h + part .. + 7 of its row, h = 0, 1.  What lies past the end of the rows or of K
+  // is asked for outside the buffers and comes as zeros.
+  const int d = (int)a.depth;
+  const __amdgpu_buffer_rsrc_t gate = buffer_at(a.p0 + (int64_t)f0 * a.ld_p), up = buffer_at(a.p1 + (int64_t)f0 * a.ld_p);
+  const __amdgpu_buffer_rsrc_t x = buffer_at(a.q);
+  const uint32_t at_f = f0 + row < a.rows_p ? (uint32_t)(row * a.ld_p) + part * 2 : kOutside;
+  const uint32_t at_x = row < a.rows_q ? (uint32_t)(row * a.ld_q) + part * 2 : kOutside;
+  struct Piece { bf16x8_t g[2], u[2], x[2]; };
+  f32x4_t acc_g = {0.f, 0.f, 0.f, 0.f}, acc_u = {0.f, 0.f, 0.f, 0.f};
+  // Blocks begin at different places of K: side by side they would all ask for the same lines of x, and, rows lying a power of
+  // two apart, for the same channels.
+  const int rounds = (d + 4 * kStepK * kDeep - 1) / (4 * kStepK * kDeep);
+  int turn = (int)blockIdx.x % rounds;
+  for (int r = 0; r < rounds; ++r) {
+    const int k0 = (turn * 4 * kDeep + wave) * kStepK;
+    turn = turn + 1 == rounds ? 0 : turn + 1;
+    Piece p[kDeep];
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = k0 + i * 4 * kStepK + 32 * h;
+        const uint32_t past = k + part < d ? 0 : kOutside;
+        p[i].g[h] = load_at(gate, at_f | past, k * 2);
+        p[i].u[h] = load_at(up, at_f | past, k * 2);
+        p[i].x[h] = load_at(x, at_x | past, k * 2);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);   // all of them under way: left to itself the compiler saves registers instead
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        acc_g = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[i].g[h], p[i].x[h], acc_g, 0, 0, 0);
+        acc_u = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[i].u[h], p[i].x[h], acc_u, 0, 0, 0);
+      }
+    }
+  }
+  sums[wave][0][lane] = acc_g;
+  sums[wave][1][lane] = acc_u;
+  __syncthreads();
+  const int f = f0 + 4 * (lane >> 4);
+  if (wave != 0 || row >= a.rows_q || f >= a.rows_p) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) {
+    acc_g += sums[w][0][lane];
+    acc_u += sums[w][1][lane];
+  }
+  bf16x4_t o;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    float act, slope;
+    activate<ACT>(acc_g[r], act, slope);
+    o[r] = (__bf16)(act * acc_u[r]);
+  }
+  *reinterpret_cast<bf16x4_t*>(a.out0 + row * a.ld_out0 + (int64_t)f * 2) = o;
+#endif
 }
 
 // Adds the parts of dx in their order and rounds once.
@@ -356,21 +439,57 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(const float* __restrict__
 
 int64_t tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
-// Rows of one launch: at most 2^12 row tiles by 2^10 column tiles of 512 threads stay under 2^32 threads.
-constexpr int64_t kLaunchRows = (int64_t)1 << 20;
-static_assert((kLaunchRows / 256) * (MOSAIC_MAX_ROW / 128) * kThreads < (int64_t)1 << 32, "threads of a launch");
+// Rows of one launch; rows past them go to further ones.
+constexpr int64_t kLaunchRows = (int64_t)1 << 17;
+static_assert(kLaunchRows <= MOSAIC_MAX_ROW && (int64_t)(MOSAIC_MAX_ROW / 64) * (MOSAIC_MAX_ROW / 64) * kThreads < (int64_t)1 << 32,
+              "threads of a launch of the smallest tiles: 64 rows by 64 features, or of both weight gradients by 128 columns");
+
+template <int MODE, int TP, int QB, int SLOTS, int ACT>
+int launch_tiles(GemmArgs a, hipStream_t stream) {
+  a.tiles_p = (int32_t)tiles(a.rows_p, MODE == kForward || MODE == kRecompute ? TP / 2 : TP);
+  a.tiles_q = (int32_t)tiles(a.rows_q, 64 * QB);
+  const dim3 grid((unsigned)((int64_t)a.tiles_q * a.tiles_p * a.splits));
+  return launch_kernel(ffn_gemm_kernel<MODE, TP, QB, SLOTS, ACT>, grid, dim3(kThreads), stream, a);
+}
+
+// The tiles there are, and what one step of 64 k takes all CUs at work, in us.  A block's step is bound by the latency of its
+// copies or by the matrix cores, so a tile takes the same where it is alone and a launch takes whole rounds of tiles.
+// Times from 16 to 2048 rows of 12288 x 4096, 18944 x 3584 and 4096 x 1024.
+struct Tile { int p, q; double step, step_alone; int per_cu; };
+constexpr Tile kTiles[] = {
+    {256, 256, 1.50, 1.50, 1}, {128, 256, 0.91, 0.91, 1}, {256, 128, 0.92, 0.92, 1},
+    {128, 128, 0.60, 0.60, 1}, {256, 64, 0.80, 0.80, 1},  {128, 64, 0.84, 0.57, 2},
+};
+constexpr int kCus = 256;
+
+struct Choice { int tile; double us; };
+Choice choose_tile(int64_t rows_p, int64_t rows_q, bool gated, int64_t steps, int64_t splits) {
+  Choice best = {0, 0.0};
+  for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
+    const Tile& t = kTiles[i];
+    const int64_t n = tiles(rows_p, gated ? t.p / 2 : t.p) * tiles(rows_q, t.q) * splits;
+    const double us = (double)tiles(n, kCus * t.per_cu) * (double)tiles(steps, splits) * (n <= kCus ? t.step_alone : t.step);
+    if (i == 0 || us < best.us) best = {i, us};
+  }
+  return best;
+}
 
 template <int MODE, int ACT>
-int launch_gemm(GemmArgs a, hipStream_t stream) {
-  a.tiles_p = (int32_t)tiles(a.rows_p, MODE == kForward || MODE == kRecompute ? kTileP / 2 : kTileP);
-  // Few rows take a narrow tile.
-  const int qb = a.rows_q <= 64 ? 1 : a.rows_q <= 128 ? 2 : 4;
-  const int64_t tiles_q = tiles(a.rows_q, 64 * qb);
-  a.tiles_q = (int32_t)tiles_q;
-  const dim3 grid((unsigned)(tiles_q * a.tiles_p * a.splits));
-  if (qb == 1) return launch_kernel(ffn_gemm_kernel<MODE, 1, ACT>, grid, dim3(kThreads), stream, a);
-  if (qb == 2) return launch_kernel(ffn_gemm_kernel<MODE, 2, ACT>, grid, dim3(kThreads), stream, a);
-  return launch_kernel(ffn_gemm_kernel<MODE, 4, ACT>, grid, dim3(kThreads), stream, a);
+int launch_gemm(const GemmArgs& a, hipStream_t stream) {
+  constexpr bool kGated = MODE == kForward || MODE == kRecompute;
+  switch (choose_tile(a.rows_p, a.rows_q, kGated, (MODE == kDx ? 2 : 1) * tiles(a.depth, kStepK), a.splits).tile) {
+    case 0: return launch_tiles<MODE, 256, 4, 2, ACT>(a, stream);
+    case 1: return launch_tiles<MODE, 128, 4, 3, ACT>(a, stream);
+    case 2: return launch_tiles<MODE, 256, 2, 3, ACT>(a, stream);
+    case 3: return launch_tiles<MODE, 128, 2, 4, ACT>(a, stream);
+    case 4: return launch_tiles<MODE, 256, 1, 4, ACT>(a, stream);
+    default: return launch_tiles<MODE, 128, 1, 3, ACT>(a, stream);
+  }
+}
+
+template <int ACT>
+int launch_few(const GemmArgs& a, hipStream_t stream) {
+  return launch_kernel(ffn_few_kernel<ACT>, dim3((unsigned)tiles(a.rows_p, 16)), dim3(kFewThreads), stream, a);
 }
 
 template <int MODE>
@@ -381,13 +500,18 @@ int launch_gated(const GemmArgs& a, int activation, hipStream_t stream) {
 
 }  // namespace
 
+// Parts of K that dx is summed in: where its tiles leave CUs idle, as many as save more than joining the parts costs (a
+// launch of ~4 us, and 8 bytes an element and part through the caches).
 int32_t ffn_dx_splits(int64_t T, int32_t d, int32_t F) {
-  const int64_t units = tiles(T, 256) * tiles(d, kTileP);
+  if (T == 0 || T > kLaunchRows) return 1;
   const int64_t steps = 2 * tiles(F, kStepK);
-  if (T == 0 || units >= 192) return 1;
-  const int64_t s = 256 / units;
-  const int64_t most = steps / 8 < 1 ? 1 : steps / 8;
-  return (int32_t)(s > most ? most : s);
+  int32_t best = 1;
+  double least = choose_tile(d, T, false, steps, 1).us;
+  for (int32_t s = 2; s <= 16 && s * 4 <= steps; ++s) {
+    const double us = choose_tile(d, T, false, steps, s).us + 4.0 + (double)(T * d) * 8.0 * s / 4e6;
+    if (us < least) { least = us; best = s; }
+  }
+  return best;
 }
 
 int launch_gated_ffn_forward(const FfnForwardArgs& f, hipStream_t stream) {
@@ -405,7 +529,9 @@ int launch_gated_ffn_forward(const FfnForwardArgs& f, hipStream_t stream) {
     a.rows_q = f.T - t < kLaunchRows ? f.T - t : kLaunchRows;
     a.q = static_cast<const char*>(f.x) + t * a.ld_q;
     a.out0 = static_cast<char*>(f.out) + t * a.ld_out0;
-    if (launch_gated<kForward>(a, f.activation, stream) != 0) return -1;
+    const int rc = f.T > kFewRows ? launch_gated<kForward>(a, f.activation, stream)
+                   : f.activation == MOSAIC_SILU ? launch_few<MOSAIC_SILU>(a, stream) : launch_few<MOSAIC_GELU_TANH>(a, stream);
+    if (rc != 0) return -1;
   }
   return 0;
 }
