@@ -1,12 +1,13 @@
 // Gated feed-forward block, act(x Wg^T) * (x Wu^T), and its gradients, on the matrix cores.
 //
-// All products run through one tile: 256 "P" rows by 64 QB "Q" rows, K in steps of 64.  P is the operand whose rows are the
-// output's contiguous columns (the accumulator layout gives a lane four consecutive P rows of one Q row, so results are
-// stored eight bytes a lane), Q the one whose rows are the output's rows:
-//   forward, and the projections again in the backward pass:  P = 128 rows of Wg and the same 128 of Wu, Q = x; the two
-//     projections of an element meet in one lane, so the activation and the product need no exchange
+// All products run through one kernel: a tile of "P" rows by "Q" rows (256 x 256 where there is work enough), K in steps of 64.
+// P is the operand whose rows are the output's contiguous columns (the accumulator layout gives a lane four consecutive P
+// rows of one Q row), Q the one whose rows are the output's rows:
+//   forward, and the projections again in the backward pass:  P = rows of Wg and as many of Wu, Q = x; the two projections
+//     of an element meet in one lane, so the activation and the product need no exchange
 //   dx:  P = columns of Wg, then of Wu (K = 2 F), Q = dg | du
 //   dw:  P = columns of x (K = T), Q = columns of dg | du
+// Operands that lie across K are read from LDS by transposing reads; nothing is transposed in memory.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -20,11 +21,10 @@ typedef __attribute__((address_space(3))) bf16x4_t* lds_bf16x4_ptr_t;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 typedef const __attribute__((address_space(3))) bf16x8_t* lds_bf16x8_ptr_t;
 
-constexpr int kThreads = 512;        // 8 waves: 2 along P (128 rows each) x 4 along Q (16 QB rows each)
+constexpr int kThreads = 512;   // 8 waves: 2 along P, 4 along Q
 constexpr int kStepK = 64;
 constexpr uint32_t kOutside = 0x80000000u;   // a buffer offset past every range here: such a lane's copy brings zeros
-
-constexpr int kXcds = 8;
+constexpr int kXcds = 8, kCus = 256;
 
 enum { kForward, kRecompute, kDx, kDw };
 
@@ -74,47 +74,46 @@ __device__ __forceinline__ void activate(float g, float& a, float& slope) {
 // for the transposing reads, of which 32 lanes take 8 k at once.
 template <int ROWS, bool KROW>
 struct Copier {
-  static constexpr int kCopies = ROWS * 128 / (kThreads * 16);
-  uint32_t offset[kCopies];   // of this lane's piece within the step, or kOutside for a row or column past the end
-  int at[kCopies];            // its k
+  static constexpr int kCopies = ROWS * 128 / (kThreads * 16);   // a wave and step
+  uint32_t offset[kCopies];   // of this lane's piece within the step, or kOutside for one past the end
 
   static __device__ __forceinline__ int turn(int k) {
     if (ROWS >= 128) return (k & 3) | (k >> 3 & 1) << 2;
     return (k >> 1 & 1) | (k >> 3 & 1) << 1;   // rows of 128 bytes: two of them span the banks
   }
 
-  __device__ __forceinline__ void place(int wave, int lane, int64_t ld, int64_t valid) {
+  // `valid`: rows there are; `left`: k there are, where rows lie along K (across K the descriptor's end cuts them).
+  __device__ __forceinline__ void place(int wave, int lane, int64_t ld, int64_t valid, int left) {
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
       const int byte = (wave * kCopies + i) * 1024 + lane * 16;
       if constexpr (KROW) {
         const int k = byte / (ROWS * 2), piece = byte % (ROWS * 2) / 16;
         const int col = ((piece >> 1) ^ turn(k)) * 16 + (piece & 1) * 8;
-        at[i] = k;
         offset[i] = col < valid ? (uint32_t)(k * (uint32_t)ld + col * 2) : kOutside;
       } else {
         const int row = byte / 128, piece = byte % 128 / 16;
         const int k = (piece ^ (row >> 1 & 7)) * 8;
-        at[i] = k;
-        offset[i] = row < valid ? (uint32_t)(row * (uint32_t)ld + k * 2) : kOutside;
+        offset[i] = row < valid && k < left ? (uint32_t)(row * (uint32_t)ld + k * 2) : kOutside;
       }
     }
   }
 
-  // Copy i of the step that `r` begins at, to the operand's LDS address `to`.  `left`: k from this step on; pieces at or past
-  // it become zeros.  Written as a statement because the compiler, which cannot tell the slots apart, puts a wait for all
-  // copies under way ahead of every transposing read that follows a copy it knows of.
-  __device__ __forceinline__ void one(int i, u32x4_t r, uint32_t to, int wave, int left) const {
-    const uint32_t from = at[i] < left ? offset[i] : kOutside;
-    const uint32_t m0 = to + (wave * kCopies + i) * 1024;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m0), "v"(from), "s"(r));   // nothing else here uses M0
+  // Copy i of the step that `r` begins at, to the operand's LDS address `to`.  Written as a statement because the compiler,
+  // which cannot tell the slots apart, puts a wait for all copies under way ahead of every transposing read that follows a
+  // copy it knows of.
+  __device__ __forceinline__ void one(int i, u32x4_t r, uint32_t to, int wave) const {
+    const uint32_t m0 = __builtin_amdgcn_readfirstlane((int)(to + (wave * kCopies + i) * 1024));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 ::"s"(m0), "v"(offset[i]), "s"(r));   // nothing else in these kernels uses M0
   }
 };
 
-// Descriptor of the bytes from `base` on: offsets up to kOutside.
-__device__ __forceinline__ u32x4_t buffer_from(const char* base) {
+// Descriptor of `bytes` bytes from `base` on.
+__device__ __forceinline__ u32x4_t buffer_from(const char* base, uint32_t bytes) {
   const uint64_t b = reinterpret_cast<uint64_t>(base);
-  return u32x4_t{(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, kOutside, 0x00020000u};
+  return u32x4_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)b), (uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32) & 0xffff),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
 
 // Reads of an operand's fragments: 16 rows, k = 32 kk + 8 (lane / 16) .. + 7.  A lane's addresses differ between blocks, halves
@@ -150,188 +149,371 @@ struct Reader {
   }
 };
 
-template <int MODE, int TP, int QB, int SLOTS, int ACT>
+// The four lanes that hold one Q row (16 apart) each have 4 consecutive P rows of every block; afterwards each has 4 NB
+// consecutive ones, NB = 2 or 4 blocks, in order: what is stored, or was loaded, is 16 bytes a lane.  `scatter` takes
+// gathered quads back.
+typedef uint32_t Quad[2];   // four bf16
+__device__ __forceinline__ void swap32(Quad& a, Quad& b) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const auto r = __builtin_amdgcn_permlane32_swap(a[h], b[h], false, false);
+    a[h] = r[0];
+    b[h] = r[1];
+  }
+}
+__device__ __forceinline__ void swap16(Quad& a, Quad& b) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const auto r = __builtin_amdgcn_permlane16_swap(a[h], b[h], false, false);
+    a[h] = r[0];
+    b[h] = r[1];
+  }
+}
+template <int NB>
+__device__ __forceinline__ void gather(Quad (&w)[NB]) {
+  if constexpr (NB == 4) { swap32(w[0], w[2]); swap32(w[1], w[3]); swap16(w[2], w[3]); }
+  else swap32(w[0], w[1]);
+  swap16(w[0], w[1]);
+}
+template <int NB>
+__device__ __forceinline__ void scatter(Quad (&w)[NB]) {
+  swap16(w[0], w[1]);
+  if constexpr (NB == 4) { swap16(w[2], w[3]); swap32(w[1], w[3]); swap32(w[0], w[2]); }
+  else swap32(w[0], w[1]);
+}
+// Gathered quads to or from `row`, whose element `c` is the first of this lane's; `end`: elements there are, a multiple of 8.
+template <int NB>
+__device__ __forceinline__ void store_quads(char* row, int c, int end, const Quad (&w)[NB]) {
+#pragma unroll
+  for (int i = 0; i < NB; i += 2)
+    if (c + 4 * i < end) *reinterpret_cast<u32x4_t*>(row + (int64_t)(c + 4 * i) * 2) = u32x4_t{w[i][0], w[i][1], w[i + 1][0], w[i + 1][1]};
+}
+template <int NB>
+__device__ __forceinline__ void load_quads(const char* row, int c, int end, bool in, Quad (&w)[NB]) {
+#pragma unroll
+  for (int i = 0; i < NB; i += 2) {
+    u32x4_t v = {0u, 0u, 0u, 0u};
+    if (in && c + 4 * i < end) v = *reinterpret_cast<const u32x4_t*>(row + (int64_t)(c + 4 * i) * 2);
+    w[i][0] = v[0]; w[i][1] = v[1]; w[i + 1][0] = v[2]; w[i + 1][1] = v[3];
+  }
+}
+__device__ __forceinline__ void pack(Quad& w, const float (&v)[4]) {
+  const bf16x4_t b = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+  const uint2 u = __builtin_bit_cast(uint2, b);
+  w[0] = u.x;
+  w[1] = u.y;
+}
+
+// Persistent blocks.  The blocks of an XCD take its run of tiles in turn, and the copies of a block's next tile are under way
+// while the results of the last one are worked out and stored.
+template <int MODE, int TP, int TQ, int SP, int SQ, int ACT>
 __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
   constexpr bool kGated = MODE == kForward || MODE == kRecompute;
   constexpr bool kRowP = !kGated, kRowQ = MODE == kDw;
-  constexpr int kTileP = TP, kTileQ = 64 * QB, kBlocksP = TP / 32;   // P blocks of a wave
-  constexpr int kBytesP = kTileP * kStepK * 2, kBytesQ = kTileQ * kStepK * 2, kSlot = kBytesP + kBytesQ;
-  constexpr int kCopiesP = TP / 64, kCopies = kCopiesP + QB;   // of a step, by every wave
-  __shared__ __attribute__((aligned(1024))) char smem[SLOTS * kSlot];
+  constexpr int kTileP = TP, kTileQ = TQ, kBlocksP = TP / 32, QB = TQ / 64;   // blocks of a wave
+  constexpr int kBytesP = kTileP * kStepK * 2, kBytesQ = kTileQ * kStepK * 2;
+  using CopierP = Copier<kTileP, kRowP>;
+  using CopierQ = Copier<kTileQ, kRowQ>;
+  constexpr int kCopiesP = CopierP::kCopies, kCopiesQ = CopierQ::kCopies;   // a wave and step
+  // With a slot more for P its copies go out in the other half of a step, into the slot of the step before, so that a wave has
+  // a copy between two groups of products all the time.
+  constexpr bool kSplit = SP != SQ;
+  static_assert(!kSplit || SP == SQ + 1, "the waits of the loop");
+  __shared__ __attribute__((aligned(1024))) char smem[SP * kBytesP + SQ * kBytesQ];   // a ring of slots for each operand
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wp = wave >> 2, wq = wave & 3;
+  const int wave_p = kGated ? wq : wave;   // gated: waves 0..3 copy gate rows, waves 4..7 the up rows behind them
 
-  // Workgroup b runs on XCD b % 8; every XCD gets a run of tiles, and within it panels of 8 Q tiles, so that what is in
+  // Workgroup b runs on XCD b % 8; every XCD gets a run of tiles, and within it panels of kPanel Q tiles, so that what is in
   // flight behind one L2 shares both operands.
-  const int n = a.tiles_p * a.tiles_q * a.splits;
-  const int b = (int)blockIdx.x, x = b % kXcds;
-  const int id = x * (n / kXcds) + (x < n % kXcds ? x : n % kXcds) + b / kXcds;
-  const int split = id / (a.tiles_p * a.tiles_q), tile = id % (a.tiles_p * a.tiles_q);
-  constexpr int kPanel = 8;
-  const int panel = tile / (kPanel * a.tiles_p);
-  const int deep = a.tiles_q - panel * kPanel < kPanel ? a.tiles_q - panel * kPanel : kPanel;
-  const int in_panel = tile - panel * kPanel * a.tiles_p;
-  const int tp = in_panel / deep;
-  const int64_t tq = panel * kPanel + in_panel % deep;
-
-  const int p_row = tp * (kGated ? kTileP / 2 : kTileP);   // first P row; gated: first feature
-  const int64_t q_row = tq * kTileQ;
-  const char* p_base[2];
-  const char* q_base;
-  Copier<kTileP, kRowP> cp;
-  Copier<kTileQ, kRowQ> cq;
-  if constexpr (kGated) {   // waves 0..3 copy gate rows, waves 4..7 the up rows behind them
-    p_base[0] = (wp == 0 ? a.p0 : a.p1) + p_row * a.ld_p;
-    p_base[1] = p_base[0];
-    cp.place(wave & 3, lane, a.ld_p, a.rows_p - p_row);
-  } else {
-    p_base[0] = a.p0 + (int64_t)p_row * 2;
-    p_base[1] = MODE == kDx ? a.p1 + (int64_t)p_row * 2 : p_base[0];
-    cp.place(wave, lane, a.ld_p, a.rows_p - p_row);
-  }
-  q_base = kRowQ ? a.q + q_row * 2 : a.q + q_row * a.ld_q;
-  cq.place(wave, lane, a.ld_q, a.rows_q - q_row);
+  const int per_split = a.tiles_p * a.tiles_q, n = per_split * a.splits;
+  const int xcd = (int)blockIdx.x % kXcds;
+  const int stride = (int)gridDim.x / kXcds + (xcd < (int)gridDim.x % kXcds ? 1 : 0);
+  int id = xcd * (n / kXcds) + (xcd < n % kXcds ? xcd : n % kXcds);   // the run's first tile
+  const int end = id + n / kXcds + (xcd < n % kXcds ? 1 : 0);
+  id += (int)blockIdx.x / kXcds;
+  if (id >= end) return;
 
   const int seg_steps = (int)((a.depth + kStepK - 1) / kStepK);
   const int all_steps = MODE == kDx ? 2 * seg_steps : seg_steps;
-  const int step0 = (int)((int64_t)all_steps * split / a.splits);
-  const int step1 = (int)((int64_t)all_steps * (split + 1) / a.splits);
 
-  // Steps past the end are copied as zeros, from nowhere, so that
-  // the loop has no branch.
-  struct Source { u32x4_t p, q; int left; };
-  auto source = [&](int step) {
-    const int seg = MODE == kDx && step >= seg_steps ? 1 : 0;
-    const int64_t k = (int64_t)(step - seg * seg_steps) * kStepK;
-    Source s;
-    s.left = step >= step1 ? 0 : a.depth - k < kStepK ? (int)(a.depth - k) : kStepK;
-    s.p = buffer_from(p_base[seg] + (kGated ? k * 2 : k * a.ld_p));
-    s.q = buffer_from(q_base + (kRowQ ? k * a.ld_q : (k + (int64_t)seg * a.depth) * 2));
-    return s;
-  };
-  auto copy = [&](const Source& s, uint32_t slot, int c) {
-    if (c < kCopiesP) cp.one(c, s.p, kGated ? slot + wp * (kBytesP / 2) : slot, kGated ? wave & 3 : wave, s.left);
-    else cq.one(c - kCopiesP, s.q, slot + kBytesP, wave, s.left);
+  // Of the tile whose copies are issued.
+  int split, p_row, step0, step1, placed_p, placed_q;   // p_row: first P row; gated: first feature
+  int64_t q_row;
+  const char *p_base0, *p_base1, *q_base;
+  CopierP cp;
+  CopierQ cq;
+  auto begin = [&](int id) __attribute__((always_inline)) {
+    split = id / per_split;
+    const int tile = id - split * per_split;
+    constexpr int kPanel = kGated ? 8 : 4;
+    const int panel = tile / (kPanel * a.tiles_p);
+    const int deep = a.tiles_q - panel * kPanel < kPanel ? a.tiles_q - panel * kPanel : kPanel;
+    const int in_panel = tile - panel * kPanel * a.tiles_p;
+    p_row = in_panel / deep * (kGated ? kTileP / 2 : kTileP);
+    q_row = (int64_t)(panel * kPanel + in_panel % deep) * kTileQ;
+    if constexpr (kGated) {   // waves 4..7 copy the up rows
+      p_base0 = p_base1 = (wp == 0 ? a.p0 : a.p1) + p_row * a.ld_p;
+    } else {
+      p_base0 = a.p0 + (int64_t)p_row * 2;
+      p_base1 = MODE == kDx ? a.p1 + (int64_t)p_row * 2 : p_base0;
+    }
+    q_base = kRowQ ? a.q + q_row * 2 : a.q + q_row * a.ld_q;
+    cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, kStepK);
+    cq.place(wave, lane, a.ld_q, a.rows_q - q_row, kStepK);
+    placed_p = placed_q = kStepK;
+    step0 = (int)((int64_t)all_steps * split / a.splits);
+    step1 = (int)((int64_t)all_steps * (split + 1) / a.splits);
   };
 
-  f32x4_t acc[kBlocksP][QB];
-#pragma unroll
-  for (int i = 0; i < kBlocksP; ++i) {
-#pragma unroll
-    for (int j = 0; j < QB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  // Where an operand's copies come from, step after step.  What lies past the end of K comes as zeros, and so do steps past
+  // the last, so that the loop has no end to look after.  Most steps only move the descriptor on: the full arithmetic in each
+  // of them cost the small tiles a tenth.
+  struct Walk { u32x4_t from; int plain; };   // plain: how many steps the descriptor only has to be moved on
+  Walk walk_p, walk_q;
+  auto find = [&](int step, int& seg, int64_t& k, Walk& w) __attribute__((always_inline)) {   // k there are in `step`
+    seg = MODE == kDx && step >= seg_steps ? 1 : 0;
+    const int at = step - seg * seg_steps, full = (int)(a.depth / kStepK);
+    k = (int64_t)at * kStepK;
+    if (step >= step1) {
+      w.plain = 0x7fffffff;
+      return 0;
+    }
+    const int last = step1 - seg * seg_steps < full ? step1 - seg * seg_steps : full;
+    w.plain = at < last ? last - 1 - at : 0;
+    return at < full ? kStepK : (int)(a.depth - k);
+  };
+  auto locate_p = [&](int step) __attribute__((always_inline)) {
+    int seg;
+    int64_t k;
+    const int left = find(step, seg, k, walk_p);
+    if (!kRowP && left != placed_p && left != 0) {   // into or out of a last step of fewer k
+      placed_p = left;
+      cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, left);
+    }
+    walk_p.from = buffer_from((seg ? p_base1 : p_base0) + (kRowP ? k * a.ld_p : k * 2),
+                              kRowP ? left * (uint32_t)a.ld_p : left == 0 ? 0 : kOutside);
+  };
+  auto locate_q = [&](int step) __attribute__((always_inline)) {
+    int seg;
+    int64_t k;
+    const int left = find(step, seg, k, walk_q);
+    if (!kRowQ && left != placed_q && left != 0) {
+      placed_q = left;
+      cq.place(wave, lane, a.ld_q, a.rows_q - q_row, left);
+    }
+    walk_q.from = buffer_from(q_base + (kRowQ ? k * a.ld_q : (k + (int64_t)seg * a.depth) * 2),
+                              kRowQ ? left * (uint32_t)a.ld_q : left == 0 ? 0 : kOutside);
+  };
+  auto move = [&](Walk& w, uint32_t bytes) __attribute__((always_inline)) {
+    const uint64_t b = ((uint64_t)w.from[1] << 32 | w.from[0]) + bytes;
+    w.from[0] = (uint32_t)b;
+    w.from[1] = (uint32_t)(b >> 32);
+    --w.plain;
+  };
+  auto step_p = [&](int step) __attribute__((always_inline)) {   // to `step`, from the one before
+    if (__builtin_expect(walk_p.plain > 0, 1)) move(walk_p, kRowP ? kStepK * (uint32_t)a.ld_p : kStepK * 2);
+    else locate_p(step);
+  };
+  auto step_q = [&](int step) __attribute__((always_inline)) {
+    if (__builtin_expect(walk_q.plain > 0, 1)) move(walk_q, kRowQ ? kStepK * (uint32_t)a.ld_q : kStepK * 2);
+    else locate_q(step);
+  };
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
+  const uint32_t ring_p = lds0, ring_q = lds0 + SP * kBytesP;
+  auto copy_p = [&](uint32_t to, int c) __attribute__((always_inline)) {
+    cp.one(c, walk_p.from, kGated ? to + wp * (kBytesP / 2) : to, wave_p);
+  };
+  auto copy_q = [&](uint32_t to, int c) __attribute__((always_inline)) { cq.one(c, walk_q.from, to, wave); };
+
   // This wave's P blocks: gated, half of them gate blocks, then the up blocks of the same features.
   Reader<kTileP, kRowP> rp;
   Reader<kTileQ, kRowQ> rq;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
-  rp.place(lds0, wp * (kGated ? kTileP / 4 : kTileP / 2), lane);
-  rq.place(lds0 + kBytesP, wq * 16 * QB, lane);
+  rp.place(ring_p, wp * (kGated ? kTileP / 4 : kTileP / 2), lane);
+  rq.place(ring_q, wq * 16 * QB, lane);
   struct Half { bf16x8_t p[kBlocksP], q[QB]; };   // the fragments of half a step, 32 k
   constexpr int kReads = kBlocksP + QB;
-  auto read = [&](Half& h, int kk, int c) {   // fragment c of them, Q first
+  auto read = [&](Half& h, int kk, int c) __attribute__((always_inline)) {   // fragment c of them, Q first
     const int i = c - QB;
     if (c < QB) h.q[c] = rq.get(c, kk);
     else h.p[i] = rp.get(kGated && i >= kBlocksP / 2 ? i + kBlocksP / 2 : i, kk);
   };
-  // Half a step: kBlocksP groups of QB products, with the other half's reads and a step's copies dealt out between them.
-  // Products come first, so that what they wait for was asked for half a step ago.
-  auto half_step = [&](const Half& use, Half& fill, int kk, const Source* s, uint32_t to) {
+  f32x4_t acc[kBlocksP][QB];
+  // Half a step: kBlocksP groups of QB products, with the other half's reads and some copies dealt out between them.  Products
+  // come first, so that what they wait for was asked for half a step ago.
+  struct Copies { int p, q; uint32_t to_p, to_q; };   // p, q: how many of each operand
+  auto half_step = [&](const Half& use, Half& fill, int kk, const Copies& n) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kBlocksP; ++i) {
 #pragma unroll
-      for (int j = 0; j < QB; ++j)
+      for (int m = 0; m < QB; ++m) {
+        const int j = i & 1 ? QB - 1 - m : m;   // to and fro: one operand of a product is always that of the last
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(use.p[i], use.q[j], acc[i][j], 0, 0, 0);
+      }
 #pragma unroll
       for (int c = kReads * i / (kBlocksP - 1); c < kReads * (i + 1) / (kBlocksP - 1) && c < kReads; ++c) read(fill, kk, c);
-      if (s != nullptr) {
 #pragma unroll
-        for (int c = kCopies * i / kBlocksP; c < kCopies * (i + 1) / kBlocksP; ++c) copy(*s, to, c);
+      for (int c = (n.p + n.q) * i / kBlocksP; c < (n.p + n.q) * (i + 1) / kBlocksP; ++c) {
+        if (c < n.p) copy_p(n.to_p, c);
+        else copy_q(n.to_q, c - n.p);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  uint32_t slot_p = ring_p, slot_q = ring_q;   // of the step being multiplied
+  auto next_p = [&](uint32_t s) __attribute__((always_inline)) { return s == ring_p + (SP - 1) * kBytesP ? ring_p : s + kBytesP; };
+  auto next_q = [&](uint32_t s) __attribute__((always_inline)) { return s == ring_q + (SQ - 1) * kBytesQ ? ring_q : s + kBytesQ; };
 
-  // A ring of slots, all but one of them under way.
-  Half h0, h1;
+  int done_p = 0, done_split = 0;   // the tile whose results are in the accumulators
+  int64_t done_q = -1;
+  for (;;) {
+    // The next tile's first copies, once all waves have read what the last half step read (zeros, for nobody).
+    const bool more = id < end;
+    if (more) {
+      begin(id);
+      uint32_t to_p = slot_p, to_q = slot_q;
 #pragma unroll
-  for (int n = 0; n < SLOTS; ++n) {
-    const Source s = source(step0 + n);
+      for (int n = 0; n < SQ; ++n) {
+        if (n < SP - (kSplit ? 1 : 0)) {
+          if (n == 0) locate_p(step0);
+          else step_p(step0 + n);
 #pragma unroll
-    for (int c = 0; c < kCopies; ++c) copy(s, lds0 + n * kSlot, c);
-  }
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((SLOTS - 1) * kCopies) : "memory");
-#pragma unroll
-  for (int c = 0; c < kReads; ++c) read(h0, 0, c);
-  uint32_t slot = lds0;
-  for (int step = step0; step < step1; ++step) {
-    half_step(h0, h1, 1, nullptr, 0);
-    // This slot has been read by this wave, and its copies to the next one have arrived; so, then, for all waves.
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((SLOTS - 2) * kCopies) : "memory");
-    const int move = slot == lds0 + (SLOTS - 1) * kSlot ? -(SLOTS - 1) * kSlot : kSlot;
-    rp.move(move);
-    rq.move(move);
-    const Source s = source(step + SLOTS);
-    half_step(h1, h0, 0, &s, slot);
-    slot += move;
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-
-  // Accumulator register r of a lane: P row 4 (lane / 16) + r, Q row lane % 16 of the block.
-  const int sub = 4 * (lane >> 4);
-#pragma unroll
-  for (int j = 0; j < QB; ++j) {
-    const int64_t q = q_row + wq * 16 * QB + j * 16 + (lane & 15);
-    if (q >= a.rows_q) continue;
-    if constexpr (kGated) {
-#pragma unroll
-      for (int i = 0; i < kBlocksP / 2; ++i) {
-        const int f = p_row + wp * (kTileP / 4) + i * 16 + sub;
-        if (f >= a.rows_p) continue;
-        bf16x4_t o;
-        if constexpr (MODE == kForward) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float act, slope;
-            activate<ACT>(acc[i][j][r], act, slope);
-            o[r] = (__bf16)(act * acc[i + kBlocksP / 2][j][r]);
-          }
-          *reinterpret_cast<bf16x4_t*>(a.out0 + q * a.ld_out0 + (int64_t)f * 2) = o;
-        } else {
-          const bf16x4_t d = *reinterpret_cast<const bf16x4_t*>(a.dout + q * a.ld_dout + (int64_t)f * 2);
-          bf16x4_t dg, du;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float act, slope;
-            const float u = acc[i + kBlocksP / 2][j][r], dr = (float)d[r];
-            activate<ACT>(acc[i][j][r], act, slope);
-            o[r] = (__bf16)(act * u);
-            dg[r] = (__bf16)(dr * u * slope);
-            du[r] = (__bf16)(dr * act);
-          }
-          if (a.out0 != nullptr) *reinterpret_cast<bf16x4_t*>(a.out0 + q * a.ld_out0 + (int64_t)f * 2) = o;
-          *reinterpret_cast<bf16x4_t*>(a.out1 + q * a.ld_out1 + (int64_t)f * 2) = dg;
-          *reinterpret_cast<bf16x4_t*>(a.out1 + q * a.ld_out1 + ((int64_t)a.F + f) * 2) = du;
+          for (int c = 0; c < kCopiesP; ++c) copy_p(to_p, c);
+          to_p = next_p(to_p);
         }
+        if (n == 0) locate_q(step0);
+        else step_q(step0 + n);
+#pragma unroll
+        for (int c = 0; c < kCopiesQ; ++c) copy_q(to_q, c);
+        to_q = next_q(to_q);
       }
-    } else {
-      char* row;
-      if constexpr (MODE == kDx) row = a.out0 + ((int64_t)split * a.rows_q + q) * a.ld_out0;
-      else row = q < a.F ? a.out0 + q * a.ld_out0 : a.out1 + (q - a.F) * a.ld_out0;
+    }
+    if (done_q >= 0) {
+      // Accumulator register r of a lane: P row 4 (lane / 16) + r, Q row lane % 16 of the block.  Gathered, a lane has
+      // 4 NB consecutive P rows from run on.
+      constexpr int kHalf = kBlocksP / 2, NB = kGated ? (kHalf < 4 ? kHalf : 4) : 4;
+      const int sub = 4 * (lane >> 4), run = 4 * NB * (lane >> 4);
+      Quad grad[MODE == kRecompute ? QB : 1][NB];   // of the outputs, all asked for ahead of their use
+      if constexpr (MODE == kRecompute) {
 #pragma unroll
-      for (int i = 0; i < kBlocksP; ++i) {
-        const int c = p_row + wp * (kTileP / 2) + i * 16 + sub;
-        if (c >= a.rows_p) continue;
-        if (a.f32) {
-          f32x4_t* to = reinterpret_cast<f32x4_t*>(row + (int64_t)c * 4);
-          *to = a.accumulate ? *to + acc[i][j] : acc[i][j];
+        for (int j = 0; j < QB; ++j) {
+          const int64_t q = done_q + wq * 16 * QB + j * 16 + (lane & 15);
+          load_quads(a.dout + q * a.ld_dout, done_p + wp * (kTileP / 4) + run, a.rows_p, q < a.rows_q, grad[j]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int j = 0; j < QB; ++j) {
+        const int64_t q = done_q + wq * 16 * QB + j * 16 + (lane & 15);
+        const bool in = q < a.rows_q;
+        if constexpr (kGated) {
+          const int f = done_p + wp * (kTileP / 4) + run;
+          Quad o[NB];
+          if constexpr (MODE == kForward) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              float v[4];
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                float act, slope;
+                activate<ACT>(acc[i][j][r], act, slope);
+                v[r] = act * acc[i + kHalf][j][r];
+              }
+              pack(o[i], v);
+            }
+          } else {
+            Quad g[NB], u[NB];
+            scatter(grad[j]);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              const bf16x4_t dr = __builtin_bit_cast(bf16x4_t, uint2{grad[j][i][0], grad[j][i][1]});
+              float vo[4], vg[4], vu[4];
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                float act, slope;
+                const float up = acc[i + kHalf][j][r], x = (float)dr[r];
+                activate<ACT>(acc[i][j][r], act, slope);
+                vo[r] = act * up;
+                vg[r] = x * up * slope;
+                vu[r] = x * act;
+              }
+              pack(o[i], vo);
+              pack(g[i], vg);
+              pack(u[i], vu);
+            }
+            gather(g);
+            gather(u);
+            if (in) {
+              store_quads(a.out1 + q * a.ld_out1, f, a.rows_p, g);
+              store_quads(a.out1 + q * a.ld_out1 + (int64_t)a.F * 2, f, a.rows_p, u);
+            }
+          }
+          gather(o);
+          if (in && a.out0 != nullptr) store_quads(a.out0 + q * a.ld_out0, f, a.rows_p, o);
         } else {
-          bf16x4_t o;
+          char* row;
+          if constexpr (MODE == kDx) row = a.out0 + ((int64_t)done_split * a.rows_q + q) * a.ld_out0;
+          else row = q < a.F ? a.out0 + q * a.ld_out0 : a.out1 + (q - a.F) * a.ld_out0;
+          const int c0 = done_p + wp * (kTileP / 2);
+          if (a.f32) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[r] = (__bf16)acc[i][j][r];
-          *reinterpret_cast<bf16x4_t*>(row + (int64_t)c * 2) = o;
+            for (int i = 0; i < kBlocksP; ++i) {
+              const int c = c0 + i * 16 + sub;
+              if (in && c < a.rows_p) {
+                f32x4_t* to = reinterpret_cast<f32x4_t*>(row + (int64_t)c * 4);
+                *to = a.accumulate ? *to + acc[i][j] : acc[i][j];
+              }
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < kBlocksP; i += 4) {
+              Quad o[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float v[4] = {acc[i + k][j][0], acc[i + k][j][1], acc[i + k][j][2], acc[i + k][j][3]};
+                pack(o[k], v);
+              }
+              gather(o);
+              if (in) store_quads(row, c0 + i * 16 + run, a.rows_p, o);
+            }
+          }
         }
       }
     }
+    if (!more) break;
+    // The first slots; with the last tile's stores behind them no count tells them from the others.
+    constexpr int kLater = (SP - (kSplit ? 2 : 1)) * kCopiesP + (SQ - 1) * kCopiesQ;
+    if (done_q < 0) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLater) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < kBlocksP; ++i) {
+#pragma unroll
+      for (int j = 0; j < QB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    Half h0, h1;
+#pragma unroll
+    for (int c = 0; c < kReads; ++c) read(h0, 0, c);
+    for (int step = step0; step < step1; ++step) {
+      if constexpr (kSplit) step_p(step + SP - 1);
+      half_step(h0, h1, 1, Copies{kSplit ? kCopiesP : 0, 0, slot_p == ring_p ? ring_p + (SP - 1) * kBytesP : slot_p - kBytesP, 0});
+      // This step's slots have been read by this wave, and its copies for the next have arrived (all but those issued since
+      // may still be under way); so, then, for all waves.
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((SP - 2) * kCopiesP + (SQ - 2) * kCopiesQ) : "memory");
+      const Copies n = {kSplit ? 0 : kCopiesP, kCopiesQ, slot_p, slot_q};
+      const uint32_t to_p = next_p(slot_p), to_q = next_q(slot_q);
+      rp.move((int)(to_p - slot_p));
+      rq.move((int)(to_q - slot_q));
+      slot_p = to_p;
+      slot_q = to_q;
+      if constexpr (!kSplit) step_p(step + SP);
+      step_q(step + SQ);
+      half_step(h1, h0, 0, n);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    done_p = p_row;
+    done_q = q_row;
+    done_split = split;
+    id += stride;
   }
 }
 
@@ -441,15 +623,16 @@ int64_t tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
 // Rows of one launch; rows past them go to further ones.
 constexpr int64_t kLaunchRows = (int64_t)1 << 17;
-static_assert(kLaunchRows <= MOSAIC_MAX_ROW && (int64_t)(MOSAIC_MAX_ROW / 64) * (MOSAIC_MAX_ROW / 64) * kThreads < (int64_t)1 << 32,
+static_assert(kLaunchRows <= MOSAIC_MAX_ROW && (int64_t)(MOSAIC_MAX_ROW / 64) * (MOSAIC_MAX_ROW / 64) * 512 < (int64_t)1 << 32,
               "threads of a launch of the smallest tiles: 64 rows by 64 features, or of both weight gradients by 128 columns");
 
-template <int MODE, int TP, int QB, int SLOTS, int ACT>
-int launch_tiles(GemmArgs a, hipStream_t stream) {
+template <int MODE, int TP, int TQ, int SP, int SQ, int ACT>
+int launch_tiles(GemmArgs a, int per_cu, hipStream_t stream) {
   a.tiles_p = (int32_t)tiles(a.rows_p, MODE == kForward || MODE == kRecompute ? TP / 2 : TP);
-  a.tiles_q = (int32_t)tiles(a.rows_q, 64 * QB);
-  const dim3 grid((unsigned)((int64_t)a.tiles_q * a.tiles_p * a.splits));
-  return launch_kernel(ffn_gemm_kernel<MODE, TP, QB, SLOTS, ACT>, grid, dim3(kThreads), stream, a);
+  a.tiles_q = (int32_t)tiles(a.rows_q, TQ);
+  const int64_t n = (int64_t)a.tiles_q * a.tiles_p * a.splits;
+  return launch_kernel(ffn_gemm_kernel<MODE, TP, TQ, SP, SQ, ACT>, dim3((unsigned)(n < kCus * per_cu ? n : kCus * per_cu)),
+                       dim3(kThreads), stream, a);
 }
 
 // The tiles there are, and what one step of 64 k takes all CUs at work, in us.  A block's step is bound by the latency of its
@@ -460,8 +643,6 @@ constexpr Tile kTiles[] = {
     {256, 256, 1.50, 1.50, 1}, {128, 256, 0.91, 0.91, 1}, {256, 128, 0.92, 0.92, 1},
     {128, 128, 0.60, 0.60, 1}, {256, 64, 0.80, 0.80, 1},  {128, 64, 0.84, 0.57, 2},
 };
-constexpr int kCus = 256;
-
 struct Choice { int tile; double us; };
 Choice choose_tile(int64_t rows_p, int64_t rows_q, bool gated, int64_t steps, int64_t splits) {
   Choice best = {0, 0.0};
@@ -478,12 +659,12 @@ template <int MODE, int ACT>
 int launch_gemm(const GemmArgs& a, hipStream_t stream) {
   constexpr bool kGated = MODE == kForward || MODE == kRecompute;
   switch (choose_tile(a.rows_p, a.rows_q, kGated, (MODE == kDx ? 2 : 1) * tiles(a.depth, kStepK), a.splits).tile) {
-    case 0: return launch_tiles<MODE, 256, 4, 2, ACT>(a, stream);
-    case 1: return launch_tiles<MODE, 128, 4, 3, ACT>(a, stream);
-    case 2: return launch_tiles<MODE, 256, 2, 3, ACT>(a, stream);
-    case 3: return launch_tiles<MODE, 128, 2, 4, ACT>(a, stream);
-    case 4: return launch_tiles<MODE, 256, 1, 4, ACT>(a, stream);
-    default: return launch_tiles<MODE, 128, 1, 3, ACT>(a, stream);
+    case 0: return launch_tiles<MODE, 256, 256, 3, 2, ACT>(a, 1, stream);
+    case 1: return launch_tiles<MODE, 128, 256, 3, 3, ACT>(a, 1, stream);
+    case 2: return launch_tiles<MODE, 256, 128, 3, 3, ACT>(a, 1, stream);
+    case 3: return launch_tiles<MODE, 128, 128, 4, 4, ACT>(a, 1, stream);
+    case 4: return launch_tiles<MODE, 256, 64, 4, 4, ACT>(a, 1, stream);
+    default: return launch_tiles<MODE, 128, 64, 3, 3, ACT>(a, 2, stream);
   }
 }
 
