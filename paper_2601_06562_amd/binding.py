@@ -382,12 +382,16 @@ def _rows(t, name, T, cols, dtype=None):
     """(pointer, row stride) of a [T, cols] device matrix with dense rows; (0, 0) for None."""
     if t is None:
         return 0, 0
-    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != cols:
+    if t.shape != (T, cols):
         raise ValueError(f"{name} must be [{T}, {cols}], got {list(t.shape)}")
-    ld = t.stride(0) if T > 1 else cols
-    if cols > 1 and t.stride(1) != 1:
+    ld, unit = t.stride()
+    if unit != 1 and cols > 1:
         raise ValueError(f"the rows of {name} must be dense")
-    return _dev_ptr(t, name, dtype), ld
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live in device memory")
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    return t.data_ptr(), ld if T > 1 else cols
 
 
 def _vector(t, name, n, dtype=None):

@@ -132,6 +132,7 @@ constexpr int kThreads = 256;
 template <typename S, int R, int NV>
 __global__ __launch_bounds__(kThreads) void rmsnorm_forward_kernel(const NormForwardArgs p) {
   constexpr int kRows = kThreads / R;
+  constexpr bool kEarly = NV <= 2;   // room for the gains beside the row
   __shared__ float lds[2 * (R > 64 ? R / 64 : 1)];
   const int lane = threadIdx.x % R;
   int64_t n = p.T;
@@ -173,6 +174,12 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_forward_kernel(const NormFor
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss[0] = __builtin_fmaf(h[v][i], h[v][i], ss[0]);
     }
+    float gain[kEarly ? NV : 1][8];
+    if constexpr (kEarly) {   // on their way while the sum is taken
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        if ((v * R + lane) * 8 < p.d) load_gamma(p.gamma, p.gamma_f32, (v * R + lane) * 8, gain[v]);
+    }
     row_sum<R>(ss, lds, turn);
     turn ^= 1;
     const float rstd = 1.0f / __builtin_sqrtf(ss[0] / (float)p.d + p.eps);
@@ -180,8 +187,8 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_forward_kernel(const NormFor
     for (int v = 0; v < NV; ++v) {
       const int c = (v * R + lane) * 8;
       const bool in = c < p.d;
-      float g[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (in) load_gamma(p.gamma, p.gamma_f32, c, g);
+      float (&g)[8] = gain[kEarly ? v : 0];
+      if (!kEarly && in) load_gamma(p.gamma, p.gamma_f32, c, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[v][i] = in ? h[v][i] * rstd * g[i] : 0.f;
       if (in && p.y != nullptr) store8(static_cast<__bf16*>(p.y) + t * p.ld_y + c, h[v]);
@@ -191,6 +198,38 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_forward_kernel(const NormFor
 }
 
 enum { kFromBf16 = 0, kFromF32 = 1, kFromQ8 = 2 };
+template <int FROM> struct Kept { using type = __bf16; };
+template <> struct Kept<kFromF32> { using type = float; };
+template <> struct Kept<kFromQ8> { using type = uint8_t; };
+
+// Eight consecutive elements as they lie in memory.
+template <typename T> struct Raw;
+template <> struct Raw<__bf16> {
+  bf16x8_t v;
+  __device__ __forceinline__ void clear() { v = bf16x8_t{}; }
+  __device__ __forceinline__ void load(const __bf16* p) { v = *reinterpret_cast<const bf16x8_t*>(p); }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (float)v[i];
+  }
+};
+template <> struct Raw<float> {
+  f32x4_t a, b;
+  __device__ __forceinline__ void clear() { a = b = f32x4_t{}; }
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const f32x4_t*>(p);
+    b = *reinterpret_cast<const f32x4_t*>(p + 4);
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[i] = a[i]; f[i + 4] = b[i]; }
+  }
+};
+template <> struct Raw<uint8_t> {
+  uint2 bits;
+  __device__ __forceinline__ void clear() { bits = uint2{0u, 0u}; }
+  __device__ __forceinline__ void load(const uint8_t* p) { bits = *reinterpret_cast<const uint2*>(p); }
+};
 
 // The rows are dealt to gridDim.x * kRows groups of R lanes, each of which sums its rows' dy * n per column in registers
 // and leaves one partial sum; norm_gamma_kernel adds those up.  Rows in turn, not in blocks: the same sums on every call.
@@ -199,33 +238,55 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_backward_kernel(const NormBa
   constexpr int kRows = kThreads / R;
   __shared__ float lds[4 * (R > 64 ? R / 64 : 1)];
   const int lane = threadIdx.x % R;
-  const int64_t first = (int64_t)blockIdx.x * kRows + threadIdx.x / R;
+  const int64_t first = (int64_t)blockIdx.x * kRows + threadIdx.x / R, stride = (int64_t)gridDim.x * kRows;
   const int shift = FROM == kFromQ8 ? group_shift_of(p.q8.group) : 0;
+  // A row as it is loaded.  Where it fits the next row is asked for while one is worked on.
+  struct Row {
+    Raw<__bf16> dy[NV];
+    Raw<typename Kept<FROM>::type> h[NV];
+    float scale[FROM == kFromQ8 ? NV : 1];
+    Raw<S> in[NV];
+  };
+  constexpr bool kAhead = NV <= 2;
+  auto load = [&](Row& r, int64_t t) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * R + lane) * 8;
+      r.dy[v].clear();
+      r.h[v].clear();
+      r.in[v].clear();
+      if (FROM == kFromQ8) r.scale[v] = 0.f;
+      if (c >= p.d) continue;
+      r.dy[v].load(static_cast<const __bf16*>(p.dy) + t * p.ld_dy + c);
+      if constexpr (FROM == kFromQ8) {
+        r.h[v].load(static_cast<const uint8_t*>(p.q8.values) + t * p.q8.ld_values + c);
+        r.scale[v] = p.q8.scales[t * p.q8.ld_scales + (c >> shift)];
+      } else {
+        r.h[v].load(static_cast<const typename Kept<FROM>::type*>(p.h) + t * p.ld_h + c);
+      }
+      if (p.dsum_in != nullptr) r.in[v].load(static_cast<const S*>(p.dsum_in) + t * p.ld_dsum_in + c);
+    }
+  };
   float dgamma[NV][8];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) dgamma[v][i] = 0.f;
   }
+  Row row;
+  if (kAhead && first < p.T) load(row, first);
   int turn = 0;
-  for (int64_t t = first; t < p.T; t += (int64_t)gridDim.x * kRows) {
-    float h[NV][8], dy[NV][8];
+  for (int64_t t = first; t < p.T; t += stride) {
+    if (!kAhead) load(row, t);
+    float h[NV][8], dy[NV][8], out[NV][8];
     float s[2] = {0.f, 0.f};   // sums of h^2 and of gamma dy h
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = (v * R + lane) * 8;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { h[v][i] = 0.f; dy[v][i] = 0.f; }
-      if (c < p.d) {
-        load8(static_cast<const __bf16*>(p.dy) + t * p.ld_dy + c, dy[v]);
-        if constexpr (FROM == kFromBf16) load8(static_cast<const __bf16*>(p.h) + t * p.ld_h + c, h[v]);
-        if constexpr (FROM == kFromF32) load8(static_cast<const float*>(p.h) + t * p.ld_h + c, h[v]);
-        if constexpr (FROM == kFromQ8) load_q8(p.q8, shift, t, c, h[v]);
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = (v * R + lane) * 8;
+      row.dy[v].get(dy[v]);
+      if constexpr (FROM == kFromQ8) from_q8(row.h[v].bits, row.scale[v], p.q8.format, h[v]);
+      else row.h[v].get(h[v]);
+      row.in[v].get(out[v]);
       float g[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (c < p.d) load_gamma(p.gamma, p.gamma_f32, c, g);
 #pragma unroll
@@ -234,6 +295,7 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_backward_kernel(const NormBa
         s[1] = __builtin_fmaf(g[i] * dy[v][i], h[v][i], s[1]);
       }
     }
+    if (kAhead && t + stride < p.T) load(row, t + stride);
     row_sum<R>(s, lds, turn);
     turn ^= 1;
     const float rstd = 1.0f / __builtin_sqrtf(s[0] / (float)p.d + p.eps);
@@ -242,16 +304,15 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_backward_kernel(const NormBa
     for (int v = 0; v < NV; ++v) {
       const int c = (v * R + lane) * 8;
       if (c >= p.d) continue;
-      float g[8], out[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      float g[8];
       load_gamma(p.gamma, p.gamma_f32, c, g);
-      if (p.dsum_in != nullptr) load8(static_cast<const S*>(p.dsum_in) + t * p.ld_dsum_in + c, out);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float n = h[v][i] * rstd;
-        out[i] = __builtin_fmaf(rstd, __builtin_fmaf(-n, along, g[i] * dy[v][i]), out[i]);
+        out[v][i] = __builtin_fmaf(rstd, __builtin_fmaf(-n, along, g[i] * dy[v][i]), out[v][i]);
         dgamma[v][i] = __builtin_fmaf(dy[v][i], n, dgamma[v][i]);
       }
-      if (p.dsum != nullptr) store8(static_cast<S*>(p.dsum) + t * p.ld_dsum + c, out);
+      if (p.dsum != nullptr) store8(static_cast<S*>(p.dsum) + t * p.ld_dsum + c, out[v]);
     }
   }
   if (p.dgamma == nullptr) return;
@@ -262,23 +323,27 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_backward_kernel(const NormBa
   }
 }
 
-// Adds `n` partial rows: 16 lanes of four columns, 16 strips of rows, joined in LDS.
-__global__ __launch_bounds__(256) void norm_gamma_kernel(const float* __restrict__ partials, int n, int d, int accumulate,
-                                                         float* __restrict__ dgamma) {
-  __shared__ f32x4_t strip[16][16];
-  const int q = threadIdx.x & 15, r0 = threadIdx.x >> 4;
-  const int c = ((int)blockIdx.x * 16 + q) * 4;
+// Adds `n` partial rows: 8 lanes of four columns, 64 strips of rows, joined in LDS.
+constexpr int kGammaThreads = 512, kGammaStrips = kGammaThreads / 8;
+__global__ __launch_bounds__(kGammaThreads) void norm_gamma_kernel(const float* __restrict__ partials, int n, int d,
+                                                                   int accumulate, float* __restrict__ dgamma) {
+  __shared__ f32x4_t strip[kGammaStrips][8];
+  const int q = threadIdx.x & 7, r0 = threadIdx.x >> 3;
+  const int c = ((int)blockIdx.x * 8 + q) * 4;
   f32x4_t s = {0.f, 0.f, 0.f, 0.f};
   if (c < d) {
-#pragma unroll 4
-    for (int r = r0; r < n; r += 16) s += *reinterpret_cast<const f32x4_t*>(partials + (int64_t)r * d + c);
+#pragma unroll 8
+    for (int r = r0; r < n; r += kGammaStrips) s += *reinterpret_cast<const f32x4_t*>(partials + (int64_t)r * d + c);
   }
   strip[r0][q] = s;
   __syncthreads();
+  for (int half = kGammaStrips / 2; half > 0; half >>= 1) {
+    if (r0 < half) strip[r0][q] += strip[r0 + half][q];
+    __syncthreads();
+  }
   if (r0 == 0 && c < d) {
-    for (int k = 1; k < 16; ++k) s += strip[k][q];
     f32x4_t* out = reinterpret_cast<f32x4_t*>(dgamma + c);
-    *out = accumulate ? *out + s : s;
+    *out = accumulate ? *out + strip[0][q] : strip[0][q];
   }
 }
 
@@ -289,7 +354,6 @@ __global__ __launch_bounds__(256) void checkpoint_store_kernel(const S* __restri
   const int shift = group_shift_of(q8.group);
   const int padded = (d + q8.group - 1) >> shift << shift;
   for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < T; t += (int64_t)gridDim.x * 4) {
-#pragma unroll 4
     for (int c = (threadIdx.x & 63) * 8; c < padded; c += 512) {
       float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (c < d) load8(x + t * ld_x + c, v);
@@ -363,12 +427,14 @@ int launch_rmsnorm_forward(const NormForwardArgs& a, bool stream_f32, hipStream_
   return stream_f32 ? forward_of<float>(a, stream) : forward_of<__bf16>(a, stream);
 }
 
-// Partial sums of dgamma: at least four rows each, so that they cost a fraction of the rows themselves.
+// Partial sums of dgamma, one for every group of lanes: two blocks a CU keep the memory busy, with at least two rows for a
+// group, so that the next one can be on its way, and the sums cost a fraction of the rows.
+constexpr int64_t kBackwardBlocks = 512;   // 16384 x 4096: 110 us, with 256 blocks 119; 8192 x 8192: 114, with 768 blocks 133
 int64_t norm_backward_partials(int64_t T, int32_t d) {
-  const int64_t rows = kThreads / lanes_for(d);
-  int64_t n = (T + 3) / 4;
-  n = n > 1024 ? 1024 : n;
-  return (n + rows - 1) / rows * rows;
+  const int64_t groups = kThreads / lanes_for(d);
+  int64_t blocks = (T + 2 * groups - 1) / (2 * groups);
+  blocks = blocks > kBackwardBlocks ? kBackwardBlocks : blocks;
+  return blocks * groups;
 }
 
 int launch_rmsnorm_backward(const NormBackwardArgs& a, bool stream_f32, hipStream_t stream) {
@@ -380,7 +446,7 @@ int launch_rmsnorm_backward(const NormBackwardArgs& a, bool stream_f32, hipStrea
     else rc = backward_of<kFromBf16, __bf16>(a, partials, stream);
   }
   if (rc != 0 || a.dgamma == nullptr) return rc;
-  return launch_kernel(norm_gamma_kernel, dim3((unsigned)((a.d + 63) / 64)), dim3(256), stream, a.partials, (int)partials,
+  return launch_kernel(norm_gamma_kernel, dim3((unsigned)((a.d + 31) / 32)), dim3(kGammaThreads), stream, a.partials, (int)partials,
                        a.d, a.accumulate, a.dgamma);
 }
 
