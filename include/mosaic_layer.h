@@ -129,7 +129,8 @@ int mosaic_gated_ffn_forward(const void *x, int64_t ld_x, const void *w_gate, co
  *   accumulate nonzero: the weight gradients are added to what dw_gate and dw_up hold (32-bit only), so that a batch can be
  *              taken in parts
  *   workspace  dev, 16-byte aligned, mosaic_gated_ffn_backward_workspace_bytes(T, d, F, q8 != NULL) bytes: dg and du,
- *              4 T F bytes, the restored input, 2 T d, and for few rows partial sums of dx
+ *              4 T F bytes, the restored input, 2 T d, and for up to 4096 rows partial sums of dx.  A
+ *              workspace for T rows serves fewer rows, too
  */
 int64_t mosaic_gated_ffn_backward_workspace_bytes(int64_t T, int32_t d, int32_t F, int32_t q8_input);
 int mosaic_gated_ffn_backward(const void *dout, int64_t ld_dout, const void *x, int64_t ld_x, const mosaic_q8_rows *q8,

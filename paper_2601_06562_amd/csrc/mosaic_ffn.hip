@@ -204,10 +204,14 @@ __device__ __forceinline__ void pack(Quad& w, const float (&v)[4]) {
   w[1] = u.y;
 }
 
-// Persistent blocks.  The blocks of an XCD take its run of tiles in turn, and the copies of a block's next tile are under way
-// while the results of the last one are worked out and stored.
+// LDS of a tile: a ring of SP slots for P, of SQ for Q.
+constexpr int ring_bytes(int TP, int TQ, int SP, int SQ) { return (SP * TP + SQ * TQ) * kStepK * 2; }
+
+// The tiles of one product, dealt to `blocks` blocks of which this is number `block`.  The blocks of an XCD take its run of
+// tiles in turn, and the copies of a block's next tile are under way while the results of the last one are worked out and
+// stored.
 template <int MODE, int TP, int TQ, int SP, int SQ, int ACT>
-__global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
+__device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int block, int blocks) {
   constexpr bool kGated = MODE == kForward || MODE == kRecompute;
   constexpr bool kRowP = !kGated, kRowQ = MODE == kDw;
   constexpr int kTileP = TP, kTileQ = TQ, kBlocksP = TP / 32, QB = TQ / 64;   // blocks of a wave
@@ -219,19 +223,18 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
   // a copy between two groups of products all the time.
   constexpr bool kSplit = SP != SQ;
   static_assert(!kSplit || SP == SQ + 1, "the waits of the loop");
-  __shared__ __attribute__((aligned(1024))) char smem[SP * kBytesP + SQ * kBytesQ];   // a ring of slots for each operand
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wp = wave >> 2, wq = wave & 3;
   const int wave_p = kGated ? wq : wave;   // gated: waves 0..3 copy gate rows, waves 4..7 the up rows behind them
 
-  // Workgroup b runs on XCD b % 8; every XCD gets a run of tiles, and within it panels of kPanel Q tiles, so that what is in
+  // Block b runs on XCD b % 8; every XCD gets a run of tiles, and within it panels of kPanel Q tiles, so that what is in
   // flight behind one L2 shares both operands.
   const int per_split = a.tiles_p * a.tiles_q, n = per_split * a.splits;
-  const int xcd = (int)blockIdx.x % kXcds;
-  const int stride = (int)gridDim.x / kXcds + (xcd < (int)gridDim.x % kXcds ? 1 : 0);
+  const int xcd = block % kXcds;
+  const int stride = blocks / kXcds + (xcd < blocks % kXcds ? 1 : 0);
   int id = xcd * (n / kXcds) + (xcd < n % kXcds ? xcd : n % kXcds);   // the run's first tile
   const int end = id + n / kXcds + (xcd < n % kXcds ? 1 : 0);
-  id += (int)blockIdx.x / kXcds;
+  id += block / kXcds;
   if (id >= end) return;
 
   const int seg_steps = (int)((a.depth + kStepK - 1) / kStepK);
@@ -517,6 +520,21 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
   }
 }
 
+template <int MODE, int TP, int TQ, int SP, int SQ, int ACT>
+__global__ __launch_bounds__(kThreads) void ffn_gemm_kernel(const GemmArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[ring_bytes(TP, TQ, SP, SQ)];
+  run_tiles<MODE, TP, TQ, SP, SQ, ACT>(a, smem, (int)blockIdx.x, (int)gridDim.x);
+}
+
+// Both gradients in one launch, a tile a block: the first `blocks_x` (a multiple of the XCDs) take dx, and as they end the
+// others follow on the CUs that come free.  For sizes at which neither product fills the chip.
+template <int TP, int TQ, int SP, int SQ>
+__global__ __launch_bounds__(kThreads) void ffn_gradients_kernel(const GemmArgs x, const GemmArgs w, int blocks_x) {
+  __shared__ __attribute__((aligned(1024))) char smem[ring_bytes(TP, TQ, SP, SQ)];
+  if ((int)blockIdx.x < blocks_x) run_tiles<kDx, TP, TQ, SP, SQ, 0>(x, smem, (int)blockIdx.x, blocks_x);
+  else run_tiles<kDw, TP, TQ, SP, SQ, 0>(w, smem, (int)blockIdx.x - blocks_x, (int)gridDim.x - blocks_x);
+}
+
 #ifdef __HIP_DEVICE_COMPILE__
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const char* base) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, kOutside, 0x00020000);
@@ -655,6 +673,54 @@ Choice choose_tile(int64_t rows_p, int64_t rows_q, bool gated, int64_t steps, in
   return best;
 }
 
+// How the gradients of a backward pass are taken: in how many parts of K dx is summed, and in which tiles both products go
+// out together (-1: in launches of their own).  The parts follow from the sizes alone, whichever gradients a call wants: dx
+// has the same bits in every call.
+struct GradientPlan { int32_t splits, tile; };
+constexpr int64_t kMostParts = 16, kPartRows = 8192;   // parts, and parts times rows
+constexpr double kLaunchUs = 4.0, kJoinBytesPerUs = 4e6;   // joining parts: a launch, and 8 bytes an element and part
+GradientPlan plan_gradients(int64_t T, int32_t d, int32_t F) {
+  GradientPlan plan = {1, -1};
+  if (T == 0 || T > kLaunchRows) return plan;
+  const int64_t steps_x = 2 * tiles(F, kStepK), steps_w = tiles(T, kStepK);
+  const double dw = choose_tile(d, 2 * (int64_t)F, false, steps_w, 1).us;
+  double least = 0.0;
+  for (int32_t s = 1; s == 1 || (s <= kMostParts && s * T <= kPartRows && s * 4 <= steps_x); ++s) {
+    const double join = s == 1 ? 0.0 : kLaunchUs + (double)(T * d) * 8.0 * s / kJoinBytesPerUs;
+    const double apart = choose_tile(d, T, false, steps_x, s).us + dw + kLaunchUs + join;
+    if (s == 1 || apart < least) {
+      least = apart;
+      plan = {s, -1};
+    }
+    for (int i : {0, 1, 3}) {
+      const Tile& t = kTiles[i];
+      const int64_t each_x = tiles(steps_x, s), n_x = tiles(d, t.p) * tiles(T, t.q) * s;
+      const int64_t n_w = tiles(d, t.p) * tiles(2 * (int64_t)F, t.q);
+      if (n_x + n_w > 8 * kCus) continue;
+      const int64_t longest = each_x > steps_w ? each_x : steps_w;
+      double rounds = (double)(n_x * each_x + n_w * steps_w) / kCus;      // as even as the blocks allow
+      if (n_x + n_w > kCus) rounds += 0.5 * (double)steps_w;
+      if (rounds < (double)longest) rounds = (double)longest;
+      const double together = rounds * t.step + join;
+      if (together < least) {
+        least = together;
+        plan = {s, i};
+      }
+    }
+  }
+  return plan;
+}
+
+template <int TP, int TQ, int SP, int SQ>
+int launch_together(GemmArgs x, GemmArgs w, hipStream_t stream) {
+  x.tiles_p = w.tiles_p = (int32_t)tiles(x.rows_p, TP);
+  x.tiles_q = (int32_t)tiles(x.rows_q, TQ);
+  w.tiles_q = (int32_t)tiles(w.rows_q, TQ);
+  const int blocks_x = (int)tiles((int64_t)x.tiles_p * x.tiles_q * x.splits, kXcds) * kXcds;
+  return launch_kernel(ffn_gradients_kernel<TP, TQ, SP, SQ>, dim3((unsigned)(blocks_x + w.tiles_p * w.tiles_q)), dim3(kThreads),
+                       stream, x, w, blocks_x);
+}
+
 template <int MODE, int ACT>
 int launch_gemm(const GemmArgs& a, hipStream_t stream) {
   constexpr bool kGated = MODE == kForward || MODE == kRecompute;
@@ -681,19 +747,8 @@ int launch_gated(const GemmArgs& a, int activation, hipStream_t stream) {
 
 }  // namespace
 
-// Parts of K that dx is summed in: where its tiles leave CUs idle, as many as save more than joining the parts costs (a
-// launch of ~4 us, and 8 bytes an element and part through the caches).
-int32_t ffn_dx_splits(int64_t T, int32_t d, int32_t F) {
-  if (T == 0 || T > kLaunchRows) return 1;
-  const int64_t steps = 2 * tiles(F, kStepK);
-  int32_t best = 1;
-  double least = choose_tile(d, T, false, steps, 1).us;
-  for (int32_t s = 2; s <= 16 && s * 4 <= steps; ++s) {
-    const double us = choose_tile(d, T, false, steps, s).us + 4.0 + (double)(T * d) * 8.0 * s / 4e6;
-    if (us < least) { least = us; best = s; }
-  }
-  return best;
-}
+// Rows of 32-bit partial sums that dx may take for up to T rows: no less for more rows, so that a workspace serves fewer too.
+int64_t ffn_partial_rows(int64_t T) { return T * kMostParts < kPartRows ? T * kMostParts : kPartRows; }
 
 int launch_gated_ffn_forward(const FfnForwardArgs& f, hipStream_t stream) {
   GemmArgs a = {};
@@ -730,7 +785,7 @@ int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
     a.rows_p = f.F;
     a.depth = f.d;
     a.splits = 1;
-      a.F = f.F;
+    a.F = f.F;
     a.ld_dout = f.ld_dout * 2;
     a.dout = static_cast<const char*>(f.dout) + t * a.ld_dout;
     a.ld_out0 = f.ld_out * 2;
@@ -739,48 +794,50 @@ int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
     a.out1 = static_cast<char*>(f.grads) + t * ld_grads;
     if (launch_gated<kRecompute>(a, f.activation, stream) != 0) return -1;
   }
-  const int32_t splits = ffn_dx_splits(f.T, f.d, f.F);
+  const GradientPlan plan = plan_gradients(f.T, f.d, f.F);
+  GemmArgs x = {};
+  x.p0 = static_cast<const char*>(f.w_gate);
+  x.p1 = static_cast<const char*>(f.w_up);
+  x.ld_p = f.ld_w * 2;
+  x.ld_q = ld_grads;
+  x.rows_p = f.d;
+  x.depth = f.F;
+  x.splits = plan.splits;
+  x.f32 = plan.splits > 1;      // then all rows are in one launch
+  x.ld_out0 = x.f32 ? (int64_t)f.d * 4 : f.ld_dx * 2;
+  GemmArgs w = {};
+  w.p0 = w.p1 = static_cast<const char*>(f.x);
+  w.q = static_cast<const char*>(f.grads);
+  w.ld_p = f.ld_x * 2;
+  w.ld_q = ld_grads;
+  w.rows_q = 2 * (int64_t)f.F;
+  w.rows_p = f.d;
+  w.depth = f.T;
+  w.splits = 1;
+  w.F = f.F;
+  w.f32 = f.dw_f32;
+  w.accumulate = f.accumulate;
+  w.out0 = static_cast<char*>(f.dw_gate);
+  w.out1 = static_cast<char*>(f.dw_up);
+  w.ld_out0 = f.ld_dw * (f.dw_f32 ? 4 : 2);
+  const bool together = plan.tile >= 0 && f.dx != nullptr && f.dw_gate != nullptr;
   for (int64_t t = 0; f.dx != nullptr && t < f.T; t += kLaunchRows) {
-    GemmArgs a = {};
-    a.p0 = static_cast<const char*>(f.w_gate);
-    a.p1 = static_cast<const char*>(f.w_up);
-    a.ld_p = f.ld_w * 2;
-    a.ld_q = ld_grads;
-    a.rows_q = f.T - t < kLaunchRows ? f.T - t : kLaunchRows;
-    a.q = static_cast<const char*>(f.grads) + t * ld_grads;
-    a.rows_p = f.d;
-    a.depth = f.F;
-    a.splits = splits;
-    a.f32 = splits > 1;      // then all rows are in one launch
-    a.ld_out0 = a.f32 ? (int64_t)f.d * 4 : f.ld_dx * 2;
-    a.out0 = a.f32 ? reinterpret_cast<char*>(f.partials) : static_cast<char*>(f.dx) + t * a.ld_out0;
-    if (launch_gemm<kDx, 0>(a, stream) != 0) return -1;
+    x.rows_q = f.T - t < kLaunchRows ? f.T - t : kLaunchRows;
+    x.q = static_cast<const char*>(f.grads) + t * ld_grads;
+    x.out0 = x.f32 ? reinterpret_cast<char*>(f.partials) : static_cast<char*>(f.dx) + t * x.ld_out0;
+    const int rc = !together ? launch_gemm<kDx, 0>(x, stream)
+                   : plan.tile == 0 ? launch_together<256, 256, 3, 2>(x, w, stream)
+                   : plan.tile == 1 ? launch_together<128, 256, 3, 3>(x, w, stream)
+                                    : launch_together<128, 128, 4, 4>(x, w, stream);
+    if (rc != 0) return -1;
   }
-  if (f.dx != nullptr && splits > 1) {
+  if (f.dx != nullptr && plan.splits > 1) {
     const int64_t blocks = tiles(f.T * (f.d / 8), 256);
     if (launch_kernel(ffn_join_kernel, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), stream, f.partials,
-                      (int)splits, f.T, f.d, static_cast<__bf16*>(f.dx), f.ld_dx) != 0)
+                      (int)plan.splits, f.T, f.d, static_cast<__bf16*>(f.dx), f.ld_dx) != 0)
       return -1;
   }
-  if (f.dw_gate != nullptr) {
-    GemmArgs a = {};
-    a.p0 = static_cast<const char*>(f.x);
-    a.p1 = a.p0;
-    a.q = static_cast<const char*>(f.grads);
-    a.ld_p = f.ld_x * 2;
-    a.ld_q = (int64_t)f.F * 4;
-    a.rows_q = 2 * (int64_t)f.F;
-    a.rows_p = f.d;
-    a.depth = f.T;
-    a.splits = 1;
-    a.F = f.F;
-    a.f32 = f.dw_f32;
-    a.accumulate = f.accumulate;
-    a.out0 = static_cast<char*>(f.dw_gate);
-    a.out1 = static_cast<char*>(f.dw_up);
-    a.ld_out0 = f.ld_dw * (f.dw_f32 ? 4 : 2);
-    if (launch_gemm<kDw, 0>(a, stream) != 0) return -1;
-  }
+  if (f.dw_gate != nullptr && !together && launch_gemm<kDw, 0>(w, stream) != 0) return -1;
   return 0;
 }
 

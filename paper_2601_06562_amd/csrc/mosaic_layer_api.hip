@@ -39,16 +39,19 @@ int check_q8(const mosaic_q8_rows* q, int32_t d) {
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// Workspace of a feed-forward backward pass: dg | du, the restored input, the partial sums of dx.
+// Workspace of a feed-forward backward pass: dg | du, the restored input, the partial sums of dx, which only up to
+// kPartialT rows are summed in parts.  A workspace for T rows serves fewer rows, too.
 struct FfnSpace {
   int64_t restored, partials, total;   // offsets, bytes
 };
+constexpr int64_t kPartialT = 4096;
 FfnSpace ffn_space(int64_t T, int32_t d, int32_t F, bool q8) {
   FfnSpace s;
   s.restored = round_up(4 * T * F, 256);
   s.partials = s.restored + (q8 ? round_up(2 * T * d, 256) : 0);
-  const int64_t splits = mosaic::ffn_dx_splits(T, d, F);
-  s.total = s.partials + (splits > 1 ? 4 * splits * T * d : 0);
+  const int64_t few = T < kPartialT ? T : kPartialT;   // the most that up to T rows need with their sums
+  const int64_t with_sums = round_up(4 * few * F, 256) + (q8 ? round_up(2 * few * d, 256) : 0) + 4 * mosaic::ffn_partial_rows(few) * d;
+  s.total = with_sums > s.partials ? with_sums : s.partials;
   return s;
 }
 

@@ -67,11 +67,11 @@ struct FfnBackwardArgs {
   void* dw_gate;  // or nullptr
   void* dw_up;
   void* grads;      // bf16 [T, 2 F]: dg | du
-  float* partials;  // fp32 [ffn_dx_splits(T, d, F), T, d], unused with one split
+  float* partials;  // fp32 [ffn_partial_rows(T), d]: sums of dx over parts of K
   int64_t ld_dout, ld_x, ld_w, ld_out, ld_dx, ld_dw, T;
   int32_t d, F, activation, dw_f32, accumulate;
 };
-int32_t ffn_dx_splits(int64_t T, int32_t d, int32_t F);
+int64_t ffn_partial_rows(int64_t T);
 int launch_gated_ffn_backward(const FfnBackwardArgs& a, hipStream_t stream);
 
 #ifdef __HIPCC__

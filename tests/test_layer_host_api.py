@@ -161,6 +161,15 @@ def test_workspaces():
     assert b.mosaic_gated_ffn_backward_workspace_bytes(4, 100, 64) == 0
 
 
+def test_a_workspace_serves_fewer_rows():
+    for d, F in ((64, 64), (512, 384), (1024, 4096), (4096, 12288)):
+        for q8_input in (False, True):
+            need = [b.mosaic_gated_ffn_backward_workspace_bytes(T, d, F, q8_input) for T in (*range(0, 9000, 37), 20000, 131072)]
+            assert need == sorted(need)
+        need = [b.mosaic_rmsnorm_backward_workspace_bytes(T, d) for T in (*range(0, 9000, 37), 20000, 131072)]
+        assert need == sorted(need)
+
+
 def test_the_binding_checks_shapes_and_types():
     x = torch.zeros((4, 64), dtype=torch.bfloat16)
     w = torch.zeros((128, 64), dtype=torch.bfloat16)
