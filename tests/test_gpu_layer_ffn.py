@@ -104,6 +104,31 @@ def test_gradients(T, d, F, kept):
     assert torch.equal(dw2, dw)
 
 
+@pytest.mark.parametrize("T,d,F", [(4100, 4104, 4104), (8201, 4104, 2056), (700, 2200, 5000), (9000, 264, 1032), (1100, 5000, 1096)])
+def test_more_tiles_than_blocks(T, d, F):
+    """Sizes of several tiles a block, ragged in every direction; the plain statement in 64 bits on the device, with the bounds
+    of the sizes above."""
+    gen, x, wg, wu = inputs(T, d, F, T + 3 * d + 5 * F, 8)
+    dout, _ = matrix(T, F, gen, 8, 0.01)
+    out, out_full = matrix(T, F, gen, 8)
+    dx, dx_full = matrix(T, d, gen, 8)
+    dw, dw_full = matrix(2 * F, d, gen, 8)
+    work = torch.empty(b.mosaic_gated_ffn_backward_workspace_bytes(T, d, F), dtype=torch.uint8, device=DEV)
+    b.mosaic_gated_ffn_forward(x, wg, wu, out)
+    b.mosaic_gated_ffn_backward(dout, x, wg, wu, dx, dw[:F], dw[F:], work)
+    exact, bound = ref.ffn_bound(x, wg, wu, "silu")
+    assert ((out.double() - exact).abs() <= bound).all()
+    del exact, bound
+    want = ref.ffn_gradients(dout, x, wg, wu, "silu")
+    for got, w in zip((dx, dw[:F], dw[F:]), want):
+        assert ref.relative(got, w) <= ref.U_BF16
+        # The elements are sums of many terms of the same spread, each rounded to bf16: an element's error has about 2^-8 / sqrt 3
+        # of the elements' root mean square as its spread; sixteen of those, and the result's own rounding.
+        rms = w.square().mean().sqrt()
+        assert ((got.double() - w).abs() <= 16 * ref.U_BF16 / 3 ** 0.5 * rms + ref.U_BF16 * w.abs()).all()
+    assert (out_full[:, F:] == 777.0).all() and (dx_full[:, d:] == 777.0).all() and (dw_full[:, d:] == 777.0).all()
+
+
 @pytest.mark.parametrize("T,d,F", [(1, 64, 64), (90, 136, 264), (700, 512, 384)])
 def test_weight_gradients_in_parts(T, d, F):
     """32-bit weight gradients, a batch taken in parts: the parts add up to what the whole gives."""
