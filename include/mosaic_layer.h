@@ -8,7 +8,8 @@
  * The conventions of mosaic.h hold: device pointers owned by the caller, `stream` a hipStream_t (NULL = the default
  * stream), calls only enqueue, allocate nothing and keep nothing; argument errors are found before anything is enqueued.
  * Matrices are row-major with dense rows; ld_* is the distance of two rows in elements.
- *   bf16 and 32-bit matrices: base 16-byte aligned, ld_* a multiple of 8
+ *   bf16 and 32-bit matrices: base 16-byte aligned, ld_* a multiple of 8, at most 2^21
+ *   an output overlaps an input only where that is said to be allowed
  *   every sum over a row, a column or a product is held in 32 bits; a result is rounded to its type once.  The exception is
  *   said at mosaic_gated_ffn_backward
  * T = rows (positions; 0 <= T < 2^31; T == 0 enqueues nothing but the clearing of sums over rows), d = hidden size,

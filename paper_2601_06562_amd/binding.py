@@ -1,7 +1,7 @@
 """ctypes binding of libmosaic.so -- argument marshalling only.
 
 Every step of the path runs in the HIP kernels behind the C ABI declared in
-``include/mosaic.h``; the functions here have the same names and only turn torch tensors
+``include/mosaic.h`` and ``include/mosaic_layer.h``; the functions here have the same names and only turn torch tensors
 into device pointers.  There is no CPU or PyTorch fallback: if the library is missing,
 loading raises.
 """
