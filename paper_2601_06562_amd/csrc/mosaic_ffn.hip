@@ -156,7 +156,7 @@ struct Reader {
 
 // The four lanes that hold one Q row (16 apart) each have 4 consecutive P rows of every block; afterwards each has 4 NB
 // consecutive ones, NB = 2 or 4 blocks, in order: what is stored, or was loaded, is 16 bytes a lane.  `scatter` takes
-// gathered quads back.
+// gathered quads back.  Three blocks stay as they are, 8 bytes a lane: only tiles of few rows have them.
 typedef uint32_t Quad[2];   // four bf16
 __device__ __forceinline__ void swap32(Quad& a, Quad& b) {
 #pragma unroll
@@ -175,13 +175,17 @@ __device__ __forceinline__ void swap16(Quad& a, Quad& b) {
   }
 }
 template <int NB>
+__device__ __forceinline__ int first_of(int lane) { return (NB == 3 ? 4 : 4 * NB) * (lane >> 4); }   // a lane's first P row
+template <int NB>
 __device__ __forceinline__ void gather(Quad (&w)[NB]) {
+  if constexpr (NB == 3) return;
   if constexpr (NB == 4) { swap32(w[0], w[2]); swap32(w[1], w[3]); swap16(w[2], w[3]); }
   else swap32(w[0], w[1]);
   swap16(w[0], w[1]);
 }
 template <int NB>
 __device__ __forceinline__ void scatter(Quad (&w)[NB]) {
+  if constexpr (NB == 3) return;
   swap16(w[0], w[1]);
   if constexpr (NB == 4) { swap16(w[2], w[3]); swap32(w[1], w[3]); swap32(w[0], w[2]); }
   else swap32(w[0], w[1]);
@@ -189,14 +193,29 @@ __device__ __forceinline__ void scatter(Quad (&w)[NB]) {
 // Gathered quads to or from `row`, whose element `c` is the first of this lane's; `end`: elements there are, a multiple of 8.
 template <int NB>
 __device__ __forceinline__ void store_quads(char* row, int c, int end, const Quad (&w)[NB]) {
+  if constexpr (NB == 3) {
 #pragma unroll
-  for (int i = 0; i < NB; i += 2)
+    for (int i = 0; i < NB; ++i)
+      if (c + 16 * i < end) *reinterpret_cast<uint2*>(row + (int64_t)(c + 16 * i) * 2) = uint2{w[i][0], w[i][1]};
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i + 1 < NB; i += 2)
     if (c + 4 * i < end) *reinterpret_cast<u32x4_t*>(row + (int64_t)(c + 4 * i) * 2) = u32x4_t{w[i][0], w[i][1], w[i + 1][0], w[i + 1][1]};
 }
 template <int NB>
 __device__ __forceinline__ void load_quads(const char* row, int c, int end, bool in, Quad (&w)[NB]) {
+  if constexpr (NB == 3) {
 #pragma unroll
-  for (int i = 0; i < NB; i += 2) {
+    for (int i = 0; i < NB; ++i) {
+      uint2 v = {0u, 0u};
+      if (in && c + 16 * i < end) v = *reinterpret_cast<const uint2*>(row + (int64_t)(c + 16 * i) * 2);
+      w[i][0] = v.x; w[i][1] = v.y;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i + 1 < NB; i += 2) {
     u32x4_t v = {0u, 0u, 0u, 0u};
     if (in && c + 4 * i < end) v = *reinterpret_cast<const u32x4_t*>(row + (int64_t)(c + 4 * i) * 2);
     w[i][0] = v[0]; w[i][1] = v[1]; w[i + 1][0] = v[2]; w[i + 1][1] = v[3];
@@ -249,7 +268,7 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
   const int all_steps = MODE == kDx ? 2 * seg_steps : seg_steps;
 
   // Of the tile whose copies are issued.
-  int split, p_row, step0, step1, placed_p, placed_q;   // p_row: first P row; gated: first feature
+  int split, p_row, step0, step1, placed_p, placed_q, turned = 0;   // p_row: first P row; gated: first feature
   int64_t q_row;
   const char *p_base0, *p_base1, *q_base;
   CopierP cp;
@@ -275,6 +294,10 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
     placed_p = placed_q = kStepK;
     step0 = (int)((int64_t)all_steps * split / a.splits);
     step1 = (int)((int64_t)all_steps * (split + 1) / a.splits);
+    // With one Q tile the time goes to the weights, which tiles read from their start: begun at different places of K they are
+    // spread over the memory's channels, where rows a power of two apart would meet in few (32 rows of d 4096, F 12288: 44.6
+    // us, so 41.2; d 3584, F 18944: 57.1 and 56.3).
+    if (kGated) turned = a.tiles_q == 1 ? tile % all_steps : 0;
   };
 
   // Where an operand's copies come from, step after step.  What lies past the end of K comes as zeros, and so do steps past
@@ -284,13 +307,22 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
   Walk walk_p, walk_q;
   auto find = [&](int step, int& seg, int64_t& k, Walk& w) __attribute__((always_inline)) {   // k there are in `step`
     seg = MODE == kDx && step >= seg_steps ? 1 : 0;
-    const int at = step - seg * seg_steps, full = (int)(a.depth / kStepK);
-    k = (int64_t)at * kStepK;
+    const int full = (int)(a.depth / kStepK);
+    int at = step - seg * seg_steps, end = step1 - seg * seg_steps;
     if (step >= step1) {
+      k = 0;
       w.plain = 0x7fffffff;
       return 0;
     }
-    const int last = step1 - seg * seg_steps < full ? step1 - seg * seg_steps : full;
+    if (kGated) {   // around K, from step `turned` on
+      at += turned;
+      if (at >= end) {
+        at -= end;
+        end = turned;
+      }
+    }
+    k = (int64_t)at * kStepK;
+    const int last = end < full ? end : full;
     w.plain = at < last ? last - 1 - at : 0;
     return at < full ? kStepK : (int)(a.depth - k);
   };
@@ -425,7 +457,7 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
       // Accumulator register r of a lane: P row 4 (lane / 16) + r, Q row lane % 16 of the block.  Gathered, a lane has
       // 4 NB consecutive P rows from run on.
       constexpr int kHalf = kBlocksP / 2, NB = kGated ? (kHalf < 4 ? kHalf : 4) : 4;
-      const int sub = 4 * (lane >> 4), run = 4 * NB * (lane >> 4);
+      const int sub = 4 * (lane >> 4), run = first_of<NB>(lane);
       Quad grad[MODE == kRecompute ? QB : 1][NB];   // of the outputs, all asked for ahead of their use
       if constexpr (MODE == kRecompute) {
 #pragma unroll
@@ -609,30 +641,35 @@ __device__ __forceinline__ bf16x8_t load_at(__amdgpu_buffer_rsrc_t r, uint32_t o
 }
 #endif
 
-// Up to 16 rows: the weights are read once, and that is all the time goes to.  A block takes 16 features of both
+// A few rows, TB blocks of 16: the weights are read once, and that is all the time goes to.  A block takes 16 features of both
 // projections; its four waves take the 64 k pieces of their rows in turn, straight into registers, so that 512 consecutive
-// bytes of a row are asked for at once and no wave waits for another before the sums meet in LDS.
-// 1 row of 12288 x 4096: 34 us, the weights at 5.9 TB/s (a tile of 128 x 64: 43 us); 16 rows 40 us, where the tile takes
-// 43; from 17 rows on it would be 45 and more, for every block reads all of x.
-constexpr int kFewRows = 16, kFewThreads = 256;
+// bytes of a row are asked for at once and no wave waits for another before the sums meet in LDS.  All of x is read by every
+// block, from L2.
+// 1 row of d 4096, F 12288: 34 us, the weights at 5.9 TB/s; of 1024 x 4096, 32 rows 6.4 us and 64 rows 8.2, where tiles take
+// 9.5.  32 features a block were slower throughout (1 row 48 us), fewer pieces under way at one row (2: 41 us).
+constexpr int kFewThreads = 256;
 
-template <int ACT>
+template <int ACT, int TB>
 __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(const GemmArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr int kDeep = 4;   // pieces under way
-  __shared__ f32x4_t sums[4][2][64];
+  __shared__ f32x4_t sums[4][2 * TB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int f0 = (int)blockIdx.x * 16;
+  const int f0 = (int)blockIdx.x * (16);
   const int row = lane & 15, part = (lane >> 4) * 8;
+  const int d = (int)a.depth;
   // A lane's fragments of a piece: k = 32 h + part .. + 7 of its row, h = 0, 1.  What lies past the end of the rows or of K
   // is asked for outside the buffers and comes as zeros.
-  const int d = (int)a.depth;
   const __amdgpu_buffer_rsrc_t gate = buffer_at(a.p0 + (int64_t)f0 * a.ld_p), up = buffer_at(a.p1 + (int64_t)f0 * a.ld_p);
   const __amdgpu_buffer_rsrc_t x = buffer_at(a.q);
   const uint32_t at_f = f0 + row < a.rows_p ? (uint32_t)(row * a.ld_p) + part * 2 : kOutside;
-  const uint32_t at_x = row < a.rows_q ? (uint32_t)(row * a.ld_q) + part * 2 : kOutside;
-  struct Piece { bf16x8_t g[2], u[2], x[2]; };
-  f32x4_t acc_g = {0.f, 0.f, 0.f, 0.f}, acc_u = {0.f, 0.f, 0.f, 0.f};
+  uint32_t at_x[TB];
+#pragma unroll
+  for (int i = 0; i < TB; ++i) at_x[i] = 16 * i + row < a.rows_q ? (uint32_t)((16 * i + row) * a.ld_q) + part * 2 : kOutside;
+  struct Piece { bf16x8_t g[2], u[2], x[2][TB]; };
+  f32x4_t acc_g[TB], acc_u[TB];
+#pragma unroll
+  for (int t = 0; t < TB; ++t) acc_g[t] = acc_u[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   // Blocks begin at different places of K: side by side they would all ask for the same lines of x, and, rows lying a power of
   // two apart, for the same channels.
   const int rounds = (d + 4 * kStepK * kDeep - 1) / (4 * kStepK * kDeep);
@@ -649,7 +686,8 @@ __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(const GemmArgs a) 
         const uint32_t past = k + part < d ? 0 : kOutside;
         p[i].g[h] = load_at(gate, at_f | past, k * 2);
         p[i].u[h] = load_at(up, at_f | past, k * 2);
-        p[i].x[h] = load_at(x, at_x | past, k * 2);
+#pragma unroll
+        for (int t = 0; t < TB; ++t) p[i].x[h][t] = load_at(x, at_x[t] | past, k * 2);
       }
     }
     __builtin_amdgcn_sched_barrier(0);   // all of them under way: left to itself the compiler saves registers instead
@@ -657,29 +695,36 @@ __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(const GemmArgs a) 
     for (int i = 0; i < kDeep; ++i) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        acc_g = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[i].g[h], p[i].x[h], acc_g, 0, 0, 0);
-        acc_u = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[i].u[h], p[i].x[h], acc_u, 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+          acc_g[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[i].g[h], p[i].x[h][t], acc_g[t], 0, 0, 0);
+          acc_u[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[i].u[h], p[i].x[h][t], acc_u[t], 0, 0, 0);
+        }
       }
     }
   }
-  sums[wave][0][lane] = acc_g;
-  sums[wave][1][lane] = acc_u;
+#pragma unroll
+  for (int t = 0; t < TB; ++t) {
+    sums[wave][2 * t][lane] = acc_g[t];
+    sums[wave][2 * t + 1][lane] = acc_u[t];
+  }
   __syncthreads();
-  const int f = f0 + 4 * (lane >> 4);
-  if (wave != 0 || row >= a.rows_q || f >= a.rows_p) return;
+  const int f = f0 + 4 * (lane >> 4), q = 16 * wave + row;   // a wave, a block of rows
+  if (wave >= TB || q >= a.rows_q || f >= a.rows_p) return;
+  f32x4_t g = sums[0][2 * wave][lane], u = sums[0][2 * wave + 1][lane];
 #pragma unroll
   for (int w = 1; w < 4; ++w) {
-    acc_g += sums[w][0][lane];
-    acc_u += sums[w][1][lane];
+    g += sums[w][2 * wave][lane];
+    u += sums[w][2 * wave + 1][lane];
   }
   bf16x4_t o;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     float act, slope;
-    activate<ACT>(acc_g[r], act, slope);
-    o[r] = (__bf16)(act * acc_u[r]);
+    activate<ACT>(g[r], act, slope);
+    o[r] = (__bf16)(act * u[r]);
   }
-  *reinterpret_cast<bf16x4_t*>(a.out0 + row * a.ld_out0 + (int64_t)f * 2) = o;
+  *reinterpret_cast<bf16x4_t*>(a.out0 + q * a.ld_out0 + (int64_t)f * 2) = o;
 #endif
 }
 
@@ -718,22 +763,27 @@ int launch_tiles(GemmArgs a, int per_cu, hipStream_t stream) {
                        dim3(kThreads), stream, a);
 }
 
-// The tiles there are, and what one step of 64 k takes all CUs at work, in us.  A block's step is bound by the latency of its
-// copies or by the matrix cores, so a tile takes the same where it is alone and a launch takes whole rounds of tiles.
+// The tiles there are, what one step of 64 k takes all CUs at work, in us, and what filling a long ring adds.  A block's step is
+// bound by the latency of its copies or by the matrix cores, so a tile takes the same where it is alone and a launch takes
+// whole rounds of tiles.  Few rows of Q are bound by how many bytes are under way: there the rings take all LDS, and 96
+// features serve where 64 are more tiles than CUs (37 rows of d 3584, F 18944 in 50.8 us, of 128 features 56.4; 32 rows
+// of d 4096, F 12288 in 37.9 with six slots, 41.2 with three in two blocks a CU).
 // Times from 16 to 8192 rows of 12288 x 4096, 18944 x 3584, 5632 x 2048, 4096 x 1024 and 2048 x 512, forward and dw: in 130
-// sizes the choice is the fastest of the six, or within 2% of it, but for two (5 and 6%); the others take up to 2.7 times as long.
-struct Tile { int p, q; double step, step_alone; int per_cu; };
+// sizes the choice of those without long rings is the fastest, or within 2% of it, but for two (5 and 6%); the others take up to
+// 2.7 times as long.
+struct Tile { int p, q; double step, step_alone, fill; int per_cu; };
 constexpr Tile kTiles[] = {
-    {256, 256, 1.50, 1.50, 1}, {128, 256, 0.91, 0.91, 1}, {256, 128, 0.92, 0.92, 1},
-    {128, 128, 0.60, 0.60, 1}, {256, 64, 0.80, 0.80, 1},  {128, 64, 0.84, 0.57, 2},
+    {256, 256, 1.50, 1.50, 0.0, 1}, {128, 256, 0.91, 0.91, 0.0, 1}, {256, 128, 0.92, 0.92, 0.0, 1}, {128, 128, 0.60, 0.60, 0.0, 1},
+    {256, 64, 0.80, 0.80, 0.0, 1},  {192, 64, 0.70, 0.70, 0.0, 1},  {128, 64, 0.55, 0.55, 0.6, 1},  {128, 64, 0.84, 0.57, 0.0, 2},
 };
 struct Choice { int tile; double us; };
 Choice choose_tile(int64_t rows_p, int64_t rows_q, bool gated, int64_t steps, int64_t splits) {
   Choice best = {0, 0.0};
   for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
     const Tile& t = kTiles[i];
+    if (t.p == 192 && !gated) continue;   // (its rows across K would not be a power of two)
     const int64_t n = tiles(rows_p, gated ? t.p / 2 : t.p) * tiles(rows_q, t.q) * splits;
-    const double us = (double)tiles(n, kCus * t.per_cu) * (double)tiles(steps, splits) * (n <= kCus ? t.step_alone : t.step);
+    const double us = (double)tiles(n, kCus * t.per_cu) * (double)tiles(steps, splits) * (n <= kCus ? t.step_alone : t.step) + t.fill;
     if (i == 0 || us < best.us) best = {i, us};
   }
   return best;
@@ -796,13 +846,31 @@ int launch_gemm(const GemmArgs& a, hipStream_t stream) {
     case 2: return launch_tiles<MODE, 256, 128, 3, 3, ACT>(a, 1, stream);
     case 3: return launch_tiles<MODE, 128, 128, 4, 4, ACT>(a, 1, stream);
     case 4: return launch_tiles<MODE, 256, 64, 4, 4, ACT>(a, 1, stream);
+    case 5: if constexpr (kGated) return launch_tiles<MODE, 192, 64, 5, 5, ACT>(a, 1, stream);
+    case 6: return launch_tiles<MODE, 128, 64, 6, 6, ACT>(a, 1, stream);
     default: return launch_tiles<MODE, 128, 64, 3, 3, ACT>(a, 2, stream);
   }
 }
 
+template <int ACT, int TB>
+int launch_few_as(const GemmArgs& a, hipStream_t stream) {
+  return launch_kernel(ffn_few_kernel<ACT, TB>, dim3((unsigned)tiles(a.rows_p, 16)), dim3(kFewThreads), stream, a);
+}
 template <int ACT>
 int launch_few(const GemmArgs& a, hipStream_t stream) {
-  return launch_kernel(ffn_few_kernel<ACT>, dim3((unsigned)tiles(a.rows_p, 16)), dim3(kFewThreads), stream, a);
+  switch (tiles(a.rows_q, 16)) {
+    case 1: return launch_few_as<ACT, 1>(a, stream);
+    case 2: return launch_few_as<ACT, 2>(a, stream);
+    case 3: return launch_few_as<ACT, 3>(a, stream);
+    default: return launch_few_as<ACT, 4>(a, stream);
+  }
+}
+// Whether these rows go to the kernel for few: where its blocks are no more than the CUs, up to its 64 rows; beyond, while what
+// the blocks read of x is little beside the weights (rows of d 4096, F 8192: 16 in 27.6 us, the tiles 30.9; 32 in 37.4 and
+// 32.4; F 12288: 8 in 37.0 and 37.4, 16 in 39.4 and 37.6; d 3584, F 18944: 4 in 49.2 and 49.6, 16 in 57.1 and 50.0).  Past the
+// features that tiles of 96 take in one round the tiles read faster (d 8192, F 28672: 1 row in 157 us for 173).
+bool few_rows(int64_t T, int32_t F) {
+  return T <= 64 && (F <= 16 * kCus || (F <= 96 * kCus && T * F <= (int64_t)1 << 17));
 }
 
 template <int MODE>
@@ -831,7 +899,7 @@ int launch_gated_ffn_forward(const FfnForwardArgs& f, hipStream_t stream) {
     a.rows_q = f.T - t < kLaunchRows ? f.T - t : kLaunchRows;
     a.q = static_cast<const char*>(f.x) + t * a.ld_q;
     a.out0 = static_cast<char*>(f.out) + t * a.ld_out0;
-    const int rc = f.T > kFewRows ? launch_gated<kForward>(a, f.activation, stream)
+    const int rc = !few_rows(f.T, f.F) ? launch_gated<kForward>(a, f.activation, stream)
                    : f.activation == MOSAIC_SILU ? launch_few<MOSAIC_SILU>(a, stream) : launch_few<MOSAIC_GELU_TANH>(a, stream);
     if (rc != 0) return -1;
   }

@@ -129,6 +129,29 @@ def test_more_tiles_than_blocks(T, d, F):
     assert (out_full[:, F:] == 777.0).all() and (dx_full[:, d:] == 777.0).all() and (dw_full[:, d:] == 777.0).all()
 
 
+@pytest.mark.parametrize("T,d,F", [(40, 264, 18952), (64, 1032, 12296), (20, 136, 24584), (9, 520, 20008), (3, 200, 30008), (100, 72, 5000), (23, 2056, 5704)])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_few_rows_of_wide_blocks(T, d, F, act):
+    """Few rows of many features, K ragged: every way that takes them, forward and again in the backward pass."""
+    gen, x, wg, wu = inputs(T, d, F, T + 3 * d + 5 * F, 8, packed=T % 2 == 1)
+    dout, _ = matrix(T, F, gen, 8, 0.01)
+    out, out_full = matrix(T, F, gen, 8)
+    again, again_full = matrix(T, F, gen, 8)
+    dx, dw = torch.empty_like(x), torch.empty((2 * F, d), dtype=torch.bfloat16, device=DEV)
+    work = torch.empty(b.mosaic_gated_ffn_backward_workspace_bytes(T, d, F), dtype=torch.uint8, device=DEV)
+    b.mosaic_gated_ffn_forward(x, wg, wu, out, activation=ACT[act])
+    b.mosaic_gated_ffn_backward(dout, x, wg, wu, dx, dw[:F], dw[F:], work, activation=ACT[act], out=again)
+    exact, bound = ref.ffn_bound(x, wg, wu, act)
+    assert ((out.double() - exact).abs() <= bound).all() and ((again.double() - exact).abs() <= bound).all()
+    for got, w in zip((dx, dw[:F], dw[F:]), ref.ffn_gradients(dout, x, wg, wu, act)):
+        # a result's rounding, 2^-8 / sqrt 3, and its terms', as much again, where there are few of them not averaged
+        assert ref.relative(got, w) <= 2 * ref.U_BF16
+    assert (out_full[:, F:] == 777.0).all() and (again_full[:, F:] == 777.0).all()
+    first = out.clone()
+    b.mosaic_gated_ffn_forward(x, wg, wu, out, activation=ACT[act])
+    assert torch.equal(out, first)
+
+
 @pytest.mark.parametrize("T,d,F", [(1, 64, 64), (90, 136, 264), (700, 512, 384)])
 def test_weight_gradients_in_parts(T, d, F):
     """32-bit weight gradients, a batch taken in parts: the parts add up to what the whole gives."""
