@@ -156,7 +156,7 @@ struct Reader {
 
 // The four lanes that hold one Q row (16 apart) each have 4 consecutive P rows of every block; afterwards each has 4 NB
 // consecutive ones, NB = 2 or 4 blocks, in order: what is stored, or was loaded, is 16 bytes a lane.  `scatter` takes
-// gathered quads back.  Three blocks stay as they are, 8 bytes a lane: only tiles of few rows have them.
+// gathered quads back.  Three blocks stay as they are and are stored by 8 bytes a lane.
 typedef uint32_t Quad[2];   // four bf16
 __device__ __forceinline__ void swap32(Quad& a, Quad& b) {
 #pragma unroll
@@ -185,7 +185,6 @@ __device__ __forceinline__ void gather(Quad (&w)[NB]) {
 }
 template <int NB>
 __device__ __forceinline__ void scatter(Quad (&w)[NB]) {
-  if constexpr (NB == 3) return;
   swap16(w[0], w[1]);
   if constexpr (NB == 4) { swap16(w[2], w[3]); swap32(w[1], w[3]); swap32(w[0], w[2]); }
   else swap32(w[0], w[1]);
@@ -205,17 +204,8 @@ __device__ __forceinline__ void store_quads(char* row, int c, int end, const Qua
 }
 template <int NB>
 __device__ __forceinline__ void load_quads(const char* row, int c, int end, bool in, Quad (&w)[NB]) {
-  if constexpr (NB == 3) {
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      uint2 v = {0u, 0u};
-      if (in && c + 16 * i < end) v = *reinterpret_cast<const uint2*>(row + (int64_t)(c + 16 * i) * 2);
-      w[i][0] = v.x; w[i][1] = v.y;
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i + 1 < NB; i += 2) {
+  for (int i = 0; i < NB; i += 2) {
     u32x4_t v = {0u, 0u, 0u, 0u};
     if (in && c + 4 * i < end) v = *reinterpret_cast<const u32x4_t*>(row + (int64_t)(c + 4 * i) * 2);
     w[i][0] = v[0]; w[i][1] = v[1]; w[i + 1][0] = v[2]; w[i + 1][1] = v[3];
@@ -777,12 +767,14 @@ constexpr Tile kTiles[] = {
     {256, 64, 0.80, 0.80, 0.0, 1},  {192, 64, 0.70, 0.70, 0.0, 1},  {128, 64, 0.55, 0.55, 0.6, 1},  {128, 64, 0.84, 0.57, 0.0, 2},
 };
 struct Choice { int tile; double us; };
-Choice choose_tile(int64_t rows_p, int64_t rows_q, bool gated, int64_t steps, int64_t splits) {
+Choice choose_tile(int mode, int64_t rows_p, int64_t rows_q, int64_t steps, int64_t splits) {
   Choice best = {0, 0.0};
   for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
     const Tile& t = kTiles[i];
-    if (t.p == 192 && !gated) continue;   // (its rows across K would not be a power of two)
-    const int64_t n = tiles(rows_p, gated ? t.p / 2 : t.p) * tiles(rows_q, t.q) * splits;
+    // Of 96 features, forward alone: across K its rows would not be a power of two, and with the gradients' epilogue it was slower
+    // than 128 features (24 rows of d 3584, F 18944: 71 us for 57).
+    if (t.p == 192 && mode != kForward) continue;
+    const int64_t n = tiles(rows_p, mode == kForward || mode == kRecompute ? t.p / 2 : t.p) * tiles(rows_q, t.q) * splits;
     const double us = (double)tiles(n, kCus * t.per_cu) * (double)tiles(steps, splits) * (n <= kCus ? t.step_alone : t.step) + t.fill;
     if (i == 0 || us < best.us) best = {i, us};
   }
@@ -799,11 +791,11 @@ GradientPlan plan_gradients(int64_t T, int32_t d, int32_t F) {
   GradientPlan plan = {1, -1};
   if (T == 0 || T > kLaunchRows) return plan;
   const int64_t steps_x = 2 * tiles(F, kStepK), steps_w = tiles(T, kStepK);
-  const double dw = choose_tile(d, 2 * (int64_t)F, false, steps_w, 1).us;
+  const double dw = choose_tile(kDw, d, 2 * (int64_t)F, steps_w, 1).us;
   double least = 0.0;
   for (int32_t s = 1; s == 1 || (s <= kMostParts && s * T <= kPartRows && s * 4 <= steps_x); ++s) {
     const double join = s == 1 ? 0.0 : kLaunchUs + (double)(T * d) * 8.0 * s / kJoinBytesPerUs;
-    const double apart = choose_tile(d, T, false, steps_x, s).us + dw + kLaunchUs + join;
+    const double apart = choose_tile(kDx, d, T, steps_x, s).us + dw + kLaunchUs + join;
     if (s == 1 || apart < least) {
       least = apart;
       plan = {s, -1};
@@ -839,14 +831,13 @@ int launch_together(GemmArgs x, GemmArgs w, hipStream_t stream) {
 
 template <int MODE, int ACT>
 int launch_gemm(const GemmArgs& a, hipStream_t stream) {
-  constexpr bool kGated = MODE == kForward || MODE == kRecompute;
-  switch (choose_tile(a.rows_p, a.rows_q, kGated, (MODE == kDx ? 2 : 1) * tiles(a.depth, kStepK), a.splits).tile) {
+  switch (choose_tile(MODE, a.rows_p, a.rows_q, (MODE == kDx ? 2 : 1) * tiles(a.depth, kStepK), a.splits).tile) {
     case 0: return launch_tiles<MODE, 256, 256, 3, 2, ACT>(a, 1, stream);
     case 1: return launch_tiles<MODE, 128, 256, 3, 3, ACT>(a, 1, stream);
     case 2: return launch_tiles<MODE, 256, 128, 3, 3, ACT>(a, 1, stream);
     case 3: return launch_tiles<MODE, 128, 128, 4, 4, ACT>(a, 1, stream);
     case 4: return launch_tiles<MODE, 256, 64, 4, 4, ACT>(a, 1, stream);
-    case 5: if constexpr (kGated) return launch_tiles<MODE, 192, 64, 5, 5, ACT>(a, 1, stream);
+    case 5: if constexpr (MODE == kForward) return launch_tiles<MODE, 192, 64, 5, 5, ACT>(a, 1, stream);
     case 6: return launch_tiles<MODE, 128, 64, 6, 6, ACT>(a, 1, stream);
     default: return launch_tiles<MODE, 128, 64, 3, 3, ACT>(a, 2, stream);
   }
