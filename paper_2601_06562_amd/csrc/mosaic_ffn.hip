@@ -156,7 +156,7 @@ struct Reader {
 
 // The four lanes that hold one Q row (16 apart) each have 4 consecutive P rows of every block; afterwards each has 4 NB
 // consecutive ones, NB = 2 or 4 blocks, in order: what is stored, or was loaded, is 16 bytes a lane.  `scatter` takes
-// gathered quads back.  Three blocks stay as they are and are stored by 8 bytes a lane.
+// gathered quads back.  Three blocks stay as they are, 8 bytes a lane.
 typedef uint32_t Quad[2];   // four bf16
 __device__ __forceinline__ void swap32(Quad& a, Quad& b) {
 #pragma unroll
@@ -185,6 +185,7 @@ __device__ __forceinline__ void gather(Quad (&w)[NB]) {
 }
 template <int NB>
 __device__ __forceinline__ void scatter(Quad (&w)[NB]) {
+  if constexpr (NB == 3) return;
   swap16(w[0], w[1]);
   if constexpr (NB == 4) { swap16(w[2], w[3]); swap32(w[1], w[3]); swap32(w[0], w[2]); }
   else swap32(w[0], w[1]);
@@ -204,8 +205,17 @@ __device__ __forceinline__ void store_quads(char* row, int c, int end, const Qua
 }
 template <int NB>
 __device__ __forceinline__ void load_quads(const char* row, int c, int end, bool in, Quad (&w)[NB]) {
+  if constexpr (NB == 3) {
 #pragma unroll
-  for (int i = 0; i < NB; i += 2) {
+    for (int i = 0; i < NB; ++i) {
+      uint2 v = {0u, 0u};
+      if (in && c + 16 * i < end) v = *reinterpret_cast<const uint2*>(row + (int64_t)(c + 16 * i) * 2);
+      w[i][0] = v.x; w[i][1] = v.y;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i + 1 < NB; i += 2) {
     u32x4_t v = {0u, 0u, 0u, 0u};
     if (in && c + 4 * i < end) v = *reinterpret_cast<const u32x4_t*>(row + (int64_t)(c + 4 * i) * 2);
     w[i][0] = v[0]; w[i][1] = v[1]; w[i + 1][0] = v[2]; w[i + 1][1] = v[3];
@@ -534,6 +544,8 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
           }
         }
       }
+      // Told by the builtin, the compiler knows that dout has arrived.  Where it did not, it waited for all copies in every step.
+      if constexpr (MODE == kRecompute) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
     }
     if (!more) break;
     // The first slots; with the last tile's stores behind them no count tells them from the others.
@@ -755,26 +767,27 @@ int launch_tiles(GemmArgs a, int per_cu, hipStream_t stream) {
 
 // The tiles there are, what one step of 64 k takes all CUs at work, in us, and what filling a long ring adds.  A block's step is
 // bound by the latency of its copies or by the matrix cores, so a tile takes the same where it is alone and a launch takes
-// whole rounds of tiles.  Few rows of Q are bound by how many bytes are under way: there the rings take all LDS, and 96
-// features serve where 64 are more tiles than CUs (37 rows of d 3584, F 18944 in 50.8 us, of 128 features 56.4; 32 rows
-// of d 4096, F 12288 in 37.9 with six slots, 41.2 with three in two blocks a CU).
-// Times from 16 to 8192 rows of 12288 x 4096, 18944 x 3584, 5632 x 2048, 4096 x 1024 and 2048 x 512, forward and dw: in 130
-// sizes the choice of those without long rings is the fastest, or within 2% of it, but for two (5 and 6%); the others take up to
+// whole rounds of tiles.  Tiles of 96 features for the rounds that those of 64 or 128 would leave part empty (d 4096, F 12288:
+// 300 rows in 77 us for 87, 1000 in 160 for 183; d 3584, F 18944: 500 in 131 for 155).  Few rows are bound by how many
+// bytes are under way: there the rings take all LDS (37 rows of d 3584, F 18944 in 50.8 us by 96 features and five slots, of
+// 128 features 56.4; 32 rows of d 4096, F 12288 in 37.9 with six slots, 41.2 with three in two blocks a CU).
+// Times from 16 to 8192 rows of 12288 x 4096, 18944 x 3584, 5632 x 2048, 4096 x 1024 and 2048 x 512, forward and dw: of the
+// first six tiles the choice is the fastest or within 2% of it in 128 of 130 sizes (6% in the worst), and the others take up to
 // 2.7 times as long.
 struct Tile { int p, q; double step, step_alone, fill; int per_cu; };
 constexpr Tile kTiles[] = {
     {256, 256, 1.50, 1.50, 0.0, 1}, {128, 256, 0.91, 0.91, 0.0, 1}, {256, 128, 0.92, 0.92, 0.0, 1}, {128, 128, 0.60, 0.60, 0.0, 1},
-    {256, 64, 0.80, 0.80, 0.0, 1},  {192, 64, 0.70, 0.70, 0.0, 1},  {128, 64, 0.55, 0.55, 0.6, 1},  {128, 64, 0.84, 0.57, 0.0, 2},
+    {256, 64, 0.80, 0.80, 0.0, 1},  {128, 64, 0.84, 0.57, 0.0, 2},  {128, 64, 0.55, 0.55, 0.6, 1},  {192, 64, 0.70, 0.70, 0.0, 1},
+    {192, 128, 0.77, 0.85, 0.0, 1}, {192, 256, 1.26, 1.26, 0.0, 1},
 };
 struct Choice { int tile; double us; };
 Choice choose_tile(int mode, int64_t rows_p, int64_t rows_q, int64_t steps, int64_t splits) {
   Choice best = {0, 0.0};
   for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
     const Tile& t = kTiles[i];
-    // Of 96 features, forward alone: across K its rows would not be a power of two, and with the gradients' epilogue it was slower
-    // than 128 features (24 rows of d 3584, F 18944: 71 us for 57).
-    if (t.p == 192 && mode != kForward) continue;
-    const int64_t n = tiles(rows_p, mode == kForward || mode == kRecompute ? t.p / 2 : t.p) * tiles(rows_q, t.q) * splits;
+    const bool gated = mode == kForward || mode == kRecompute;
+    if (t.p == 192 && !gated) continue;   // across K its rows would not be a power of two
+    const int64_t n = tiles(rows_p, gated ? t.p / 2 : t.p) * tiles(rows_q, t.q) * splits;
     const double us = (double)tiles(n, kCus * t.per_cu) * (double)tiles(steps, splits) * (n <= kCus ? t.step_alone : t.step) + t.fill;
     if (i == 0 || us < best.us) best = {i, us};
   }
@@ -831,16 +844,24 @@ int launch_together(GemmArgs x, GemmArgs w, hipStream_t stream) {
 
 template <int MODE, int ACT>
 int launch_gemm(const GemmArgs& a, hipStream_t stream) {
-  switch (choose_tile(MODE, a.rows_p, a.rows_q, (MODE == kDx ? 2 : 1) * tiles(a.depth, kStepK), a.splits).tile) {
+  const int tile = choose_tile(MODE, a.rows_p, a.rows_q, (MODE == kDx ? 2 : 1) * tiles(a.depth, kStepK), a.splits).tile;
+  switch (tile) {
     case 0: return launch_tiles<MODE, 256, 256, 3, 2, ACT>(a, 1, stream);
     case 1: return launch_tiles<MODE, 128, 256, 3, 3, ACT>(a, 1, stream);
     case 2: return launch_tiles<MODE, 256, 128, 3, 3, ACT>(a, 1, stream);
     case 3: return launch_tiles<MODE, 128, 128, 4, 4, ACT>(a, 1, stream);
     case 4: return launch_tiles<MODE, 256, 64, 4, 4, ACT>(a, 1, stream);
-    case 5: if constexpr (MODE == kForward) return launch_tiles<MODE, 192, 64, 5, 5, ACT>(a, 1, stream);
+    case 5: return launch_tiles<MODE, 128, 64, 3, 3, ACT>(a, 2, stream);
     case 6: return launch_tiles<MODE, 128, 64, 6, 6, ACT>(a, 1, stream);
-    default: return launch_tiles<MODE, 128, 64, 3, 3, ACT>(a, 2, stream);
   }
+  if constexpr (MODE == kForward || MODE == kRecompute) {
+    switch (tile) {
+      case 7: return launch_tiles<MODE, 192, 64, 5, 5, ACT>(a, 1, stream);
+      case 8: return launch_tiles<MODE, 192, 128, 4, 4, ACT>(a, 1, stream);
+      case 9: return launch_tiles<MODE, 192, 256, 3, 2, ACT>(a, 1, stream);
+    }
+  }
+  return -1;
 }
 
 template <int ACT, int TB>

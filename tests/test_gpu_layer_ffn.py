@@ -152,6 +152,13 @@ def test_few_rows_of_wide_blocks(T, d, F, act):
     assert torch.equal(out, first)
 
 
+@pytest.mark.parametrize("T,d,F,act", [(290, 200, 12200, "silu"), (300, 1032, 12280, "gelu"), (1000, 72, 12280, "silu"),
+                                       (120, 328, 18952, "gelu"), (200, 136, 18936, "silu"), (2040, 520, 5632, "gelu")])
+def test_rows_by_features_between_the_tiles(T, d, F, act):
+    """Numbers of features that neither 64 nor 128 a tile divide well among the compute units; see test_few_rows_of_wide_blocks."""
+    test_few_rows_of_wide_blocks(T, d, F, act)
+
+
 @pytest.mark.parametrize("T,d,F", [(1, 64, 64), (90, 136, 264), (700, 512, 384)])
 def test_weight_gradients_in_parts(T, d, F):
     """32-bit weight gradients, a batch taken in parts: the parts add up to what the whole gives."""
