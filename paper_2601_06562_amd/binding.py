@@ -198,9 +198,13 @@ def _stream_ptr(stream):
     return stream.cuda_stream
 
 
-def _dev_ptr(t, name, dtype=None):
+def _dev_ptr(t, name, dtype=None, dense=True):
+    """The address of a device tensor, 0 for None.  `dense`: the library walks its elements side by side, so a strided or
+    expanded one would be read, or written, in other places than its own."""
     if t is None:
         return 0
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
     if not t.is_cuda:
         raise ValueError(f"{name} must live in device memory")
     if dtype is not None and t.dtype != dtype:
@@ -251,7 +255,7 @@ def mosaic_masked_logits_reduce(hidden, w, idx, count, max_rows, out_token, out_
         raise ValueError("hidden rows and w must be dense along d")
     ld_h = hidden.stride(0) if T > 1 else d
     _check(lib().mosaic_masked_logits_reduce(
-        _dev_ptr(hidden, "hidden", torch.bfloat16), T, d, ld_h, _dev_ptr(w, "w", torch.bfloat16), V,
+        _dev_ptr(hidden, "hidden", torch.bfloat16, dense=False), T, d, ld_h, _dev_ptr(w, "w", torch.bfloat16), V,
         _dev_ptr(idx, "idx", torch.int32), _dev_ptr(count, "count", torch.int32), max_rows,
         _dev_ptr(out_token, "out_token", torch.int32), _dev_ptr(out_conf, "out_conf", torch.float32),
         _dev_ptr(out_lse, "out_lse", torch.float32), ctypes.byref(plan), *_workspace_args(workspace),
@@ -269,7 +273,7 @@ def mosaic_masked_logits_reduce_static(hidden, w, idx, count, max_rows, out_toke
         raise ValueError("hidden rows and w must be dense along d")
     ld_h = hidden.stride(0) if T > 1 else d
     _check(lib().mosaic_masked_logits_reduce_static(
-        _dev_ptr(hidden, "hidden", torch.bfloat16), T, d, ld_h, _dev_ptr(w, "w", torch.bfloat16), V,
+        _dev_ptr(hidden, "hidden", torch.bfloat16, dense=False), T, d, ld_h, _dev_ptr(w, "w", torch.bfloat16), V,
         _dev_ptr(idx, "idx", torch.int32), _dev_ptr(count, "count", torch.int32), max_rows,
         _dev_ptr(out_token, "out_token", torch.int32), _dev_ptr(out_conf, "out_conf", torch.float32),
         _dev_ptr(out_lse, "out_lse", torch.float32), ctypes.byref(plan), _stream_ptr(stream)),
@@ -299,7 +303,7 @@ def mosaic_masked_logits_sample(hidden, w, idx, count, max_rows, temperature, se
         raise ValueError("hidden rows and w must be dense along d")
     ld_h = hidden.stride(0) if T > 1 else d
     _check(lib().mosaic_masked_logits_sample(
-        _dev_ptr(hidden, "hidden", torch.bfloat16), T, d, ld_h, _dev_ptr(w, "w", torch.bfloat16), V,
+        _dev_ptr(hidden, "hidden", torch.bfloat16, dense=False), T, d, ld_h, _dev_ptr(w, "w", torch.bfloat16), V,
         _dev_ptr(idx, "idx", torch.int32), _dev_ptr(noise_idx, "noise_idx", torch.int32),
         _dev_ptr(count, "count", torch.int32), max_rows, float(temperature), int(seed) & 0xFFFFFFFFFFFFFFFF,
         _dev_ptr(out_token, "out_token", torch.int32), _dev_ptr(out_conf, "out_conf", torch.float32),
@@ -451,6 +455,7 @@ def mosaic_rmsnorm_forward(x, residual, gamma, eps, y, sum=None, q8=None, idx=No
         raise TypeError("sum must have the residual's type")
     if q8 is not None and q8.shape != (T, d):
         raise ValueError("q8 must have the shape of the rows")
+    p_idx, p_count = _dev_ptr(idx, "idx", torch.int32), _dev_ptr(count, "count", torch.int32)
     p_x, ld_x = _rows(x, "x", T, d, torch.bfloat16)
     p_r, ld_r = _rows(residual, "residual", T, d)
     p_s, ld_s = _rows(sum, "sum", T, d)
@@ -461,8 +466,8 @@ def mosaic_rmsnorm_forward(x, residual, gamma, eps, y, sum=None, q8=None, idx=No
         raise ValueError("idx holds fewer than max_rows entries")
     _check(_layer().mosaic_rmsnorm_forward(
         p_x, ld_x, p_r, stream_type, ld_r, _vector(gamma, "gamma", d), _type_of(gamma, "gamma"), float(eps), T, d,
-        _dev_ptr(idx, "idx", torch.int32), _dev_ptr(count, "count", torch.int32), max_rows, p_s, ld_s, p_y, ld_y,
-        q8._ref if q8 is not None else None, _stream_ptr(stream)), "mosaic_rmsnorm_forward")
+        p_idx, p_count, max_rows, p_s, ld_s, p_y, ld_y, q8._ref if q8 is not None else None,
+        _stream_ptr(stream)), "mosaic_rmsnorm_forward")
 
 
 def mosaic_rmsnorm_backward_workspace_bytes(T, d) -> int:
