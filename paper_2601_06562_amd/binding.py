@@ -455,7 +455,13 @@ def mosaic_rmsnorm_forward(x, residual, gamma, eps, y, sum=None, q8=None, idx=No
         raise TypeError("sum must have the residual's type")
     if q8 is not None and q8.shape != (T, d):
         raise ValueError("q8 must have the shape of the rows")
+    if (idx is None) != (count is None):
+        raise ValueError("idx and count go together")
+    if count is not None and count.numel() == 0:
+        raise ValueError("count must hold an element")
     p_idx, p_count = _dev_ptr(idx, "idx", torch.int32), _dev_ptr(count, "count", torch.int32)
+    if idx is not None and idx.numel() == 0:
+        p_idx = p_count   # an empty tensor has no address, which would stand for all rows; max_rows is 0 and nobody reads it
     p_x, ld_x = _rows(x, "x", T, d, torch.bfloat16)
     p_r, ld_r = _rows(residual, "residual", T, d)
     p_s, ld_s = _rows(sum, "sum", T, d)
