@@ -13,7 +13,8 @@
  *   every sum over a row, a column or a product is held in 32 bits; a result is rounded to its type once.  The exception is
  *   said at mosaic_gated_ffn_backward
  * T = rows (positions; 0 <= T < 2^31; T == 0 enqueues nothing but the clearing of sums over rows), d = hidden size,
- * F = feed-forward size; d and F are multiples of 8, at most MOSAIC_MAX_ROW (the norms and checkpoints: MOSAIC_MAX_NORM_ROW).
+ * F = feed-forward size; d and F are multiples of 8, at most MOSAIC_MAX_ROW (the norms, the checkpoints and what works from
+ * 8-bit rows: d at most MOSAIC_MAX_NORM_ROW).  A workspace query gives 0 for sizes that its call refuses.
  * Results do not depend on anything but the arguments: no atomics, the same bits on every call.
  */
 #ifndef MOSAIC_LAYER_H_

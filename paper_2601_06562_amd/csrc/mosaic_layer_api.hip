@@ -198,7 +198,9 @@ int mosaic_gated_ffn_forward(const void* x, int64_t ld_x, const void* w_gate, co
 }
 
 int64_t mosaic_gated_ffn_backward_workspace_bytes(int64_t T, int32_t d, int32_t F, int32_t q8_input) {
-  if (check_sizes(T, d, MOSAIC_MAX_ROW) != MOSAIC_OK || check_sizes(T, F, MOSAIC_MAX_ROW) != MOSAIC_OK) return 0;
+  if (check_sizes(T, d, q8_input != 0 ? MOSAIC_MAX_NORM_ROW : MOSAIC_MAX_ROW) != MOSAIC_OK ||
+      check_sizes(T, F, MOSAIC_MAX_ROW) != MOSAIC_OK)
+    return 0;
   return ffn_space(T, d, F, q8_input != 0).total;
 }
 
