@@ -210,7 +210,7 @@ int mosaic_gated_ffn_backward(const void* dout, int64_t ld_dout, const void* x, 
                               void* dw_up, int32_t dw_type, int64_t ld_dw, int32_t accumulate, void* workspace,
                               int64_t workspace_bytes, void* stream) {
   if ((activation != MOSAIC_SILU && activation != MOSAIC_GELU_TANH) || !known_type(dw_type) ||
-      (dw_gate == nullptr) != (dw_up == nullptr) || (accumulate != 0 && dw_type != MOSAIC_F32) ||
+      (dw_gate == nullptr) != (dw_up == nullptr) || (accumulate != 0 && dw_gate != nullptr && dw_type != MOSAIC_F32) ||
       (dx == nullptr && dw_gate == nullptr && out == nullptr))
     return MOSAIC_ERR_INVALID_ARG;
   MOSAIC_RETURN_IF(check_sizes(T, d, q8 != nullptr ? MOSAIC_MAX_NORM_ROW : MOSAIC_MAX_ROW));
