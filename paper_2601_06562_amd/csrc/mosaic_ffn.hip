@@ -16,10 +16,13 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "mosaic_ffn_choice.h"
 #include "mosaic_layer_internal.h"
 
 namespace mosaic {
 namespace {
+
+using namespace ffn;
 
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 typedef __attribute__((address_space(3))) bf16x4_t* lds_bf16x4_ptr_t;
@@ -27,11 +30,8 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 typedef const __attribute__((address_space(3))) bf16x8_t* lds_bf16x8_ptr_t;
 
 constexpr int kThreads = 512;   // 8 waves: 2 along P, 4 along Q
-constexpr int kStepK = 64;
 constexpr uint32_t kOutside = 0x80000000u;   // a buffer offset past every range here: such a lane's copy brings zeros
-constexpr int kXcds = 8, kCus = 256;
-
-enum { kForward, kRecompute, kDx, kDw };
+constexpr int kXcds = 8;
 
 struct GemmArgs {
   const char* p0;      // P: weights (gate / its columns), or x
@@ -239,7 +239,7 @@ constexpr int ring_bytes(int TP, int TQ, int SP, int SQ) { return (SP * TP + SQ 
 // stored.
 template <int MODE, int TP, int TQ, int SP, int SQ, int ACT>
 __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int block, int blocks) {
-  constexpr bool kGated = MODE == kForward || MODE == kRecompute;
+  constexpr bool kGated = gated_mode(MODE);
   constexpr bool kRowP = !kGated, kRowQ = MODE == kDw;
   constexpr int kTileP = TP, kTileQ = TQ, kBlocksP = TP / 32, QB = TQ / 64;   // blocks of a wave
   constexpr int kBytesP = kTileP * kStepK * 2, kBytesQ = kTileQ * kStepK * 2;
@@ -749,116 +749,43 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(const float* __restrict__
   }
 }
 
-int64_t tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
-
-// Rows of one launch; rows past them go to further ones.
-constexpr int64_t kLaunchRows = (int64_t)1 << 17;
-static_assert(kLaunchRows <= MOSAIC_MAX_ROW && (int64_t)(MOSAIC_MAX_ROW / 64) * (MOSAIC_MAX_ROW / 64) * 512 < (int64_t)1 << 32,
-              "threads of a launch of the smallest tiles: 64 rows by 64 features, or of both weight gradients by 128 columns");
-
-template <int MODE, int TP, int TQ, int SP, int SQ, int ACT>
-int launch_tiles(GemmArgs a, int per_cu, hipStream_t stream) {
-  a.tiles_p = (int32_t)tiles(a.rows_p, MODE == kForward || MODE == kRecompute ? TP / 2 : TP);
-  a.tiles_q = (int32_t)tiles(a.rows_q, TQ);
-  const int64_t n = (int64_t)a.tiles_q * a.tiles_p * a.splits;
-  return launch_kernel(ffn_gemm_kernel<MODE, TP, TQ, SP, SQ, ACT>, dim3((unsigned)(n < kCus * per_cu ? n : kCus * per_cu)),
+template <int MODE, int TILE, int SP, int SQ, int ACT>
+int launch_tiles(GemmArgs a, hipStream_t stream) {
+  const TileGrid g = tile_grid(MODE, TILE, a.rows_p, a.rows_q, a.splits);
+  a.tiles_p = g.p;
+  a.tiles_q = g.q;
+  return launch_kernel(ffn_gemm_kernel<MODE, kTiles[TILE].p, kTiles[TILE].q, SP, SQ, ACT>, dim3((unsigned)g.blocks),
                        dim3(kThreads), stream, a);
 }
 
-// The tiles there are, what one step of 64 k takes all CUs at work, in us, and what filling a long ring adds.  A block's step is
-// bound by the latency of its copies or by the matrix cores, so a tile takes the same where it is alone and a launch takes
-// whole rounds of tiles.  Tiles of 96 features for the rounds that those of 64 or 128 would leave part empty (d 4096, F 12288:
-// 300 rows in 77 us for 87, 1000 in 160 for 183; d 3584, F 18944: 500 in 131 for 155).  Few rows are bound by how many
-// bytes are under way: there the rings take all LDS (37 rows of d 3584, F 18944 in 50.8 us by 96 features and five slots, of
-// 128 features 56.4; 32 rows of d 4096, F 12288 in 37.9 with six slots, 41.2 with three in two blocks a CU).
-// Times from 16 to 8192 rows of 12288 x 4096, 18944 x 3584, 5632 x 2048, 4096 x 1024 and 2048 x 512, forward and dw: of the
-// first six tiles the choice is the fastest or within 2% of it in 128 of 130 sizes (6% in the worst), and the others take up to
-// 2.7 times as long.
-struct Tile { int p, q; double step, step_alone, fill; int per_cu; };
-constexpr Tile kTiles[] = {
-    {256, 256, 1.50, 1.50, 0.0, 1}, {128, 256, 0.91, 0.91, 0.0, 1}, {256, 128, 0.92, 0.92, 0.0, 1}, {128, 128, 0.60, 0.60, 0.0, 1},
-    {256, 64, 0.80, 0.80, 0.0, 1},  {128, 64, 0.84, 0.57, 0.0, 2},  {128, 64, 0.55, 0.55, 0.6, 1},  {192, 64, 0.70, 0.70, 0.0, 1},
-    {192, 128, 0.77, 0.85, 0.0, 1}, {192, 256, 1.26, 1.26, 0.0, 1},
-};
-struct Choice { int tile; double us; };
-Choice choose_tile(int mode, int64_t rows_p, int64_t rows_q, int64_t steps, int64_t splits) {
-  Choice best = {0, 0.0};
-  for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
-    const Tile& t = kTiles[i];
-    const bool gated = mode == kForward || mode == kRecompute;
-    if (t.p == 192 && !gated) continue;   // across K its rows would not be a power of two
-    const int64_t n = tiles(rows_p, gated ? t.p / 2 : t.p) * tiles(rows_q, t.q) * splits;
-    const double us = (double)tiles(n, kCus * t.per_cu) * (double)tiles(steps, splits) * (n <= kCus ? t.step_alone : t.step) + t.fill;
-    if (i == 0 || us < best.us) best = {i, us};
-  }
-  return best;
-}
-
-// How the gradients of a backward pass are taken: in how many parts of K dx is summed, and in which tiles both products go
-// out together (-1: in launches of their own).  The parts follow from the sizes alone, whichever gradients a call wants: dx
-// has the same bits in every call.
-struct GradientPlan { int32_t splits, tile; };
-constexpr int64_t kMostParts = 16, kPartRows = 8192;   // parts, and parts times rows
-constexpr double kLaunchUs = 4.0, kJoinBytesPerUs = 4e6;   // joining parts: a launch, and 8 bytes an element and part
-GradientPlan plan_gradients(int64_t T, int32_t d, int32_t F) {
-  GradientPlan plan = {1, -1};
-  if (T == 0 || T > kLaunchRows) return plan;
-  const int64_t steps_x = 2 * tiles(F, kStepK), steps_w = tiles(T, kStepK);
-  const double dw = choose_tile(kDw, d, 2 * (int64_t)F, steps_w, 1).us;
-  double least = 0.0;
-  for (int32_t s = 1; s == 1 || (s <= kMostParts && s * T <= kPartRows && s * 4 <= steps_x); ++s) {
-    const double join = s == 1 ? 0.0 : kLaunchUs + (double)(T * d) * 8.0 * s / kJoinBytesPerUs;
-    const double apart = choose_tile(kDx, d, T, steps_x, s).us + dw + kLaunchUs + join;
-    if (s == 1 || apart < least) {
-      least = apart;
-      plan = {s, -1};
-    }
-    for (int i : {0, 1, 3}) {
-      const Tile& t = kTiles[i];
-      const int64_t each_x = tiles(steps_x, s), n_x = tiles(d, t.p) * tiles(T, t.q) * s;
-      const int64_t n_w = tiles(d, t.p) * tiles(2 * (int64_t)F, t.q);
-      if (n_x + n_w > 8 * kCus) continue;
-      const int64_t longest = each_x > steps_w ? each_x : steps_w;
-      double rounds = (double)(n_x * each_x + n_w * steps_w) / kCus;      // as even as the blocks allow
-      if (n_x + n_w > kCus) rounds += 0.5 * (double)steps_w;
-      if (rounds < (double)longest) rounds = (double)longest;
-      const double together = rounds * t.step + join;
-      if (together < least) {
-        least = together;
-        plan = {s, i};
-      }
-    }
-  }
-  return plan;
-}
-
-template <int TP, int TQ, int SP, int SQ>
+template <int TILE, int SP, int SQ>
 int launch_together(GemmArgs x, GemmArgs w, hipStream_t stream) {
-  x.tiles_p = w.tiles_p = (int32_t)tiles(x.rows_p, TP);
-  x.tiles_q = (int32_t)tiles(x.rows_q, TQ);
-  w.tiles_q = (int32_t)tiles(w.rows_q, TQ);
-  const int blocks_x = (int)tiles((int64_t)x.tiles_p * x.tiles_q * x.splits, kXcds) * kXcds;
-  return launch_kernel(ffn_gradients_kernel<TP, TQ, SP, SQ>, dim3((unsigned)(blocks_x + w.tiles_p * w.tiles_q)), dim3(kThreads),
-                       stream, x, w, blocks_x);
+  const TileGrid gx = tile_grid(kDx, TILE, x.rows_p, x.rows_q, x.splits), gw = tile_grid(kDw, TILE, w.rows_p, w.rows_q, 1);
+  x.tiles_p = w.tiles_p = gx.p;
+  x.tiles_q = gx.q;
+  w.tiles_q = gw.q;
+  const int blocks_x = (int)tiles(gx.n, kXcds) * kXcds;
+  return launch_kernel(ffn_gradients_kernel<kTiles[TILE].p, kTiles[TILE].q, SP, SQ>, dim3((unsigned)(blocks_x + gw.n)),
+                       dim3(kThreads), stream, x, w, blocks_x);
 }
 
 template <int MODE, int ACT>
 int launch_gemm(const GemmArgs& a, hipStream_t stream) {
   const int tile = choose_tile(MODE, a.rows_p, a.rows_q, (MODE == kDx ? 2 : 1) * tiles(a.depth, kStepK), a.splits).tile;
   switch (tile) {
-    case 0: return launch_tiles<MODE, 256, 256, 3, 2, ACT>(a, 1, stream);
-    case 1: return launch_tiles<MODE, 128, 256, 3, 3, ACT>(a, 1, stream);
-    case 2: return launch_tiles<MODE, 256, 128, 3, 3, ACT>(a, 1, stream);
-    case 3: return launch_tiles<MODE, 128, 128, 4, 4, ACT>(a, 1, stream);
-    case 4: return launch_tiles<MODE, 256, 64, 4, 4, ACT>(a, 1, stream);
-    case 5: return launch_tiles<MODE, 128, 64, 3, 3, ACT>(a, 2, stream);
-    case 6: return launch_tiles<MODE, 128, 64, 6, 6, ACT>(a, 1, stream);
+    case 0: return launch_tiles<MODE, 0, 3, 2, ACT>(a, stream);
+    case 1: return launch_tiles<MODE, 1, 3, 3, ACT>(a, stream);
+    case 2: return launch_tiles<MODE, 2, 3, 3, ACT>(a, stream);
+    case 3: return launch_tiles<MODE, 3, 4, 4, ACT>(a, stream);
+    case 4: return launch_tiles<MODE, 4, 4, 4, ACT>(a, stream);
+    case 5: return launch_tiles<MODE, 5, 3, 3, ACT>(a, stream);
+    case 6: return launch_tiles<MODE, 6, 6, 6, ACT>(a, stream);
   }
-  if constexpr (MODE == kForward || MODE == kRecompute) {
+  if constexpr (gated_mode(MODE)) {
     switch (tile) {
-      case 7: return launch_tiles<MODE, 192, 64, 5, 5, ACT>(a, 1, stream);
-      case 8: return launch_tiles<MODE, 192, 128, 4, 4, ACT>(a, 1, stream);
-      case 9: return launch_tiles<MODE, 192, 256, 3, 2, ACT>(a, 1, stream);
+      case 7: return launch_tiles<MODE, 7, 5, 5, ACT>(a, stream);
+      case 8: return launch_tiles<MODE, 8, 4, 4, ACT>(a, stream);
+      case 9: return launch_tiles<MODE, 9, 3, 2, ACT>(a, stream);
     }
   }
   return -1;
@@ -877,14 +804,6 @@ int launch_few(const GemmArgs& a, hipStream_t stream) {
     default: return launch_few_as<ACT, 4>(a, stream);
   }
 }
-// Whether these rows go to the kernel for few: where its blocks are no more than the CUs, up to its 64 rows; beyond, while what
-// the blocks read of x is little beside the weights (rows of d 4096, F 8192: 16 in 27.6 us, the tiles 30.9; 32 in 37.4 and
-// 32.4; F 12288: 8 in 37.0 and 37.4, 16 in 39.4 and 37.6; d 3584, F 18944: 4 in 49.2 and 49.6, 16 in 57.1 and 50.0).  Past the
-// features that tiles of 96 take in one round the tiles read faster (d 8192, F 28672: 1 row in 157 us for 173).
-bool few_rows(int64_t T, int32_t F) {
-  return T <= 64 && (F <= 16 * kCus || (F <= 96 * kCus && T * F <= (int64_t)1 << 17));
-}
-
 template <int MODE>
 int launch_gated(const GemmArgs& a, int activation, hipStream_t stream) {
   return activation == MOSAIC_SILU ? launch_gemm<MODE, MOSAIC_SILU>(a, stream)
@@ -972,9 +891,9 @@ int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
     x.q = static_cast<const char*>(f.grads) + t * ld_grads;
     x.out0 = x.f32 ? reinterpret_cast<char*>(f.partials) : static_cast<char*>(f.dx) + t * x.ld_out0;
     const int rc = !together ? launch_gemm<kDx, 0>(x, stream)
-                   : plan.tile == 0 ? launch_together<256, 256, 3, 2>(x, w, stream)
-                   : plan.tile == 1 ? launch_together<128, 256, 3, 3>(x, w, stream)
-                                    : launch_together<128, 128, 4, 4>(x, w, stream);
+                   : plan.tile == 0 ? launch_together<0, 3, 2>(x, w, stream)
+                   : plan.tile == 1 ? launch_together<1, 3, 3>(x, w, stream)
+                                    : launch_together<3, 4, 4>(x, w, stream);
     if (rc != 0) return -1;
   }
   if (f.dx != nullptr && plan.splits > 1) {

@@ -1,0 +1,115 @@
+// Which kernel and tiles a product of the feed-forward block takes (mosaic_ffn.hip), from its sizes alone: host code without
+// a GPU's headers, so that the choice for any size can be asked for where there is none.
+#ifndef MOSAIC_FFN_CHOICE_H_
+#define MOSAIC_FFN_CHOICE_H_
+
+#include <stdint.h>
+
+#include <initializer_list>
+
+#include "mosaic_layer.h"
+
+namespace mosaic {
+namespace ffn {
+
+constexpr int kStepK = 64;
+constexpr int kCus = 256;
+
+enum { kForward, kRecompute, kDx, kDw };
+constexpr bool gated_mode(int mode) { return mode == kForward || mode == kRecompute; }
+
+inline int64_t tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
+
+// Rows of one launch; rows past them go to further ones.
+constexpr int64_t kLaunchRows = (int64_t)1 << 17;
+static_assert(kLaunchRows <= MOSAIC_MAX_ROW && (int64_t)(MOSAIC_MAX_ROW / 64) * (MOSAIC_MAX_ROW / 64) * 512 < (int64_t)1 << 32,
+              "threads of a launch of the smallest tiles: 64 rows by 64 features, or of both weight gradients by 128 columns");
+
+// The tiles there are, what one step of 64 k takes all CUs at work, in us, and what filling a long ring adds.  A block's step is
+// bound by the latency of its copies or by the matrix cores, so a tile takes the same where it is alone and a launch takes
+// whole rounds of tiles.  Tiles of 96 features for the rounds that those of 64 or 128 would leave part empty (d 4096, F 12288:
+// 300 rows in 77 us for 87, 1000 in 160 for 183; d 3584, F 18944: 500 in 131 for 155).  Few rows are bound by how many
+// bytes are under way: there the rings take all LDS (37 rows of d 3584, F 18944 in 50.8 us by 96 features and five slots, of
+// 128 features 56.4; 32 rows of d 4096, F 12288 in 37.9 with six slots, 41.2 with three in two blocks a CU).
+// Times from 16 to 8192 rows of 12288 x 4096, 18944 x 3584, 5632 x 2048, 4096 x 1024 and 2048 x 512, forward and dw: of the
+// first six tiles the choice is the fastest or within 2% of it in 128 of 130 sizes (6% in the worst), and the others take up to
+// 2.7 times as long.
+struct Tile { int p, q; double step, step_alone, fill; int per_cu; };
+constexpr Tile kTiles[] = {
+    {256, 256, 1.50, 1.50, 0.0, 1}, {128, 256, 0.91, 0.91, 0.0, 1}, {256, 128, 0.92, 0.92, 0.0, 1}, {128, 128, 0.60, 0.60, 0.0, 1},
+    {256, 64, 0.80, 0.80, 0.0, 1},  {128, 64, 0.84, 0.57, 0.0, 2},  {128, 64, 0.55, 0.55, 0.6, 1},  {192, 64, 0.70, 0.70, 0.0, 1},
+    {192, 128, 0.77, 0.85, 0.0, 1}, {192, 256, 1.26, 1.26, 0.0, 1},
+};
+
+// The launch of a product in tile `i`: its tiles, dealt to `blocks` blocks in turn.
+struct TileGrid { int32_t p, q; int64_t n; int32_t blocks; };
+inline TileGrid tile_grid(int mode, int i, int64_t rows_p, int64_t rows_q, int64_t splits) {
+  const Tile& t = kTiles[i];
+  TileGrid g = {(int32_t)tiles(rows_p, gated_mode(mode) ? t.p / 2 : t.p), (int32_t)tiles(rows_q, t.q), 0, 0};
+  g.n = (int64_t)g.p * g.q * splits;
+  g.blocks = (int32_t)(g.n < kCus * t.per_cu ? g.n : kCus * t.per_cu);
+  return g;
+}
+
+struct Choice { int tile; double us; };
+inline Choice choose_tile(int mode, int64_t rows_p, int64_t rows_q, int64_t steps, int64_t splits) {
+  Choice best = {0, 0.0};
+  for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
+    const Tile& t = kTiles[i];
+    if (t.p == 192 && !gated_mode(mode)) continue;   // across K its rows would not be a power of two
+    const int64_t n = tile_grid(mode, i, rows_p, rows_q, splits).n;
+    const double us = (double)tiles(n, kCus * t.per_cu) * (double)tiles(steps, splits) * (n <= kCus ? t.step_alone : t.step) + t.fill;
+    if (i == 0 || us < best.us) best = {i, us};
+  }
+  return best;
+}
+
+// How the gradients of a backward pass are taken: in how many parts of K dx is summed, and in which tiles both products go
+// out together (-1: in launches of their own).  The parts follow from the sizes alone, whichever gradients a call wants: dx
+// has the same bits in every call.
+struct GradientPlan { int32_t splits, tile; };
+constexpr int64_t kMostParts = 16, kPartRows = 8192;   // parts, and parts times rows
+constexpr double kLaunchUs = 4.0, kJoinBytesPerUs = 4e6;   // joining parts: a launch, and 8 bytes an element and part
+inline GradientPlan plan_gradients(int64_t T, int32_t d, int32_t F) {
+  GradientPlan plan = {1, -1};
+  if (T == 0 || T > kLaunchRows) return plan;
+  const int64_t steps_x = 2 * tiles(F, kStepK), steps_w = tiles(T, kStepK);
+  const double dw = choose_tile(kDw, d, 2 * (int64_t)F, steps_w, 1).us;
+  double least = 0.0;
+  for (int32_t s = 1; s == 1 || (s <= kMostParts && s * T <= kPartRows && s * 4 <= steps_x); ++s) {
+    const double join = s == 1 ? 0.0 : kLaunchUs + (double)(T * d) * 8.0 * s / kJoinBytesPerUs;
+    const double apart = choose_tile(kDx, d, T, steps_x, s).us + dw + kLaunchUs + join;
+    if (s == 1 || apart < least) {
+      least = apart;
+      plan = {s, -1};
+    }
+    for (int i : {0, 1, 3}) {
+      const Tile& t = kTiles[i];
+      const int64_t each_x = tiles(steps_x, s), n_x = tiles(d, t.p) * tiles(T, t.q) * s;
+      const int64_t n_w = tiles(d, t.p) * tiles(2 * (int64_t)F, t.q);
+      if (n_x + n_w > 8 * kCus) continue;
+      const int64_t longest = each_x > steps_w ? each_x : steps_w;
+      double rounds = (double)(n_x * each_x + n_w * steps_w) / kCus;      // as even as the blocks allow
+      if (n_x + n_w > kCus) rounds += 0.5 * (double)steps_w;
+      if (rounds < (double)longest) rounds = (double)longest;
+      const double together = rounds * t.step + join;
+      if (together < least) {
+        least = together;
+        plan = {s, i};
+      }
+    }
+  }
+  return plan;
+}
+
+// Whether these rows go to the kernel for few: where its blocks are no more than the CUs, up to its 64 rows; beyond, while what
+// the blocks read of x is little beside the weights (rows of d 4096, F 8192: 16 in 27.6 us, the tiles 30.9; 32 in 37.4 and
+// 32.4; F 12288: 8 in 37.0 and 37.4, 16 in 39.4 and 37.6; d 3584, F 18944: 4 in 49.2 and 49.6, 16 in 57.1 and 50.0).  Past the
+// features that tiles of 96 take in one round the tiles read faster (d 8192, F 28672: 1 row in 157 us for 173).
+inline bool few_rows(int64_t T, int32_t F) {
+  return T <= 64 && (F <= 16 * kCus || (F <= 96 * kCus && T * F <= (int64_t)1 << 17));
+}
+
+}  // namespace ffn
+}  // namespace mosaic
+#endif
