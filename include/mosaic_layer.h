@@ -15,7 +15,9 @@
  * T = rows (positions; 0 <= T < 2^31; T == 0 enqueues nothing but the clearing of sums over rows), d = hidden size,
  * F = feed-forward size; d and F are multiples of 8, at most MOSAIC_MAX_ROW (the norms, the checkpoints and what works from
  * 8-bit rows: d at most MOSAIC_MAX_NORM_ROW).  A workspace query gives 0 for sizes that its call refuses.
- * Results do not depend on anything but the arguments: no atomics, the same bits on every call.
+ * Results do not depend on anything but the arguments: no atomics, the same bits on every call.  A row's norm, its gradient and its
+ * 8 bits are the same whatever other rows the call has.  The feed-forward block sums a product's K in an order that follows
+ * from the sizes, T among them: the same rows in calls of another number of rows may differ in their last bits.
  */
 #ifndef MOSAIC_LAYER_H_
 #define MOSAIC_LAYER_H_
