@@ -20,10 +20,13 @@ constexpr bool gated_mode(int mode) { return mode == kForward || mode == kRecomp
 
 inline int64_t tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
-// Rows of one launch; rows past them go to further ones.
+// Rows of one launch; rows past them go to further ones.  It bounds the tiles of a launch, which the kernels number in 32 bits:
+// the smallest are of 64 rows by 64 features (a weight gradient's by 128 columns, of both at once), and dx has parts of K only
+// where parts times rows stay within kPartRows.
 constexpr int64_t kLaunchRows = (int64_t)1 << 17;
-static_assert(kLaunchRows <= MOSAIC_MAX_ROW && (int64_t)(MOSAIC_MAX_ROW / 64) * (MOSAIC_MAX_ROW / 64) * 512 < (int64_t)1 << 32,
-              "threads of a launch of the smallest tiles: 64 rows by 64 features, or of both weight gradients by 128 columns");
+static_assert((kLaunchRows / 64) * (MOSAIC_MAX_ROW / 64) <= INT32_MAX &&
+                  (2 * (int64_t)MOSAIC_MAX_ROW / 64) * (MOSAIC_MAX_ROW / 128) <= INT32_MAX,
+              "tiles of a launch of the projections, or dx, and of the weight gradients");
 
 // The tiles there are, what one step of 64 k takes all CUs at work, in us, and what filling a long ring adds.  A block's step is
 // bound by the latency of its copies or by the matrix cores, so a tile takes the same where it is alone and a launch takes
