@@ -149,3 +149,33 @@ def test_checkpoints_of_more_rows_than_a_round(T, d):
         want = x[at].double()
         assert ((back - want).abs() <= 0.5 * scales + 4 * ref.U_F32 * want.abs()).all()
         assert torch.equal(out[at], ref.restored(q8.values[at], q8.scales[at], 64).float())
+
+
+@pytest.mark.parametrize("T,d", [(1500, 4104), (1101, 8192), (1030, 8200), (1030, 12296), (1027, 16384)])
+@pytest.mark.parametrize("kept", ["bf16", "f32", "int8", "e4m3"])
+def test_norms_of_wide_rows(T, d, kept):
+    """Rows of more than 4096 columns, several a block in the backward pass, where the next row is not asked for ahead."""
+    gen = device_generator(T + d)
+    stream = torch.float32 if kept == "f32" else torch.bfloat16
+    x, r = matrix(T, d, gen), matrix(T, d, gen, stream, 2.0)
+    dy, dsum_in = matrix(T, d, gen, scale=0.01), matrix(T, d, gen, stream, 0.01)
+    gamma = 1 + 0.2 * torch.randn(d, generator=gen, device=DEV)
+    y, total, dsum = torch.empty_like(x), torch.empty_like(r), torch.empty_like(r)
+    dgamma = torch.empty(d, device=DEV)
+    work = torch.empty(b.mosaic_rmsnorm_backward_workspace_bytes(T, d), dtype=torch.uint8, device=DEV)
+    b.mosaic_rmsnorm_forward(x, r, gamma, EPS, y, sum=total)
+    check_norm(y, x.double() + r.double(), gamma)
+    source, h = total, total
+    if kept in ("int8", "e4m3"):
+        source = b.Q8Rows.empty(T, d, torch.int8 if kept == "int8" else torch.float8_e4m3fn, 64, DEV)
+        b.mosaic_checkpoint_store(total, source)
+        h = ref.restored(source.values, source.scales, 64)
+    b.mosaic_rmsnorm_backward(dy, source, gamma, EPS, dsum, dgamma, work, dsum_in=dsum_in)
+    want, want_gamma = ref.norm_gradients(dy, h, gamma, EPS, dsum_in)
+    rms = torch.sqrt(h.double().square().mean(dim=1, keepdim=True) + EPS)
+    n, c = h.double() / rms, dy.double() * gamma.double()
+    size = (c.abs() + n.abs() * (c * n).abs().mean(dim=1, keepdim=True)) / rms + dsum_in.double().abs()
+    unit = ref.U_BF16 if stream == torch.bfloat16 else ref.U_F32
+    assert ((dsum.double() - want).abs() <= unit * want.abs() + (d + 32) * ref.U_F32 * size + 1e-38).all()
+    size = (dy.double() * n).abs().sum(dim=0)
+    assert ((dgamma.double() - want_gamma).abs() <= (T + d + 32) * ref.U_F32 * size + 1e-38).all()
