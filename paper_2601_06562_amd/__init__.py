@@ -1,7 +1,8 @@
 """MI355X-native mask-only logits for diffusion-LLM denoising steps (Mosaic, arXiv 2601.06562).
 
 The product is the HIP library behind ``include/mosaic.h`` and, for the layer work on either side
-of the logits, ``include/mosaic_layer.h``; ``binding`` marshals torch device tensors to it, ``workloads`` draws the seeded synthetic inputs, ``build`` compiles the library.
+of the logits, ``include/mosaic_layer.h``; ``binding`` marshals torch device tensors to it,
+``workloads`` draws the seeded synthetic inputs, ``build`` compiles the library.
 """
 from . import binding, workloads  # noqa: F401
 from .binding import (MaskOnlyLogits, MosaicError, MosaicPlan, Q8Rows, mosaic_checkpoint_load,  # noqa: F401

@@ -9,10 +9,12 @@
 //   dw:  P = columns of x (K = T), Q = columns of dg | du
 // Operands that lie across K are read from LDS by transposing reads; nothing is transposed in memory.
 //
-// What bounds it, on one MI355X (16384 rows of d 4096, F 12288, counters and times of 256 x 256 tiles): forward 2290 us,
-// 1.44 PFLOP/s, the projections with the gradients' epilogue 2500, dx 2270, dw 2290.  The matrix cores are busy 78% of the
+// What bounds it, on MI355X (16384 rows of d 4096, F 12288, 256 x 256 tiles; boxes differ by 3%): forward 2230 to 2290 us, 1.44
+// to 1.48 PFLOP/s, the projections with the gradients' epilogue 2500, dx 2270, dw 2290.  The matrix cores are busy 78% of the
 // cycles, LDS 30% and without conflicts, at a clock of 1.65 GHz that the card's power sets: without barriers and waits the same
-// tile gains 3%.  A library's plain product of the same sizes takes 2100 us.
+// tile gains 3%.  A library's plain product of the same sizes takes 2100 us.  The projections of the backward pass, which have
+// the most operands, keep some scalar registers in vector lanes; those are read back between tiles and where a step does
+// more than move the descriptors on, not in the steps that only do that.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -384,8 +386,9 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
   f32x4_t acc[kBlocksP][QB];
   // Where the registers hold it, the largest tile takes both halves of K of a block back to back: a product that adds to the
   // block of the one before it.  The card's power is what such a product runs at, and this order draws less of it: 16384 rows
-  // of d 4096 x F 12288 forward in 2280 us for 2330, dx 2270 for 2314.  (dw, which reads both operands by transposing, would
-  // spill 117 registers: eight times slower.)  fq: a step's Q fragments; fp: those of two pairs of P blocks.
+  // of d 4096 x F 12288, both orders in turn on one box, forward in 2280 us for 2330, dx 2270 for 2314.  (dw, which reads both
+  // operands by transposing, would spill 117 registers: eight times slower.)
+  // fq: a step's Q fragments; fp: those of two pairs of P blocks.
   constexpr bool kPaired = TP == 256 && TQ == 256 && MODE != kDw;
   static_assert(!kPaired || (kSplit && SQ == 2 && 2 * kCopiesP <= (kBlocksP / 2 - 1) * QB - 2 && kCopiesQ <= QB + 1),
                 "P's copies before the meeting of a step, Q's behind it");
@@ -503,6 +506,8 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
                 vu[r] = x * act;
               }
               pack(o[i], vo);
+              // dg and du in 16 bits, once from 32, as the matrix products behind take them: it adds as much as the rounding
+              // of the results does (a relative 0.0023 in the 2-norm, where that alone is 0.0017).
               pack(g[i], vg);
               pack(u[i], vu);
             }
@@ -647,8 +652,9 @@ __device__ __forceinline__ bf16x8_t load_at(__amdgpu_buffer_rsrc_t r, uint32_t o
 // projections; its four waves take the 64 k pieces of their rows in turn, straight into registers, so that 512 consecutive
 // bytes of a row are asked for at once and no wave waits for another before the sums meet in LDS.  All of x is read by every
 // block, from L2.
-// 1 row of d 4096, F 12288: 34 us, the weights at 5.9 TB/s; of 1024 x 4096, 32 rows 6.4 us and 64 rows 8.2, where tiles take
-// 9.5.  32 features a block were slower throughout (1 row 48 us), fewer pieces under way at one row (2: 41 us).
+// 1 row of d 4096, F 12288: 34.2 to 34.5 us, the weights at 5.8 to 5.9 TB/s, as well with those of 24 layers in turn (4.8 GB, so
+// that no cache holds them) as with one layer's; of 1024 x 4096, 32 rows 6.4 us and 64 rows 8.2, where tiles take 9.5.
+// 32 features a block were slower throughout (1 row 48 us), fewer pieces under way at one row (2: 41 us).
 constexpr int kFewThreads = 256;
 
 template <int ACT, int TB>
@@ -657,7 +663,7 @@ __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(const GemmArgs a) 
   constexpr int kDeep = 4;   // pieces under way
   __shared__ f32x4_t sums[4][2 * TB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int f0 = (int)blockIdx.x * (16);
+  const int f0 = (int)blockIdx.x * 16;
   const int row = lane & 15, part = (lane >> 4) * 8;
   const int d = (int)a.depth;
   // A lane's fragments of a piece: k = 32 h + part .. + 7 of its row, h = 0, 1.  What lies past the end of the rows or of K

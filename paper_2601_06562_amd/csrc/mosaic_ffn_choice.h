@@ -34,9 +34,9 @@ static_assert((kLaunchRows / 64) * (MOSAIC_MAX_ROW / 64) <= INT32_MAX &&
 // 300 rows in 77 us for 87, 1000 in 160 for 183; d 3584, F 18944: 500 in 131 for 155).  Few rows are bound by how many
 // bytes are under way: there the rings take all LDS (37 rows of d 3584, F 18944 in 50.8 us by 96 features and five slots, of
 // 128 features 56.4; 32 rows of d 4096, F 12288 in 37.9 with six slots, 41.2 with three in two blocks a CU).
-// Times from 16 to 8192 rows of 12288 x 4096, 18944 x 3584, 5632 x 2048, 4096 x 1024 and 2048 x 512, forward and dw: of the
-// first six tiles the choice is the fastest or within 2% of it in 128 of 130 sizes (6% in the worst), and the others take up to
-// 2.7 times as long.
+// Each tile forced in turn, 16 to 8192 rows of 12288 x 4096, 18944 x 3584, 5632 x 2048, 4096 x 1024 and 2048 x 512, weights from
+// memory, all four products, 270 times: the choice is within 2% of the fastest in 216 and within 5% in 256.  The most it loses is
+// 13%, where the projections of the backward pass would do better with 192 x 256 (1024 rows of 12288 x 4096, 194 us for 173).
 struct Tile { int p, q; double step, step_alone, fill; int per_cu; };
 constexpr Tile kTiles[] = {
     {256, 256, 1.50, 1.50, 0.0, 1}, {128, 256, 0.91, 0.91, 0.0, 1}, {256, 128, 0.92, 0.92, 0.0, 1}, {128, 128, 0.60, 0.60, 0.0, 1},
@@ -108,7 +108,10 @@ inline GradientPlan plan_gradients(int64_t T, int32_t d, int32_t F) {
 // Whether these rows go to the kernel for few: where its blocks are no more than the CUs, up to its 64 rows; beyond, while what
 // the blocks read of x is little beside the weights (rows of d 4096, F 8192: 16 in 27.6 us, the tiles 30.9; 32 in 37.4 and
 // 32.4; F 12288: 8 in 37.0 and 37.4, 16 in 39.4 and 37.6; d 3584, F 18944: 4 in 49.2 and 49.6, 16 in 57.1 and 50.0).  Past the
-// features that tiles of 96 take in one round the tiles read faster (d 8192, F 28672: 1 row in 157 us for 173).
+// features that tiles of 96 take in one round the tiles read faster (d 8192, F 28672: 1 row in 157 us for 173).  The rule has no
+// d in it: up to F 4096 this kernel was the faster one for 1, 8, 16, 32 and 64 rows of every d from 1024 to 16384 (64 rows of F
+// 4096, d 16384: 110 us and 112); at F 8192, 1 to 16 rows, up to d 8192 (there 47 to 49 us and 52 to 54), but not at d 16384
+// (138 to 148 us and 102 to 108).
 inline bool few_rows(int64_t T, int32_t F) {
   return T <= 64 && (F <= 16 * kCus || (F <= 96 * kCus && T * F <= (int64_t)1 << 17));
 }

@@ -131,6 +131,8 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float* lds, int turn) {
 // four), NV vectors of 8 columns each, so that the sum of squares is one exchange and the row is not read again.  Four waves a
 // row beyond 1024 columns: 16384 x 4096 in bf16 in 97 us, where a wave a row, with four times the registers and fewer rows in
 // flight, took 145.  32768 x 4096, 32-bit stream, with the 8-bit output: 332 us, 5.7 TB/s.  1 row: 4 us.
+// Beyond 8192 columns a lane holds 64 of them and fewer rows are in flight: 4096 x 16384 in 143 us, 3.8 TB/s (32-bit stream
+// 184, 4.4).
 constexpr int kThreads = 256;
 
 template <typename S, int R, int NV>
@@ -239,7 +241,8 @@ template <> struct Raw<uint8_t> {
 // and leaves one partial sum; norm_gamma_kernel adds those up.  Rows in turn, not in blocks: the same sums on every call.
 // With n = h rstd and c = gamma dy the gradient is rstd (c - n mean(c n)): both sums of a row are one exchange.
 // 16384 x 4096 in bf16: 110 us, 4.9 TB/s; without the next row on its way 114.  1003 x 3584 from 8 bits: 11 us, of which the
-// traffic is 5: two rows a block leave little to overlap, and one or four a block take as long.
+// traffic is 5: two rows a block leave little to overlap, and one or four a block take as long.  Beyond 4096 columns the next row
+// is not asked for ahead, beyond 8192 a SIMD holds one wave: 8192 x 8192 in 112 us, 4.8 TB/s, 4096 x 16384 in 141, 3.8.
 template <int FROM, typename S, int R, int NV>
 __global__ __launch_bounds__(kThreads) void rmsnorm_backward_kernel(const NormBackwardArgs p) {
   constexpr int kRows = kThreads / R;
@@ -361,7 +364,8 @@ __global__ __launch_bounds__(kGammaThreads) void norm_gamma_kernel(const float* 
 
 // A wave per row and turn; `padded` columns so that the lanes of a group all take part in its maximum.  The scale needs the
 // group's columns alone, which neighbouring lanes hold: no exchange beyond 16 lanes, one pass.
-// 65535 x 3584 in bf16: stored in 148 us, restored in 116 (4.8 and 6.1 TB/s).
+// 65535 x 3584: bf16 stored in 134 to 148 us, restored in 116 to 130 (4.8 to 6.1 TB/s); 32-bit stored in 228, restored in 309
+// (5.1 and 3.8 TB/s).
 template <typename S>
 __global__ __launch_bounds__(256) void checkpoint_store_kernel(const S* __restrict__ x, int64_t ld_x, int64_t T, int d,
                                                                const mosaic_q8_rows q8) {
