@@ -123,7 +123,9 @@ int mosaic_gated_ffn_forward(const void *x, int64_t ld_x, const void *w_gate, co
  * g = x w_gate^T, u = x w_up^T:
  *   dg = dout * u * act'(g),  du = dout * act(g)      rounded to bf16, for the matrix cores (up to 2^-8 relative
  *                                                     per term, as for the results; in the 2-norm of a result of
- *                                                     many terms 0.0023 in all, where its own rounding is 0.0017)
+ *                                                     many terms 0.0023 in all, where its own rounding is 0.0017);
+ *                                                     up to 32 rows with what that leaves over in a second number
+ *                                                     each, so that the results' own rounding is all there is
  *   dx = dg w_gate + du w_up,   dw_gate = dg^T x,   dw_up = du^T x
  *   x          bf16 [T, d], or NULL and
  *   q8         its rows in 8 bits; the gradients are those at the values they stand for
@@ -134,7 +136,7 @@ int mosaic_gated_ffn_forward(const void *x, int64_t ld_x, const void *w_gate, co
  *   accumulate nonzero: the weight gradients are added to what dw_gate and dw_up hold (32-bit only), so that a batch can be
  *              taken in parts
  *   workspace  dev, 16-byte aligned, mosaic_gated_ffn_backward_workspace_bytes(T, d, F, q8 != NULL) bytes: dg and du,
- *              4 T F bytes, the restored input, 2 T d, and for up to 4096 rows partial sums of dx.  A
+ *              4 T F bytes (up to 32 rows 8 T F), the restored input, 2 T d, and for up to 4096 rows partial sums of dx.  A
  *              workspace for T rows serves fewer rows, too
  */
 int64_t mosaic_gated_ffn_backward_workspace_bytes(int64_t T, int32_t d, int32_t F, int32_t q8_input);

@@ -51,6 +51,8 @@ struct GemmArgs {
   char* out0;          // forward: out; kRecompute: out or nullptr; kDx: dx or the partial sums; kDw: dw_gate
   char* out1;          // kRecompute: dg | du; kDw: dw_up
   int64_t ld_out0, ld_out1;
+  int64_t low;         // kRecompute: from a row of dg | du to that of its low halves, bytes; 0: none are wanted
+  int32_t repeat;      // kDw: rows of x there are where K, one step then, takes them twice; else 0
 };
 
 __device__ __forceinline__ float sigmoid(float z) {
@@ -90,14 +92,16 @@ struct Copier {
   }
 
   // `valid`: rows there are; `left`: k there are, where rows lie along K (across K the descriptor's end cuts them).
-  __device__ __forceinline__ void place(int wave, int lane, int64_t ld, int64_t valid, int left) {
+  // `repeat`: across K, rows there are that come a second time behind themselves, or 0.
+  __device__ __forceinline__ void place(int wave, int lane, int64_t ld, int64_t valid, int left, int repeat = 0) {
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
       const int byte = (wave * kCopies + i) * 1024 + lane * 16;
       if constexpr (KROW) {
         const int k = byte / (ROWS * 2), piece = byte % (ROWS * 2) / 16;
         const int col = ((piece >> 1) ^ turn(k)) * 16 + (piece & 1) * 8;
-        offset[i] = col < valid ? (uint32_t)(k * (uint32_t)ld + col * 2) : kOutside;
+        const int from = repeat != 0 && k >= repeat ? k - repeat : k;
+        offset[i] = col < valid ? (uint32_t)(from * (uint32_t)ld + col * 2) : kOutside;
       } else {
         const int row = byte / 128, piece = byte % 128 / 16;
         const int k = (piece ^ (row >> 1 & 7)) * 8;
@@ -229,6 +233,17 @@ __device__ __forceinline__ void pack(Quad& w, const float (&v)[4]) {
   w[0] = u.x;
   w[1] = u.y;
 }
+// What the rounding to `high` left of v, rounded in turn; zero beside what is no finite number.
+__device__ __forceinline__ void pack_low(Quad& w, const Quad& high, const float (&v)[4]) {
+  const bf16x4_t h = __builtin_bit_cast(bf16x4_t, uint2{high[0], high[1]});
+  float low[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const float l = v[r] - (float)h[r];
+    low[r] = __builtin_fabsf(l) < __builtin_inff() ? l : 0.f;
+  }
+  pack(w, low);
+}
 
 // LDS of a tile: a ring of SP slots for P, of SQ for Q.
 constexpr int ring_bytes(int TP, int TQ, int SP, int SQ) { return (SP * TP + SQ * TQ) * kStepK * 2; }
@@ -291,7 +306,7 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
       p_base1 = MODE == kDx ? a.p1 + (int64_t)p_row * 2 : p_base0;
     }
     q_base = kRowQ ? a.q + q_row * 2 : a.q + q_row * a.ld_q;
-    cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, kStepK);
+    cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, kStepK, MODE == kDw ? a.repeat : 0);
     cq.place(wave, lane, a.ld_q, a.rows_q - q_row, kStepK);
     placed_p = placed_q = kStepK;
     step0 = (int)((int64_t)all_steps * split / a.splits);
@@ -336,8 +351,9 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
       placed_p = left;
       cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, left);
     }
+    const int rows = MODE == kDw && a.repeat != 0 && left != 0 ? a.repeat : left;   // across K: there are behind the base
     walk_p.from = buffer_from((seg ? p_base1 : p_base0) + (kRowP ? k * a.ld_p : k * 2),
-                              kRowP ? left * (uint32_t)a.ld_p : left == 0 ? 0 : kOutside);
+                              kRowP ? rows * (uint32_t)a.ld_p : left == 0 ? 0 : kOutside);
   };
   auto locate_q = [&](int step) __attribute__((always_inline)) {
     int seg;
@@ -490,7 +506,8 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
               pack(o[i], v);
             }
           } else {
-            Quad g[NB], u[NB];
+            constexpr bool kLow = TQ == 64;   // the tiles that few rows take
+            Quad g[NB], u[NB], gl[kLow ? NB : 1], ul[kLow ? NB : 1];
             scatter(grad[j]);
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
@@ -507,15 +524,30 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
               }
               pack(o[i], vo);
               // dg and du in 16 bits, once from 32, as the matrix products behind take them: it adds as much as the rounding
-              // of the results does (a relative 0.0023 in the 2-norm, where that alone is 0.0017).
+              // of the results does (a relative 0.0023 in the 2-norm, where that alone is 0.0017); few rows, in whose sums it
+              // does not average out, carry what is left over in a second row.
               pack(g[i], vg);
               pack(u[i], vu);
+              if constexpr (kLow) {
+                pack_low(gl[i], g[i], vg);
+                pack_low(ul[i], u[i], vu);
+              }
             }
             gather(g);
             gather(u);
             if (in) {
               store_quads(a.out1 + q * a.ld_out1, f, a.rows_p, g);
               store_quads(a.out1 + q * a.ld_out1 + (int64_t)a.F * 2, f, a.rows_p, u);
+            }
+            if constexpr (kLow) {
+              if (a.low != 0) {
+                gather(gl);
+                gather(ul);
+                if (in) {
+                  store_quads(a.out1 + a.low + q * a.ld_out1, f, a.rows_p, gl);
+                  store_quads(a.out1 + a.low + q * a.ld_out1 + (int64_t)a.F * 2, f, a.rows_p, ul);
+                }
+              }
             }
           }
           gather(o);
@@ -736,20 +768,30 @@ __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(const GemmArgs a) 
 #endif
 }
 
-// Adds the parts of dx in their order and rounds once.  Bound by its reads: six parts of 1237 x 1024 in 6 us, 5.4 TB/s.
+// Adds the parts of dx in their order and rounds once.  Bound by its reads: six parts of 1237 x 1024 in 6 us, 5.4 TB/s; for few rows
+// by their latency, so that eight parts are asked for at once: 32 parts of 1 x 512 in 3.9 us, one after another 9.4.
 __global__ __launch_bounds__(256) void ffn_join_kernel(const float* __restrict__ partials, int splits, int64_t T, int d,
                                                        __bf16* __restrict__ dx, int64_t ld) {
+  constexpr int kAtOnce = 8;
   const int per_row = d / 8;
   const int64_t all = T * per_row;
   for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
     const int64_t t = e / per_row;
     const int c = (int)(e - t * per_row) * 8;
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < splits; ++k) {
-      float v[8];
-      load8(partials + ((int64_t)k * T + t) * d + c, v);
+    for (int k = 0; k < splits; k += kAtOnce) {
+      float v[kAtOnce][8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] += v[i];
+      for (int n = 0; n < kAtOnce; ++n) {   // past the last part the last one again, which nobody adds
+        const int part = k + n < splits ? k + n : splits - 1;
+        load8(partials + ((int64_t)part * T + t) * d + c, v[n]);
+      }
+      __builtin_amdgcn_sched_barrier(0);    // all of them under way
+#pragma unroll
+      for (int n = 0; n < kAtOnce; ++n) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += k + n < splits ? v[n][i] : 0.f;
+      }
     }
     store8(dx + t * ld + c, s);
   }
@@ -818,8 +860,16 @@ int launch_gated(const GemmArgs& a, int activation, hipStream_t stream) {
 
 }  // namespace
 
-// Rows of 32-bit partial sums that dx may take for up to T rows: no less for more rows, so that a workspace serves fewer too.
-int64_t ffn_partial_rows(int64_t T) { return T * kMostParts < kPartRows ? T * kMostParts : kPartRows; }
+// Rows of dg | du with their low halves, and of 32-bit partial sums that dx may take, for up to T rows: no less for more rows, so
+// that a workspace serves fewer too.
+int64_t ffn_gradient_rows(int64_t T) {
+  const int64_t halves = 2 * (T < kHalvesRows ? T : kHalvesRows);
+  return T > halves ? T : halves;
+}
+int64_t ffn_partial_rows(int64_t T) {
+  const int64_t halves = 2 * kMostParts * (T < kHalvesRows ? T : kHalvesRows), whole = T * kMostParts < kPartRows ? T * kMostParts : kPartRows;
+  return whole > halves ? whole : halves;
+}
 
 int launch_gated_ffn_forward(const FfnForwardArgs& f, hipStream_t stream) {
   GemmArgs a = {};
@@ -845,6 +895,8 @@ int launch_gated_ffn_forward(const FfnForwardArgs& f, hipStream_t stream) {
 
 int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
   const int64_t ld_grads = (int64_t)f.F * 4;
+  const bool halves = with_low_halves(f.T);
+  const int64_t rows = halves ? 2 * f.T : f.T;   // of dg | du
   for (int64_t t = 0; t < f.T; t += kLaunchRows) {
     GemmArgs a = {};
     a.p0 = static_cast<const char*>(f.w_gate);
@@ -863,6 +915,7 @@ int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
     a.out0 = f.out == nullptr ? nullptr : static_cast<char*>(f.out) + t * a.ld_out0;
     a.ld_out1 = ld_grads;
     a.out1 = static_cast<char*>(f.grads) + t * ld_grads;
+    a.low = halves ? f.T * ld_grads : 0;
     if (launch_gated<kRecompute>(a, f.activation, stream) != 0) return -1;
   }
   const GradientPlan plan = plan_gradients(f.T, f.d, f.F);
@@ -874,7 +927,8 @@ int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
   x.rows_p = f.d;
   x.depth = f.F;
   x.splits = plan.splits;
-  x.f32 = plan.splits > 1;      // then all rows are in one launch
+  const int parts = (int)plan.splits * (halves ? 2 : 1);   // of dx, added by the join: of every part of K the rows, then their low halves
+  x.f32 = parts > 1;            // then all rows are in one launch
   x.ld_out0 = x.f32 ? (int64_t)f.d * 4 : f.ld_dx * 2;
   GemmArgs w = {};
   w.p0 = w.p1 = static_cast<const char*>(f.x);
@@ -883,7 +937,8 @@ int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
   w.ld_q = ld_grads;
   w.rows_q = 2 * (int64_t)f.F;
   w.rows_p = f.d;
-  w.depth = f.T;
+  w.depth = rows;
+  w.repeat = halves ? (int32_t)f.T : 0;
   w.splits = 1;
   w.F = f.F;
   w.f32 = f.dw_f32;
@@ -892,8 +947,8 @@ int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
   w.out1 = static_cast<char*>(f.dw_up);
   w.ld_out0 = f.ld_dw * (f.dw_f32 ? 4 : 2);
   const bool together = plan.tile >= 0 && f.dx != nullptr && f.dw_gate != nullptr;
-  for (int64_t t = 0; f.dx != nullptr && t < f.T; t += kLaunchRows) {
-    x.rows_q = f.T - t < kLaunchRows ? f.T - t : kLaunchRows;
+  for (int64_t t = 0; f.dx != nullptr && t < rows; t += kLaunchRows) {
+    x.rows_q = rows - t < kLaunchRows ? rows - t : kLaunchRows;
     x.q = static_cast<const char*>(f.grads) + t * ld_grads;
     x.out0 = x.f32 ? reinterpret_cast<char*>(f.partials) : static_cast<char*>(f.dx) + t * x.ld_out0;
     const int rc = !together ? launch_gemm<kDx, 0>(x, stream)
@@ -902,10 +957,10 @@ int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
                                     : launch_together<3, 4, 4>(x, w, stream);
     if (rc != 0) return -1;
   }
-  if (f.dx != nullptr && plan.splits > 1) {
+  if (f.dx != nullptr && parts > 1) {
     const int64_t blocks = tiles(f.T * (f.d / 8), 256);
     if (launch_kernel(ffn_join_kernel, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), stream, f.partials,
-                      (int)plan.splits, f.T, f.d, static_cast<__bf16*>(f.dx), f.ld_dx) != 0)
+                      parts, f.T, f.d, static_cast<__bf16*>(f.dx), f.ld_dx) != 0)
       return -1;
   }
   if (f.dw_gate != nullptr && !together && launch_gemm<kDw, 0>(w, stream) != 0) return -1;

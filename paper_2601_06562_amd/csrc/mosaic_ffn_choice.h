@@ -37,6 +37,14 @@ static_assert((kLaunchRows / 64) * (MOSAIC_MAX_ROW / 64) <= INT32_MAX &&
 // Each tile forced in turn, 16 to 8192 rows of 12288 x 4096, 18944 x 3584, 5632 x 2048, 4096 x 1024 and 2048 x 512, weights from
 // memory, all four products, 270 times: the choice is within 2% of the fastest in 216 and within 5% in 256.  The most it loses is
 // 13%, where the projections of the backward pass would do better with 192 x 256 (1024 rows of 12288 x 4096, 194 us for 173).
+// Up to how many rows dg and du have a second number an element, what the rounding of the first left over.  Twice the rows then
+// still fit one tile of rows for dx and one step of K for the weights' gradients, so it costs up to 3% of a call (32 rows of d
+// 4096, F 12288: 148 us for 144; 1 row 139 either way).  In the gradients of few rows few terms count, and the rounding of
+// those does not average out: with it the error against 64 bits was up to 1.57 times that of the results' own rounding (1 to 3
+// rows of d 512, F 2048); from 33 rows on it is 1.44 at most, about the square root of 2.
+constexpr int64_t kHalvesRows = 32;
+inline bool with_low_halves(int64_t T) { return T > 0 && T <= kHalvesRows; }
+
 struct Tile { int p, q; double step, step_alone, fill; int per_cu; };
 constexpr Tile kTiles[] = {
     {256, 256, 1.50, 1.50, 0.0, 1}, {128, 256, 0.91, 0.91, 0.0, 1}, {256, 128, 0.92, 0.92, 0.0, 1}, {128, 128, 0.60, 0.60, 0.0, 1},
@@ -56,13 +64,14 @@ inline TileGrid tile_grid(int mode, int i, int64_t rows_p, int64_t rows_q, int64
 
 struct Choice { int tile; double us; };
 inline Choice choose_tile(int mode, int64_t rows_p, int64_t rows_q, int64_t steps, int64_t splits) {
-  Choice best = {0, 0.0};
+  Choice best = {-1, 0.0};
   for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
     const Tile& t = kTiles[i];
     if (t.p == 192 && !gated_mode(mode)) continue;   // across K its rows would not be a power of two
+    if (t.q > 64 && gated_mode(mode) && rows_q <= 64) continue;   // (slower; and the tiles of 64 rows write low halves)
     const int64_t n = tile_grid(mode, i, rows_p, rows_q, splits).n;
     const double us = (double)tiles(n, kCus * t.per_cu) * (double)tiles(steps, splits) * (n <= kCus ? t.step_alone : t.step) + t.fill;
-    if (i == 0 || us < best.us) best = {i, us};
+    if (best.tile < 0 || us < best.us) best = {i, us};
   }
   return best;
 }
@@ -80,7 +89,8 @@ inline GradientPlan plan_gradients(int64_t T, int32_t d, int32_t F) {
   const double dw = choose_tile(kDw, d, 2 * (int64_t)F, steps_w, 1).us;
   double least = 0.0;
   for (int32_t s = 1; s == 1 || (s <= kMostParts && s * T <= kPartRows && s * 4 <= steps_x); ++s) {
-    const double join = s == 1 ? 0.0 : kLaunchUs + (double)(T * d) * 8.0 * s / kJoinBytesPerUs;
+    const int32_t parts = with_low_halves(T) ? 2 * s : s;
+    const double join = parts == 1 ? 0.0 : kLaunchUs + (double)(T * d) * 8.0 * parts / kJoinBytesPerUs;
     const double apart = choose_tile(kDx, d, T, steps_x, s).us + dw + kLaunchUs + join;
     if (s == 1 || apart < least) {
       least = apart;

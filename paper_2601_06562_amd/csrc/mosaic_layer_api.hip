@@ -47,10 +47,11 @@ struct FfnSpace {
 constexpr int64_t kPartialT = 4096;
 FfnSpace ffn_space(int64_t T, int32_t d, int32_t F, bool q8) {
   FfnSpace s;
-  s.restored = round_up(4 * T * F, 256);
+  s.restored = round_up(4 * mosaic::ffn_gradient_rows(T) * F, 256);
   s.partials = s.restored + (q8 ? round_up(2 * T * d, 256) : 0);
   const int64_t few = T < kPartialT ? T : kPartialT;   // the most that up to T rows need with their sums
-  const int64_t with_sums = round_up(4 * few * F, 256) + (q8 ? round_up(2 * few * d, 256) : 0) + 4 * mosaic::ffn_partial_rows(few) * d;
+  const int64_t with_sums = round_up(4 * mosaic::ffn_gradient_rows(few) * F, 256) + (q8 ? round_up(2 * few * d, 256) : 0) +
+                            4 * mosaic::ffn_partial_rows(few) * d;
   s.total = with_sums > s.partials ? with_sums : s.partials;
   return s;
 }

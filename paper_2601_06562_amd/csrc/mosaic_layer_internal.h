@@ -66,11 +66,12 @@ struct FfnBackwardArgs {
   void* dx;       // or nullptr
   void* dw_gate;  // or nullptr
   void* dw_up;
-  void* grads;      // bf16 [T, 2 F]: dg | du
-  float* partials;  // fp32 [ffn_partial_rows(T), d]: sums of dx over parts of K
+  void* grads;      // bf16 [ffn_gradient_rows(T), 2 F]: dg | du, for few rows their low halves behind them
+  float* partials;  // fp32 [ffn_partial_rows(T), d]: sums of dx over parts of K and halves
   int64_t ld_dout, ld_x, ld_w, ld_out, ld_dx, ld_dw, T;
   int32_t d, F, activation, dw_f32, accumulate;
 };
+int64_t ffn_gradient_rows(int64_t T);
 int64_t ffn_partial_rows(int64_t T);
 int launch_gated_ffn_backward(const FfnBackwardArgs& a, hipStream_t stream);
 
