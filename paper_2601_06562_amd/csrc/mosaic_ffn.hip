@@ -9,7 +9,7 @@
 //   dw:  P = columns of x (K = T), Q = columns of dg | du
 // Operands that lie across K are read from LDS by transposing reads; nothing is transposed in memory.
 //
-// What bounds it, on MI355X (16384 rows of d 4096, F 12288, 256 x 256 tiles; boxes differ by 3%): forward 2230 to 2290 us, 1.44
+// What bounds it, on MI355X (16384 rows of d 4096, F 12288, 256 x 256 tiles; cards differ by 3%): forward 2230 to 2290 us, 1.44
 // to 1.48 PFLOP/s, the projections with the gradients' epilogue 2500, dx 2270, dw 2290.  The matrix cores are busy 78% of the
 // cycles, LDS 30% and without conflicts, at a clock of 1.65 GHz that the card's power sets: without barriers and waits the same
 // tile gains 3%.  A library's plain product of the same sizes takes 2100 us.  The projections of the backward pass, which have
@@ -402,7 +402,7 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
   f32x4_t acc[kBlocksP][QB];
   // Where the registers hold it, the largest tile takes both halves of K of a block back to back: a product that adds to the
   // block of the one before it.  The card's power is what such a product runs at, and this order draws less of it: 16384 rows
-  // of d 4096 x F 12288, both orders in turn on one box, forward in 2280 us for 2330, dx 2270 for 2314.  (dw, which reads both
+  // of d 4096 x F 12288, both orders in turn on one card, forward in 2280 us for 2330, dx 2270 for 2314.  (dw, which reads both
   // operands by transposing, would spill 117 registers: eight times slower.)
   // fq: a step's Q fragments; fp: those of two pairs of P blocks.
   constexpr bool kPaired = TP == 256 && TQ == 256 && MODE != kDw;
