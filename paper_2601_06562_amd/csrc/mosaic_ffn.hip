@@ -9,7 +9,7 @@
 //   dw:  P = columns of x (K = T), Q = columns of dg | du
 // Operands that lie across K are read from LDS by transposing reads; nothing is transposed in memory.
 //
-// What bounds it, on MI355X (16384 rows of d 4096, F 12288, 256 x 256 tiles; cards differ by 3%): forward 2230 to 2290 us, 1.44
+// What bounds it, on MI355X (16384 rows of d 4096, F 12288, 256 x 256 tiles; cards differ by 4%): forward 2230 to 2320 us, 1.42
 // to 1.48 PFLOP/s, the projections with the gradients' epilogue 2500, dx 2270, dw 2290.  The matrix cores are busy 78% of the
 // cycles, LDS 30% and without conflicts, at a clock of 1.65 GHz that the card's power sets: without barriers and waits the same
 // tile gains 3%.  A library's plain product of the same sizes takes 2100 us.  The projections of the backward pass, which have
