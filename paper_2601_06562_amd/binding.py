@@ -1,8 +1,8 @@
 """ctypes binding of libmosaic.so -- argument marshalling only.
 
 Every step of the path runs in the HIP kernels behind the C ABI declared in
-``include/mosaic.h`` and ``include/mosaic_layer.h``; the functions here have the same names and only turn torch tensors
-into device pointers.  There is no CPU or PyTorch fallback: if the library is missing,
+``include/mosaic.h``, ``include/mosaic_layer.h`` and ``include/mosaic_tokens.h``; the functions here have the same names
+and only turn torch tensors into device pointers.  There is no CPU or PyTorch fallback: if the library is missing,
 loading raises.
 """
 from __future__ import annotations
@@ -42,6 +42,10 @@ LAYER_EXPORTS = (   # include/mosaic_layer.h
     "mosaic_checkpoint_store", "mosaic_checkpoint_load", "mosaic_rmsnorm_forward",
     "mosaic_rmsnorm_backward_workspace_bytes", "mosaic_rmsnorm_backward", "mosaic_gated_ffn_forward",
     "mosaic_gated_ffn_backward_workspace_bytes", "mosaic_gated_ffn_backward",
+)
+TOKEN_EXPORTS = (   # include/mosaic_tokens.h
+    "mosaic_embedding_forward", "mosaic_embedding_backward_workspace_bytes", "mosaic_embedding_backward",
+    "mosaic_dropout_forward", "mosaic_dropout_backward",
 )
 BF16, F32 = 0, 1                     # mosaic_type
 INT8, E4M3 = 0, 1                    # mosaic_q8_format
@@ -562,6 +566,90 @@ def mosaic_gated_ffn_backward(dout, x, w_gate, w_up, dx, dw_gate, dw_up, workspa
         p_do, ld_do, p_x, ld_x, q8._ref if q8 is not None else None, p_g, p_u, ld_w, T, d, F, int(activation), p_o, ld_o,
         p_dx, ld_dx, p_dg, p_du, dw_type, ld_dw, int(bool(accumulate)), *_workspace_args(workspace), _stream_ptr(stream)),
         "mosaic_gated_ffn_backward")
+
+
+# ---- tokens into rows and rows back onto given tokens (include/mosaic_tokens.h)
+
+_token_lib = None
+
+
+def _tokens():
+    """lib(), with the prototypes of include/mosaic_tokens.h."""
+    global _token_lib
+    if _token_lib is None:
+        L = lib()
+        p, i64, i32, u64, f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_uint64, ctypes.c_float
+        L.mosaic_embedding_forward.restype = ctypes.c_int
+        L.mosaic_embedding_forward.argtypes = [p, i64, p, p, i32, i64, i32, i32, f32, p, i32, i64, p]
+        L.mosaic_embedding_backward_workspace_bytes.restype = i64
+        L.mosaic_embedding_backward_workspace_bytes.argtypes = [i64, i32, i32]
+        L.mosaic_embedding_backward.restype = ctypes.c_int
+        L.mosaic_embedding_backward.argtypes = [p, i32, i64, p, i64, p, i32, i32, f32, p, i32, i64, i32, p, i64, p]
+        L.mosaic_dropout_forward.restype = ctypes.c_int
+        L.mosaic_dropout_forward.argtypes = [p, i64, p, i32, i64, i64, i32, f32, u64, i32, i64, p, i64, p]
+        L.mosaic_dropout_backward.restype = ctypes.c_int
+        L.mosaic_dropout_backward.argtypes = [p, i32, i64, i64, i32, f32, u64, i32, i64, p, i64, p]
+        _token_lib = L
+    return _token_lib
+
+
+def _count_ptr(count):
+    if count is None:
+        return 0
+    if count.numel() == 0:
+        raise ValueError("count must hold an element")
+    return _dev_ptr(count, "count", torch.int32)
+
+
+def mosaic_embedding_forward(tokens, table, out, scale=1.0, count=None, stream=None):
+    """out[t] = scale * table[tokens[t]], zeros where a token lies outside the table: tokens int32 [T], table bf16 or float32
+    [V, d], out bf16 or float32 [T, d].  count (int32 [1] or None): only so many rows are written."""
+    T, (V, d) = tokens.numel(), table.shape
+    p_table, ld_table = _rows(table, "table", V, d)
+    p_out, ld_out = _rows(out, "out", T, d)
+    _check(_tokens().mosaic_embedding_forward(_dev_ptr(tokens, "tokens", torch.int32), T, _count_ptr(count), p_table,
+                                              _type_of(table, "table"), ld_table, V, d, float(scale), p_out,
+                                              _type_of(out, "out"), ld_out, _stream_ptr(stream)), "mosaic_embedding_forward")
+
+
+def mosaic_embedding_backward_workspace_bytes(T, d, V) -> int:
+    return int(_tokens().mosaic_embedding_backward_workspace_bytes(T, d, V))
+
+
+def mosaic_embedding_backward(dout, tokens, dtable, workspace, scale=1.0, count=None, accumulate=False, stream=None):
+    """dtable[v] = scale * the sum of dout over the positions of token v (added to what dtable holds if accumulate, float32
+    only): dout bf16 or float32 [T, d], tokens int32 [T], dtable bf16 or float32 [V, d]."""
+    T, (V, d) = tokens.numel(), dtable.shape
+    p_dout, ld_dout = _rows(dout, "dout", T, d)
+    p_table, ld_table = _rows(dtable, "dtable", V, d)
+    _check(_tokens().mosaic_embedding_backward(
+        p_dout, _type_of(dout, "dout"), ld_dout, _dev_ptr(tokens, "tokens", torch.int32), T, _count_ptr(count), V, d,
+        float(scale), p_table, _type_of(dtable, "dtable"), ld_table, int(bool(accumulate)), *_workspace_args(workspace),
+        _stream_ptr(stream)), "mosaic_embedding_backward")
+
+
+def mosaic_dropout_forward(x, residual, out, p, seed, site=0, first_row=0, stream=None):
+    """out = x with a share p of its elements dropped and the others grown [+ residual]: x bf16 [T, d], residual (or None) and
+    out bf16 or float32, both of one type.  The mask follows from seed, site, first_row + row, and column."""
+    T, d = x.shape
+    if residual is not None and residual.dtype != out.dtype:
+        raise TypeError("out must have the residual's type")
+    p_x, ld_x = _rows(x, "x", T, d, torch.bfloat16)
+    p_r, ld_r = _rows(residual, "residual", T, d)
+    p_o, ld_o = _rows(out, "out", T, d)
+    _check(_tokens().mosaic_dropout_forward(p_x, ld_x, p_r, _type_of(out, "out"), ld_r, T, d, float(p),
+                                            int(seed) & 0xFFFFFFFFFFFFFFFF, int(site), int(first_row), p_o, ld_o,
+                                            _stream_ptr(stream)), "mosaic_dropout_forward")
+
+
+def mosaic_dropout_backward(dout, dx, p, seed, site=0, first_row=0, stream=None):
+    """dx (bf16 [T, d]) from dout (bf16 or float32) by the mask that mosaic_dropout_forward makes of the same arguments."""
+    T, d = dout.shape
+    p_g, ld_g = _rows(dout, "dout", T, d)
+    p_x, ld_x = _rows(dx, "dx", T, d, torch.bfloat16)
+    _check(_tokens().mosaic_dropout_backward(p_g, _type_of(dout, "dout"), ld_g, T, d, float(p),
+                                             int(seed) & 0xFFFFFFFFFFFFFFFF, int(site), int(first_row), p_x, ld_x,
+                                             _stream_ptr(stream)), "mosaic_dropout_backward")
 
 
 class VmmWorkspace:

@@ -1,0 +1,150 @@
+// C ABI entry points of the token operators: argument validation, then enqueue.  See include/mosaic_tokens.h.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "mosaic_arguments.h"
+#include "mosaic_tokens_internal.h"
+
+namespace {
+
+using namespace mosaic::arguments;
+
+constexpr int32_t kMostVocab = INT32_MAX - 256;
+
+int check_vocab(int32_t V) {
+  if (V <= 0) return MOSAIC_ERR_INVALID_ARG;
+  return V > kMostVocab ? MOSAIC_ERR_UNSUPPORTED_SHAPE : MOSAIC_OK;
+}
+
+// The row numbers that tokens, lists and counts are.
+bool bad_list(const int32_t* tokens, const int32_t* count) { return tokens == nullptr || misaligned(tokens, 4) || misaligned(count, 4); }
+
+struct EmbeddingSpace {
+  int64_t partials, total;   // offsets, bytes; the sort's space comes first
+};
+EmbeddingSpace embedding_space(int64_t T, int32_t d, int32_t V) {
+  EmbeddingSpace s;
+  s.partials = mosaic::sort_tokens_bytes(T, V);
+  s.total = s.partials + 4 * mosaic::token_sum_partials(T) * d;
+  return s;
+}
+
+int check_dropout(int32_t type, int64_t T, int32_t d, float p, int32_t site, int64_t first_row) {
+  if (!known_type(type) || !(p >= 0.f && p <= 1.f - 0x1p-16f) || site < 0 || site == INT32_MAX || first_row < 0)
+    return MOSAIC_ERR_INVALID_ARG;
+  MOSAIC_RETURN_IF(check_sizes(T, d, MOSAIC_MAX_ROW));
+  return first_row > INT64_MAX - T ? MOSAIC_ERR_UNSUPPORTED_SHAPE : MOSAIC_OK;
+}
+mosaic::DropoutArgs dropout_args(int64_t T, int32_t d, float p, uint64_t seed, int32_t site, int64_t first_row) {
+  mosaic::DropoutArgs a = {};
+  a.T = T;
+  a.d = d;
+  a.first_row = first_row;
+  a.border = (uint32_t)lrint((double)p * 65536.0);
+  a.grow = (float)(65536.0 / (65536.0 - a.border));
+  a.key_low = (uint32_t)seed;
+  a.key_high = (uint32_t)(seed >> 32);
+  a.site = (uint32_t)site + 1;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int mosaic_embedding_forward(const int32_t* tokens, int64_t T, const int32_t* count, const void* table, int32_t table_type,
+                             int64_t ld_table, int32_t V, int32_t d, float scale, void* out, int32_t out_type,
+                             int64_t ld_out, void* stream) {
+  if (!known_type(table_type) || !known_type(out_type) || !isfinite(scale)) return MOSAIC_ERR_INVALID_ARG;
+  MOSAIC_RETURN_IF(check_sizes(T, d, MOSAIC_MAX_ROW));
+  MOSAIC_RETURN_IF(check_vocab(V));
+  if (T == 0) return MOSAIC_OK;
+  if (bad_list(tokens, count)) return MOSAIC_ERR_INVALID_ARG;
+  MOSAIC_RETURN_IF(check_matrix(table, ld_table, d));
+  MOSAIC_RETURN_IF(check_matrix(out, ld_out, d));
+  mosaic::EmbedArgs a = {};
+  a.tokens = tokens;
+  a.count = count;
+  a.table = table;
+  a.out = out;
+  a.T = T;
+  a.ld_table = ld_table;
+  a.ld_out = ld_out;
+  a.V = V;
+  a.d = d;
+  a.scale = scale;
+  return launched(mosaic::launch_embedding_forward(a, table_type == MOSAIC_F32, out_type == MOSAIC_F32, static_cast<hipStream_t>(stream)));
+}
+
+int64_t mosaic_embedding_backward_workspace_bytes(int64_t T, int32_t d, int32_t V) {
+  if (check_sizes(T, d, MOSAIC_MAX_ROW) != MOSAIC_OK || check_vocab(V) != MOSAIC_OK) return 0;
+  return embedding_space(T, d, V).total;
+}
+
+int mosaic_embedding_backward(const void* dout, int32_t dout_type, int64_t ld_dout, const int32_t* tokens, int64_t T,
+                              const int32_t* count, int32_t V, int32_t d, float scale, void* dtable, int32_t dtable_type,
+                              int64_t ld_dtable, int32_t accumulate, void* workspace, int64_t workspace_bytes,
+                              void* stream) {
+  if (!known_type(dout_type) || !known_type(dtable_type) || !isfinite(scale) || (accumulate != 0 && dtable_type != MOSAIC_F32))
+    return MOSAIC_ERR_INVALID_ARG;
+  MOSAIC_RETURN_IF(check_sizes(T, d, MOSAIC_MAX_ROW));
+  MOSAIC_RETURN_IF(check_vocab(V));
+  MOSAIC_RETURN_IF(check_matrix(dtable, ld_dtable, d));
+  if (T > 0) {
+    if (bad_list(tokens, count)) return MOSAIC_ERR_INVALID_ARG;
+    MOSAIC_RETURN_IF(check_matrix(dout, ld_dout, d));
+    if (workspace == nullptr || misaligned(workspace)) return MOSAIC_ERR_INVALID_ARG;
+    if (workspace_bytes < mosaic_embedding_backward_workspace_bytes(T, d, V)) return MOSAIC_ERR_WORKSPACE_TOO_SMALL;
+  } else if (accumulate != 0) {
+    return MOSAIC_OK;
+  }
+  hipStream_t on = static_cast<hipStream_t>(stream);
+  mosaic::TokenSumArgs a = {};
+  if (T > 0 && mosaic::launch_sort_tokens(tokens, T, count, V, workspace, &a.sorted, on) != 0) return MOSAIC_ERR_HIP;
+  a.rows = dout;
+  a.partials = T > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + embedding_space(T, d, V).partials) : nullptr;
+  a.sums = dtable;
+  a.n = T;
+  a.ld_rows = ld_dout;
+  a.ld_sums = ld_dtable;
+  a.V = V;
+  a.d = d;
+  a.accumulate = accumulate != 0;
+  a.scale = scale;
+  return launched(mosaic::launch_token_sums(a, dout_type == MOSAIC_F32, dtable_type == MOSAIC_F32, on));
+}
+
+int mosaic_dropout_forward(const void* x, int64_t ld_x, const void* residual, int32_t stream_type, int64_t ld_residual,
+                           int64_t T, int32_t d, float p, uint64_t seed, int32_t site, int64_t first_row, void* out,
+                           int64_t ld_out, void* stream) {
+  MOSAIC_RETURN_IF(check_dropout(stream_type, T, d, p, site, first_row));
+  if (T == 0) return MOSAIC_OK;
+  MOSAIC_RETURN_IF(check_matrix(x, ld_x, d));
+  MOSAIC_RETURN_IF(check_optional(residual, ld_residual, d));
+  MOSAIC_RETURN_IF(check_matrix(out, ld_out, d));
+  mosaic::DropoutArgs a = dropout_args(T, d, p, seed, site, first_row);
+  a.x = x;
+  a.residual = residual;
+  a.out = out;
+  a.ld_x = ld_x;
+  a.ld_residual = ld_residual;
+  a.ld_out = ld_out;
+  return launched(mosaic::launch_dropout(a, false, stream_type == MOSAIC_F32, static_cast<hipStream_t>(stream)));
+}
+
+int mosaic_dropout_backward(const void* dout, int32_t stream_type, int64_t ld_dout, int64_t T, int32_t d, float p,
+                            uint64_t seed, int32_t site, int64_t first_row, void* dx, int64_t ld_dx, void* stream) {
+  MOSAIC_RETURN_IF(check_dropout(stream_type, T, d, p, site, first_row));
+  if (T == 0) return MOSAIC_OK;
+  MOSAIC_RETURN_IF(check_matrix(dout, ld_dout, d));
+  MOSAIC_RETURN_IF(check_matrix(dx, ld_dx, d));
+  mosaic::DropoutArgs a = dropout_args(T, d, p, seed, site, first_row);
+  a.x = dout;
+  a.out = dx;
+  a.ld_x = ld_dout;
+  a.ld_out = ld_dx;
+  return launched(mosaic::launch_dropout(a, stream_type == MOSAIC_F32, false, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,61 @@
+// Internal declarations of the token operators (mosaic_tokens.h): argument blocks, launchers, layouts of workspaces.
+#ifndef MOSAIC_TOKENS_INTERNAL_H_
+#define MOSAIC_TOKENS_INTERNAL_H_
+
+#include "mosaic_layer_internal.h"
+#include "mosaic_tokens.h"
+
+namespace mosaic {
+
+// ---- embedding lookup (mosaic_embed.hip)
+struct EmbedArgs {
+  const int32_t* tokens;
+  const int32_t* count;   // or nullptr
+  const void* table;
+  void* out;
+  int64_t T, ld_table, ld_out;   // strides in elements
+  int32_t V, d;
+  float scale;
+};
+int launch_embedding_forward(const EmbedArgs& a, bool table_f32, bool out_f32, hipStream_t stream);
+
+// Positions sorted by their tokens: keys ascending, positions of a key ascending; what is left out has the key V and comes last.
+struct SortedTokens {
+  int32_t* keys;       // [n]
+  int32_t* at;         // [n]
+  uint32_t* present;   // a bit for each of V ids: some token names it
+};
+// Bytes that sorting n tokens of V takes, and where in them the results are.
+int64_t sort_tokens_bytes(int64_t n, int32_t V);
+int launch_sort_tokens(const int32_t* tokens, int64_t n, const int32_t* count, int32_t V, void* space, SortedTokens* out,
+                       hipStream_t stream);
+
+// Sums of rows by token, over sorted positions.
+struct TokenSumArgs {
+  SortedTokens sorted;
+  const void* rows;      // [n, ld_rows]
+  const float* weights;  // a factor for each row, or nullptr
+  float* partials;       // [token_sum_partials(n), d]
+  void* sums;            // of token v: row v; compact: row first[v], the place of its first position
+  int32_t* first;        // compact: [V], -1 where no token names v; else nullptr
+  int64_t n, ld_rows, ld_sums;
+  int32_t V, d, accumulate;
+  float scale;
+};
+int64_t token_sum_partials(int64_t n);
+int launch_token_sums(const TokenSumArgs& a, bool rows_f32, bool sums_f32, hipStream_t stream);
+
+// ---- dropout (mosaic_embed.hip)
+struct DropoutArgs {
+  const void* x;
+  const void* residual;   // of out's type, or nullptr
+  void* out;
+  int64_t T, ld_x, ld_residual, ld_out, first_row;
+  int32_t d;
+  uint32_t border, key_low, key_high, site;
+  float grow;
+};
+int launch_dropout(const DropoutArgs& a, bool x_f32, bool out_f32, hipStream_t stream);
+
+}  // namespace mosaic
+#endif
