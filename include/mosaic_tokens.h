@@ -83,6 +83,35 @@ int mosaic_dropout_forward(const void *x, int64_t ld_x, const void *residual, in
 int mosaic_dropout_backward(const void *dout, int32_t stream_type, int64_t ld_dout, int64_t T, int32_t d, float p,
                             uint64_t seed, int32_t site, int64_t first_row, void *dx, int64_t ld_dx, void *stream);
 
+/*
+ * Log probabilities of given tokens at listed rows, with the entropy of a row's distribution and its most probable
+ * alternatives; no logits are written.  For every j < M = min(*count, max_rows), with h = hidden[idx[j]]:
+ *   x[v]           = sum_k h[k] * w[v, k]              bf16 x bf16, 32-bit sums, no bias
+ *   out_lse[j]     = log sum_v exp(x[v])
+ *   out_logprob[j] = x[targets[j]] - out_lse[j];  0 where targets[j] lies outside [0, V) (a row without a target)
+ *   out_entropy[j] = - sum_v p[v] log p[v],  p[v] = exp(x[v] - out_lse[j])
+ *   top_id[j, i], top_logprob[j, i], i < n_top:  the ids with the largest logits, the lower id first among equals, and
+ *                    x[id] - out_lse[j];  -1 and -infinity past the vocabulary
+ *   hidden     bf16 [T, d];  w: bf16 [V, d]
+ *   idx, count dev int32, as mosaic_mask_compact makes them, or both NULL for all rows (then max_rows = T).  Rows may be listed
+ *              in any order and more than once; an entry outside [0, T) is clamped to it
+ *   max_rows   bound on *count, at most 2^31 - 1.  What the call takes follows from the rows found; its workspace from the bound
+ *   targets    dev int32[max_rows], of the listed rows in their order; needed for out_logprob alone
+ *   out_*      dev float[max_rows], each may be NULL, not all of them with n_top = 0; entries from M on are left as they were
+ *   n_top      0 .. MOSAIC_MAX_TOP;  top_id int32 and top_logprob float [max_rows, n_top], dense, NULL where it is 0
+ *   workspace  dev, 16-byte aligned, mosaic_masked_logprobs_workspace_bytes bytes: sums of the vocabulary's parts, with
+ *              alternatives their candidates (38 to 151 MB), and, where the hidden states pass 2 GiB, the listed rows side by side
+ * A NaN among a row's logits makes that row's log probabilities, entropy and log-sum-exp NaN and its alternatives unspecified
+ * (ids in [-1, V)); other rows are not affected.
+ * How the vocabulary is parted follows from the rows found: a row's last bits may depend on their number.
+ */
+#define MOSAIC_MAX_TOP 16
+int64_t mosaic_masked_logprobs_workspace_bytes(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, int32_t n_top);
+int mosaic_masked_logprobs(const void *hidden, int64_t ld_h, int64_t T, int32_t d, const void *w, int64_t ld_w, int32_t V,
+                           const int32_t *idx, const int32_t *count, int64_t max_rows, const int32_t *targets,
+                           float *out_logprob, float *out_entropy, float *out_lse, int32_t n_top, int32_t *top_id,
+                           float *top_logprob, void *workspace, int64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

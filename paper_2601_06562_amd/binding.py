@@ -45,8 +45,9 @@ LAYER_EXPORTS = (   # include/mosaic_layer.h
 )
 TOKEN_EXPORTS = (   # include/mosaic_tokens.h
     "mosaic_embedding_forward", "mosaic_embedding_backward_workspace_bytes", "mosaic_embedding_backward",
-    "mosaic_dropout_forward", "mosaic_dropout_backward",
+    "mosaic_dropout_forward", "mosaic_dropout_backward", "mosaic_masked_logprobs_workspace_bytes", "mosaic_masked_logprobs",
 )
+MAX_TOP = 16                         # alternatives a row that mosaic_masked_logprobs gives at most
 BF16, F32 = 0, 1                     # mosaic_type
 INT8, E4M3 = 0, 1                    # mosaic_q8_format
 ACT_SILU, ACT_GELU_TANH = 0, 1       # mosaic_activation
@@ -589,6 +590,10 @@ def _tokens():
         L.mosaic_dropout_forward.argtypes = [p, i64, p, i32, i64, i64, i32, f32, u64, i32, i64, p, i64, p]
         L.mosaic_dropout_backward.restype = ctypes.c_int
         L.mosaic_dropout_backward.argtypes = [p, i32, i64, i64, i32, f32, u64, i32, i64, p, i64, p]
+        L.mosaic_masked_logprobs_workspace_bytes.restype = i64
+        L.mosaic_masked_logprobs_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32]
+        L.mosaic_masked_logprobs.restype = ctypes.c_int
+        L.mosaic_masked_logprobs.argtypes = [p, i64, i64, i32, p, i64, i32, p, p, i64, p, p, p, p, i32, p, p, p, i64, p]
         _token_lib = L
     return _token_lib
 
@@ -650,6 +655,52 @@ def mosaic_dropout_backward(dout, dx, p, seed, site=0, first_row=0, stream=None)
     _check(_tokens().mosaic_dropout_backward(p_g, _type_of(dout, "dout"), ld_g, T, d, float(p),
                                              int(seed) & 0xFFFFFFFFFFFFFFFF, int(site), int(first_row), p_x, ld_x,
                                              _stream_ptr(stream)), "mosaic_dropout_backward")
+
+
+def _list_args(hidden, w, idx, count, max_rows):
+    """(hidden pointer, ld_h, T, d, w pointer, ld_w, V, idx pointer, count pointer) of a pass over listed rows."""
+    (T, d), V = hidden.shape, w.shape[0]
+    p_h, ld_h = _rows(hidden, "hidden", T, d, torch.bfloat16)
+    p_w, ld_w = _rows(w, "w", V, d, torch.bfloat16)
+    if (idx is None) != (count is None):
+        raise ValueError("idx and count go together")
+    if idx is not None and idx.numel() < max_rows:
+        raise ValueError("idx holds fewer than max_rows entries")
+    return p_h, ld_h, T, d, p_w, ld_w, V, _dev_ptr(idx, "idx", torch.int32), _count_ptr(count)
+
+
+def _per_row(t, name, max_rows, dtype=torch.float32):
+    """The address of a dense tensor with an element for each of max_rows rows, 0 for None."""
+    if t is not None and t.numel() < max_rows:
+        raise ValueError(f"{name} holds fewer than max_rows elements")
+    return _dev_ptr(t, name, dtype)
+
+
+def mosaic_masked_logprobs_workspace_bytes(T, max_rows, d, V, n_top=0, ld_h=None) -> int:
+    """ld_h: the hidden states' row stride in elements (default: d)."""
+    return int(_tokens().mosaic_masked_logprobs_workspace_bytes(T, d if ld_h is None else ld_h, max_rows, d, V, n_top))
+
+
+def mosaic_masked_logprobs(hidden, w, idx, count, max_rows, targets, out_logprob, out_entropy, out_lse, workspace, top_id=None,
+                           top_logprob=None, stream=None):
+    """Log probabilities of targets[j] at hidden[idx[j]], the rows' entropies and log-sum-exps (float32, None where not wanted),
+    and the n_top most probable ids with theirs (top_id int32 and top_logprob float32 [max_rows, n_top], or None).  hidden
+    bf16 [T, d], w bf16 [V, d], targets int32 (outside [0, V): none); idx, count as mosaic_mask_compact makes them, or None
+    for all rows."""
+    p_h, ld_h, T, d, p_w, ld_w, V, p_idx, p_count = _list_args(hidden, w, idx, count, max_rows)
+    if (top_id is None) != (top_logprob is None):
+        raise ValueError("top_id and top_logprob go together")
+    n_top = 0
+    if top_id is not None:
+        n_top = top_id.shape[1]
+        if top_id.shape != top_logprob.shape or top_id.shape[0] < max_rows:
+            raise ValueError("top_id and top_logprob must both be [max_rows, n_top]")
+    _check(_tokens().mosaic_masked_logprobs(
+        p_h, ld_h, T, d, p_w, ld_w, V, p_idx, p_count, max_rows, _per_row(targets, "targets", max_rows, torch.int32),
+        _per_row(out_logprob, "out_logprob", max_rows), _per_row(out_entropy, "out_entropy", max_rows),
+        _per_row(out_lse, "out_lse", max_rows), n_top, _dev_ptr(top_id, "top_id", torch.int32),
+        _dev_ptr(top_logprob, "top_logprob", torch.float32), *_workspace_args(workspace), _stream_ptr(stream)),
+        "mosaic_masked_logprobs")
 
 
 class VmmWorkspace:

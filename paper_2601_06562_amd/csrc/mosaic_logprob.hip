@@ -1,0 +1,732 @@
+// Log probabilities of given tokens at listed rows, with entropy and the most probable alternatives, and their gradients: the
+// logits of a tile are made on the matrix cores, worked on in the accumulators, and never written.
+//
+// A tile is 256 vocabulary ids ("P", the weights' rows) by 64, 128 or 256 listed rows ("Q", gathered as they are copied), K in
+// steps of 64 through rings of slots in LDS.  A unit is a tile of rows and a part of the vocabulary, whose tiles a block takes one
+// after another; the state of a row is held between them.
+#include <hip/hip_runtime.h>
+#include <limits.h>
+#include <stdint.h>
+
+#include "mosaic_tile.h"
+#include "mosaic_tokens_internal.h"
+
+namespace mosaic {
+namespace {
+
+using namespace tile;
+
+constexpr int kCus = 256;
+constexpr int kVocab = 256;            // ids of a tile
+constexpr int kHalf = kVocab / 2;      // ids of a wave's half
+constexpr int kMostSplits = 256;       // parts of the vocabulary
+constexpr int kMostUnits = 512;        // units, where there is more than one part
+constexpr float kNeg = -0x1p100f;      // "minus infinity" that survives subtraction
+constexpr float kLog2e = 1.4426950408889634f;
+// A wave's list of candidates for a row's alternatives: what a compression leaves, and all that one tile can add.
+constexpr int kMostTop = MOSAIC_MAX_TOP;
+constexpr int kListRoom = kHalf + kMostTop;
+
+struct Candidate { float x; int32_t id; };
+
+struct LogitParams {
+  const char* w;
+  const char* x;
+  int64_t ld_w, ld_x;        // bytes
+  const int32_t* idx;        // or nullptr: x holds the listed rows side by side
+  const int32_t* count;      // or nullptr
+  const int32_t* targets;    // or nullptr
+  int32_t T, max_rows, V, d, n_top;
+  // statistics: of the halves of every part of the vocabulary, rows side by side
+  float *part_m, *part_s, *part_t;
+  Candidate* part_top;       // n_top each
+  float* target_logit;       // [max_rows]
+  Candidate* lists;          // of every block's waves and rows, kListRoom each
+};
+
+__device__ __forceinline__ int rows_found(const LogitParams& p) {
+  if (p.count == nullptr) return p.max_rows;
+  const int n = *p.count;
+  return n < 0 ? 0 : n < p.max_rows ? n : p.max_rows;
+}
+
+// Rows of a tile for so many rows, by what a step of 64 k takes: 256 rows 1.50 us, 128 rows 0.92.
+__host__ __device__ inline int tile_rows(int64_t rows) {
+  if (rows <= 64) return 64;
+  if (rows <= 128) return 128;
+  return 92 * ((rows + 127) / 128) < 150 * ((rows + 255) / 256) ? 128 : 256;
+}
+
+// Into how many parts the vocabulary's tiles go: the least time of the longest block, a unit costing about two tiles' steps of
+// 64 k more than its tiles.  One lane tries every 64th count.
+__device__ __forceinline__ int choose_parts(int row_tiles, int vocab_tiles, int steps) {
+  const int lane = threadIdx.x & 63;
+  uint32_t best = 0xffffffffu;
+  for (int s = lane + 1; s <= kMostSplits; s += 64) {
+    if (s > vocab_tiles || (s > 1 && row_tiles * s > kMostUnits)) break;
+    const uint32_t rounds = (uint32_t)(row_tiles * s + kCus - 1) / kCus, longest = (uint32_t)(vocab_tiles + s - 1) / s;
+    const uint64_t cost = (uint64_t)rounds * ((uint64_t)longest * steps + 2);
+    const uint32_t c = (uint32_t)(cost < 0x7fffff ? cost : 0x7fffff) << 9 | s;   // equal costs: the fewest parts
+    best = c < best ? c : best;
+  }
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)best, x, 64);
+    best = o < best ? o : best;
+  }
+  return __builtin_amdgcn_readfirstlane((int)(best & 511));
+}
+
+// Copies of rows along K: 8 rows of 128 bytes a copy and wave, pieces at piece ^ (row / 2 % 8).
+template <int N>
+struct RowCopier {
+  uint32_t offset[N];
+  uint32_t past;   // bit i: this lane's piece of copy i lies past the end of K in the last step, where K is no multiple of 64
+
+  static __device__ __forceinline__ int row_of(int wave, int lane, int i) { return (wave * N + i) * 8 + (lane >> 3); }
+  // Row `row` of the tile lies `bytes` from the base, or nowhere.
+  __device__ __forceinline__ void place(int i, int lane, int row, bool there, uint32_t bytes, int tail) {
+    const int k = ((lane & 7) ^ (row >> 1 & 7)) * 8;
+    offset[i] = there ? bytes + k * 2 : kOutside;
+    past = (past & ~(1u << i)) | (there && tail != 0 && k >= tail ? 1u : 0u) << i;
+  }
+  __device__ __forceinline__ void flip() {   // into the last step, or out of it
+#pragma unroll
+    for (int i = 0; i < N; ++i) offset[i] ^= (past >> i & 1) << 31;
+  }
+  __device__ __forceinline__ void one(int i, u32x4_t r, uint32_t to, int wave) const {
+    const uint32_t m0 = __builtin_amdgcn_readfirstlane((int)(to + (wave * N + i) * 1024));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m0), "v"(offset[i]), "s"(r));
+  }
+};
+
+// Over the four lanes that hold one row (16 apart).
+__device__ __forceinline__ float row_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float row_min(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float y = fminf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return fminf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float y = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// The largest number below x (of those that are no denormals).
+__device__ __forceinline__ float below(float x) {
+  const int b = __float_as_int(x);
+  if (__builtin_fabsf(x) < 0x1p-125f) return -0x1p-125f;
+  return __int_as_float(b > 0 ? b - 1 : b + 1);
+}
+
+// What a lane holds between tiles, of one row of its wave: of column block g = lane / 16 (with QB column blocks, g % QB).
+//   m, s, t   the largest logit, sum e^(x - m), sum (x - m) e^(x - m)
+//   tau       ids of later tiles with a logit of tau or less are none of the n_top best of this half
+//   n         candidates in the list
+struct RowState { float m, s, t, tau; int n; };
+
+// Sorts a row's candidates and keeps the n best, in `to`: by logit, then by id.  A lane takes a row.
+template <int N>
+__device__ __forceinline__ void keep_best(RowState& st, const Candidate* list, Candidate* to, int n) {
+  float x[N];
+  int id[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) { x[k] = -__builtin_inff(); id[k] = INT_MAX; }
+  for (int e = 0; e < st.n; e += 4) {
+    Candidate c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = list[e + i < st.n ? e + i : e];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float cx = e + i < st.n ? c[i].x : -__builtin_inff();
+      int ci = e + i < st.n ? c[i].id : INT_MAX;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const bool first = cx > x[k] || (cx == x[k] && ci < id[k]);
+        const float ox = x[k];
+        const int oi = id[k];
+        x[k] = first ? cx : ox;
+        id[k] = first ? ci : oi;
+        cx = first ? ox : cx;
+        ci = first ? oi : ci;
+      }
+    }
+  }
+  float last = kNeg;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    if (k < n) {
+      to[k] = Candidate{x[k], id[k]};
+      last = x[k];
+    }
+  }
+  if (st.n >= n) {
+    st.n = n;
+    st.tau = fmaxf(last, kNeg);
+  }
+}
+
+// Reduces a finished tile into the rows' states.  v0: the id of this lane's first accumulator; row0: the first row of column
+// block 0 of its wave.
+template <int QB>
+__device__ __forceinline__ void reduce_tile(const LogitParams& p, f32x4_t (&acc)[8][QB], RowState& st, int64_t v0, int row0, int rows,
+                                            bool ragged, Candidate* lists) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, mine = g % QB;
+  int target[QB];
+#pragma unroll
+  for (int j = 0; j < QB; ++j) {
+    const int row = row0 + 16 * j + l16;
+    target[j] = p.targets != nullptr && row < rows ? p.targets[row] : -1;
+  }
+  if (ragged) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < QB; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (v0 + 16 * i + r >= p.V) acc[i][j][r] = kNeg;
+  }
+  float own_m = 0.f, own_s = 0.f, own_t = 0.f;
+#pragma unroll
+  for (int j = 0; j < QB; ++j) {
+    float most[4];   // of quarters of the lane's ids
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float m = fmaxf(acc[2 * k][j][0], acc[2 * k + 1][j][0]);
+#pragma unroll
+      for (int r = 1; r < 4; ++r) m = fmaxf(fmaxf(m, acc[2 * k][j][r]), acc[2 * k + 1][j][r]);
+      most[k] = m;
+    }
+    const float lane_m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+    const float m = row_max(lane_m);
+    float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        const float u0 = acc[i][j][r] - m, u1 = acc[i][j][r + 1] - m;
+        const float e0 = __builtin_amdgcn_exp2f(u0 * kLog2e), e1 = __builtin_amdgcn_exp2f(u1 * kLog2e);
+        s0 += e0;
+        s1 += e1;
+        t0 = __builtin_fmaf(u0, e0, t0);
+        t1 = __builtin_fmaf(u1, e1, t1);
+      }
+    }
+    const float s = row_sum(s0 + s1), t = row_sum(t0 + t1);
+    own_m = mine == j ? m : own_m;
+    own_s = mine == j ? s : own_s;
+    own_t = mine == j ? t : own_t;
+
+    // the target's logit, in the one lane that holds it
+    const int64_t rel64 = target[j] - v0;
+    const bool here = target[j] >= 0 && target[j] < p.V && rel64 >= 0 && rel64 < kHalf && (rel64 & 15) < 4;
+    if (__any(here)) {
+      const int rel = here ? (int)rel64 : -1;
+      float x = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x = rel == 16 * i + r ? acc[i][j][r] : x;
+      if (here) p.target_logit[row0 + 16 * j + l16] = x;
+    }
+
+    if (p.n_top > 0) {
+      // Of n_top sets of ids the least of the sets' largest is no more than the n_top-th largest of all: 4, 8 or 16 sets.
+      float bound = lane_m;
+      if (p.n_top > 4) bound = fminf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+      if (p.n_top > 8) bound = fminf(fminf(most[0], most[1]), fminf(most[2], most[3]));
+      bound = row_min(bound);
+      const int from = 16 * j + l16;
+      float tau = fmaxf(__shfl(st.tau, from, 64), below(fmaxf(bound, kNeg)));
+      tau = row0 + from < rows ? fmaxf(tau, kNeg) : __builtin_inff();
+      int n = __shfl(st.n, from, 64);
+      if (__any(lane_m > tau)) {
+        Candidate* list = lists + from * kListRoom;
+        const uint64_t of_row = (uint64_t)0x0001000100010001 << l16, lower = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float most4 = fmaxf(fmaxf(acc[i][j][0], acc[i][j][1]), fmaxf(acc[i][j][2], acc[i][j][3]));
+          if (__any(most4 > tau)) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const bool hit = acc[i][j][r] > tau;
+              const uint64_t hits = __ballot(hit) & of_row;
+              const int at = n + __popcll(hits & lower);
+              if (hit && at < kListRoom) list[at] = Candidate{acc[i][j][r], (int32_t)(v0 + 16 * i + r)};
+              n += __popcll(hits);
+            }
+          }
+        }
+      }
+      st.n = mine == j ? n : st.n;
+    }
+  }
+  const float m = fmaxf(st.m, own_m);
+  const float a = __builtin_amdgcn_exp2f((st.m - m) * kLog2e), b = __builtin_amdgcn_exp2f((own_m - m) * kLog2e);
+  st.t = a * (st.t + st.s * (st.m - m)) + b * (own_t + own_s * (own_m - m));
+  st.s = a * st.s + b * own_s;
+  st.m = m;
+}
+
+// All units of this block, in tiles of TQ rows.
+template <int TQ, int SP, int SQ>
+__device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int rows) {
+  constexpr int QB = TQ / 64, kBytesP = kVocab * kTileK * 2, kBytesQ = TQ * kTileK * 2;
+  constexpr int kCopiesP = 4, kCopiesQ = QB, kBlocksP = 8;
+  constexpr bool kSplit = SP != SQ;
+  static_assert(!kSplit || SP == SQ + 1, "the waits of the loop");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wp = wave >> 2, wq = wave & 3;
+  const int steps = (p.d + kTileK - 1) / kTileK, tail = p.d % kTileK;
+  const int row_tiles = (rows + TQ - 1) / TQ, vocab_tiles = (int)(((int64_t)p.V + kVocab - 1) / kVocab);
+  const int parts = choose_parts(row_tiles, vocab_tiles, steps);
+
+  // Block b runs on XCD b % 8; every XCD gets a run of units, and within it panels of row tiles, so that what is in flight
+  // behind one L2 shares weights and rows.
+  const int n = row_tiles * parts, blocks = (int)gridDim.x, xcd = (int)blockIdx.x % kXcds;
+  const int stride = blocks / kXcds + (xcd < blocks % kXcds ? 1 : 0);
+  int unit = xcd * (n / kXcds) + (xcd < n % kXcds ? xcd : n % kXcds);
+  const int end = unit + n / kXcds + (xcd < n % kXcds ? 1 : 0);
+  unit += (int)blockIdx.x / kXcds;
+  if (unit >= end) return;
+  const int panel = row_tiles < 8 ? row_tiles : 8;
+
+  Candidate* const lists = p.lists == nullptr ? nullptr : p.lists + ((int64_t)blockIdx.x * 8 + wave) * (16 * QB) * kListRoom;
+
+  // Of the tile whose copies are issued.
+  int part = 0, row0 = 0, vt = 0, vt_end = 0, turned = 0;
+  RowCopier<kCopiesP> cp;
+  RowCopier<kCopiesQ> cq;
+  cp.past = cq.past = 0;
+  const char* q_base = p.x;
+  // Where an operand's copies come from: K goes round from step `turned` on; steps past the last bring zeros.
+  struct Walk { u32x4_t from; int k, left; };
+  Walk wp_, wq_;
+  auto start_unit = [&]() __attribute__((always_inline)) {
+    const int per_panel = panel * parts, pn = unit / per_panel, in = unit - pn * per_panel;
+    const int deep = row_tiles - pn * panel < panel ? row_tiles - pn * panel : panel;
+    part = in / deep;
+    row0 = (pn * panel + in % deep) * TQ;
+    vt = (int)((int64_t)vocab_tiles * part / parts);
+    vt_end = (int)((int64_t)vocab_tiles * (part + 1) / parts);
+    if (p.idx == nullptr) q_base = p.x + (int64_t)row0 * p.ld_x;
+#pragma unroll
+    for (int i = 0; i < kCopiesQ; ++i) {
+      const int row = RowCopier<kCopiesQ>::row_of(wave, lane, i);
+      const bool there = row0 + row < rows;
+      uint32_t bytes = (uint32_t)row * (uint32_t)p.ld_x;
+      if (p.idx != nullptr && there) {
+        int t = p.idx[row0 + row];
+        t = t < 0 ? 0 : (t > p.T - 1 ? p.T - 1 : t);   // a bad entry of a caller's list reads a valid row
+        bytes = (uint32_t)t * (uint32_t)p.ld_x;
+      }
+      cq.place(i, lane, row, there, bytes, tail);
+    }
+  };
+  const char* p_base = p.w;
+  auto start_tile = [&]() __attribute__((always_inline)) {
+    const int64_t v = (int64_t)vt * kVocab;
+    p_base = p.w + v * p.ld_w;
+#pragma unroll
+    for (int i = 0; i < kCopiesP; ++i) {
+      const int row = RowCopier<kCopiesP>::row_of(wave, lane, i);
+      cp.place(i, lane, row, v + row < p.V, (uint32_t)row * (uint32_t)p.ld_w, tail);
+    }
+    turned = row_tiles == 1 ? vt % steps : 0;   // with one tile of rows blocks begin at different places of K
+  };
+  auto first = [&](Walk& w, const char* base, auto& c) __attribute__((always_inline)) {
+    w.k = turned;
+    w.left = steps;
+    w.from = buffer_from(base + (int64_t)turned * (kTileK * 2), kOutside);
+    if (tail != 0 && w.k == steps - 1) c.flip();
+  };
+  auto next = [&](Walk& w, auto& c) __attribute__((always_inline)) {
+    if (--w.left <= 0) {
+      if (w.left == 0 && tail != 0 && w.k == steps - 1) c.flip();
+      w.from[2] = 0;
+      return;
+    }
+    const bool wrap = w.k + 1 == steps;
+    if (tail != 0 && (wrap || w.k + 2 == steps)) c.flip();   // out of the last step, or into it
+    const int64_t by = wrap ? -(int64_t)(steps - 1) * (kTileK * 2) : kTileK * 2;
+    const uint64_t b = ((uint64_t)w.from[1] << 32 | w.from[0]) + (uint64_t)by;
+    w.from[0] = (uint32_t)b;
+    w.from[1] = (uint32_t)(b >> 32);
+    w.k = wrap ? 0 : w.k + 1;
+  };
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
+  const uint32_t ring_p = lds0, ring_q = lds0 + SP * kBytesP;
+  auto copy_p = [&](uint32_t to, int c) __attribute__((always_inline)) { cp.one(c, wp_.from, to, wave); };
+  auto copy_q = [&](uint32_t to, int c) __attribute__((always_inline)) { cq.one(c, wq_.from, to, wave); };
+  Reader<kVocab, false> rp;
+  Reader<TQ, false> rq;
+  rp.place(ring_p, wp * kHalf, lane);
+  rq.place(ring_q, wq * 16 * QB, lane);
+
+  f32x4_t acc[kBlocksP][QB];
+  struct Half { bf16x8_t p[kBlocksP], q[QB]; };
+  constexpr int kReads = kBlocksP + QB;
+  auto read = [&](Half& h, int kk, int c) __attribute__((always_inline)) {
+    if (c < QB) h.q[c] = rq.get(c, kk);
+    else h.p[c - QB] = rp.get(c - QB, kk);
+  };
+  // The largest tile takes both halves of K of a block back to back, which draws less power.
+  constexpr bool kPaired = TQ == 256;
+  static_assert(!kPaired || (kSplit && SQ == 2), "the copies of a step");
+  bf16x8_t fq[2 * QB], fp[2][2][2];
+  auto read_pair = [&](int i, int c) __attribute__((always_inline)) { fp[i / 2 % 2][c / 2][c % 2] = rp.get((i + c / 2) % kBlocksP, c % 2); };
+  struct Copies { int p, q; uint32_t to_p, to_q; };
+  auto half_step = [&](const Half& use, Half& fill, int kk, const Copies& n) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kBlocksP; ++i) {
+#pragma unroll
+      for (int m = 0; m < QB; ++m) {
+        const int j = i & 1 ? QB - 1 - m : m;
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(use.p[i], use.q[j], acc[i][j], 0, 0, 0);
+      }
+#pragma unroll
+      for (int c = kReads * i / (kBlocksP - 1); c < kReads * (i + 1) / (kBlocksP - 1) && c < kReads; ++c) read(fill, kk, c);
+#pragma unroll
+      for (int c = (n.p + n.q) * i / kBlocksP; c < (n.p + n.q) * (i + 1) / kBlocksP; ++c) {
+        if (c < n.p) copy_p(n.to_p, c);
+        else copy_q(n.to_q, c - n.p);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  uint32_t slot_p = ring_p, slot_q = ring_q;   // of the step being multiplied
+  auto next_p = [&](uint32_t s) __attribute__((always_inline)) { return s == ring_p + (SP - 1) * kBytesP ? ring_p : s + kBytesP; };
+  auto next_q = [&](uint32_t s) __attribute__((always_inline)) { return s == ring_q + (SQ - 1) * kBytesQ ? ring_q : s + kBytesQ; };
+  auto last_p = [&]() __attribute__((always_inline)) { return slot_p == ring_p ? ring_p + (SP - 1) * kBytesP : slot_p - kBytesP; };
+  // The meeting of a step: its slots have been read by this wave, and its copies for the next have arrived; so, then, for all waves.
+  auto meet = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((SP - 2) * kCopiesP + (SQ - 2) * kCopiesQ) : "memory");
+    const uint32_t to_p = next_p(slot_p), to_q = next_q(slot_q);
+    rp.move((int)(to_p - slot_p));
+    rq.move((int)(to_q - slot_q));
+    slot_p = to_p;
+    slot_q = to_q;
+  };
+
+  RowState st = {kNeg, 0.f, 0.f, kNeg, 0};
+  int done_vt = -1, done_row0 = 0, done_part = 0, done_tiles = 0;   // the tile whose logits are in the accumulators
+  bool done_last = false, fresh = true;                              // the last of its unit; fresh: a unit is to be begun
+  for (;;) {
+    const bool more = unit < end;
+    if (more) {
+      if (fresh) start_unit();
+      start_tile();
+      uint32_t to_p = slot_p, to_q = slot_q;
+#pragma unroll
+      for (int s = 0; s < SQ; ++s) {
+        if (s < SP - (kSplit ? 1 : 0)) {
+          if (s == 0) first(wp_, p_base, cp);
+          else next(wp_, cp);
+#pragma unroll
+          for (int c = 0; c < kCopiesP; ++c) copy_p(to_p, c);
+          to_p = next_p(to_p);
+        }
+        if (s == 0) first(wq_, q_base, cq);
+        else next(wq_, cq);
+#pragma unroll
+        for (int c = 0; c < kCopiesQ; ++c) copy_q(to_q, c);
+        to_q = next_q(to_q);
+      }
+    }
+    if (done_vt >= 0) {
+      const int64_t v = (int64_t)done_vt * kVocab;
+      const int q0 = done_row0 + wq * 16 * QB, g = lane >> 4;
+      reduce_tile<QB>(p, acc, st, v + wp * kHalf + 4 * g, q0, rows, v + kVocab > p.V, lists);
+      ++done_tiles;
+      const int64_t row = q0 + 16 * g + (lane & 15), of_half = 2 * done_part + wp;
+      const bool owner = g < QB && row < rows;
+      if (p.n_top > 0) {
+        const bool now = done_last || (done_tiles & (done_tiles - 1)) == 0 || __any(owner && st.n > kListRoom - kHalf);
+        if (now) {
+          __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // the list's entries were stored by other lanes
+          if (owner) {
+            Candidate* list = lists + (16 * g + (lane & 15)) * kListRoom;
+            Candidate* to = done_last ? p.part_top + (of_half * rows + row) * p.n_top : list;
+            if (p.n_top <= 4) keep_best<4>(st, list, to, p.n_top);
+            else if (p.n_top <= 8) keep_best<8>(st, list, to, p.n_top);
+            else keep_best<16>(st, list, to, p.n_top);
+          }
+          __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");
+        }
+      }
+      if (done_last) {
+        if (owner) {
+          p.part_m[of_half * rows + row] = st.m;
+          p.part_s[of_half * rows + row] = st.s;
+          p.part_t[of_half * rows + row] = st.t;
+        }
+        st = RowState{kNeg, 0.f, 0.f, kNeg, 0};
+        done_tiles = 0;
+      }
+    }
+    if (!more) break;
+    // The first slots; with the last tile's stores behind them no count tells them from the others.
+    constexpr int kLater = (SP - (kSplit ? 2 : 1)) * kCopiesP + (SQ - 1) * kCopiesQ;
+    if (done_vt < 0) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLater) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < kBlocksP; ++i)
+#pragma unroll
+      for (int j = 0; j < QB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if constexpr (kPaired) {
+#pragma unroll
+      for (int c = 0; c < 2 * QB; ++c) fq[c] = rq.get(c % QB, c / QB);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) read_pair(0, c);
+      for (int step = 0; step < steps; ++step) {
+        const uint32_t free_p = last_p(), free_q = slot_q;
+        next(wp_, cp);
+#pragma unroll
+        for (int i = 0; i < kBlocksP; i += 2) {
+#pragma unroll
+          for (int j = 0; j < QB; ++j) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+              for (int kk = 0; kk < 2; ++kk) {
+                f32x4_t& sum = acc[i + b][j];
+                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[i / 2 % 2][b][kk], fq[kk * QB + j], sum, 0, 0, 0);
+              }
+            }
+            if (j < 2) {
+              read_pair(i + 2, 2 * j);
+              read_pair(i + 2, 2 * j + 1);
+            }
+            if (i == kBlocksP - 4 && j == 2) {   // all of this step has been read
+              meet();
+              next(wq_, cq);
+            }
+            if (i == kBlocksP - 2) {   // the next step's, as this one's last products go
+              fq[j] = rq.get(j, 0);
+              fq[QB + j] = rq.get(j, 1);
+            }
+            const int at = i / 2 * QB + j, from_q = (kBlocksP / 2 - 1) * QB - 1;   // P's copies before the meeting, Q's behind it
+            if (at < 2 * kCopiesP && at % 2 == 1) copy_p(free_p, at / 2);
+            if (at >= from_q && at - from_q < kCopiesQ) copy_q(free_q, at - from_q);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+    } else {
+      Half h0, h1;
+#pragma unroll
+      for (int c = 0; c < kReads; ++c) read(h0, 0, c);
+      for (int step = 0; step < steps; ++step) {
+        if constexpr (kSplit) next(wp_, cp);
+        half_step(h0, h1, 1, Copies{kSplit ? kCopiesP : 0, 0, last_p(), 0});
+        const Copies n = {kSplit ? 0 : kCopiesP, kCopiesQ, slot_p, slot_q};
+        meet();
+        if constexpr (!kSplit) next(wp_, cp);
+        next(wq_, cq);
+        half_step(h1, h0, 0, n);
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    done_vt = vt;
+    done_row0 = row0;
+    done_part = part;
+    done_last = fresh = ++vt == vt_end;
+    if (fresh) unit += stride;
+  }
+}
+
+constexpr int kLds = 160 * 1024;
+static_assert(ring_bytes(kVocab, 256, 3, 2) <= kLds && ring_bytes(kVocab, 128, 3, 3) <= kLds && ring_bytes(kVocab, 64, 4, 4) <= kLds, "rings");
+
+__global__ __launch_bounds__(kThreads) void logprob_kernel(const LogitParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem[kLds];
+  const int rows = rows_found(p);
+  if (rows <= 0) return;
+  const int tile = tile_rows(rows);
+  if (tile == 256) run_units<256, 3, 2>(p, smem, rows);
+  else if (tile == 128) run_units<128, 3, 3>(p, smem, rows);
+  else run_units<64, 4, 4>(p, smem, rows);
+}
+
+// Joins a row's parts: a block a row, a thread every 256th part.
+constexpr int kJoinThreads = 256;
+struct JoinParams {
+  LogitParams l;
+  float *out_logprob, *out_entropy, *out_lse, *top_logprob;
+  int32_t* top_id;
+};
+template <typename T, typename F>
+__device__ __forceinline__ T over_block(T v, T* lds, F f) {
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) v = f(v, __shfl_xor(v, x, 64));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = lds[0];
+#pragma unroll
+  for (int w = 1; w < kJoinThreads / 64; ++w) v = f(v, lds[w]);
+  return v;
+}
+__global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(const JoinParams p) {
+  __shared__ double lds_d[kJoinThreads / 64];
+  __shared__ float lds_f[kJoinThreads / 64];
+  __shared__ long long lds_l[kJoinThreads / 64];
+  const LogitParams& l = p.l;
+  const int rows = rows_found(l);
+  const int tile = tile_rows(rows);
+  const int vocab_tiles = (int)(((int64_t)l.V + kVocab - 1) / kVocab);
+  const int halves = rows > 0 ? 2 * choose_parts((rows + tile - 1) / tile, vocab_tiles, (l.d + kTileK - 1) / kTileK) : 0;
+  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+    float m = kNeg;
+    for (int h = threadIdx.x; h < halves; h += kJoinThreads) m = fmaxf(m, l.part_m[(int64_t)h * rows + row]);
+    m = over_block(m, lds_f, [](float a, float b) { return fmaxf(a, b); });
+    double s = 0.0, t = 0.0;
+    for (int h = threadIdx.x; h < halves; h += kJoinThreads) {
+      const int64_t at = (int64_t)h * rows + row;
+      const float pm = l.part_m[at], ps = l.part_s[at];
+      const float scale = __builtin_amdgcn_exp2f((pm - m) * kLog2e);
+      s += (double)scale * ps;
+      t += (double)scale * ((double)l.part_t[at] + (double)ps * (pm - m));
+    }
+    s = over_block(s, lds_d, [](double a, double b) { return a + b; });
+    t = over_block(t, lds_d, [](double a, double b) { return a + b; });
+    const float log_s = logf((float)s);
+    if (threadIdx.x == 0) {
+      if (p.out_lse != nullptr) p.out_lse[row] = m + log_s;
+      if (p.out_entropy != nullptr) p.out_entropy[row] = log_s - (float)(t / s);
+      if (p.out_logprob != nullptr) {
+        const int target = l.targets[row];
+        p.out_logprob[row] = (uint32_t)target < (uint32_t)l.V ? (l.target_logit[row] - m) - log_s : 0.f;
+      }
+    }
+    // The best n_top of the parts' best: each time the first behind the one before, by logit, then by id.
+    float past_x = __builtin_inff();
+    int past_id = -1;
+    for (int k = 0; k < l.n_top; ++k) {
+      float x = -__builtin_inff();
+      int id = INT_MAX;
+      for (int e = threadIdx.x; e < halves * l.n_top; e += kJoinThreads) {
+        const Candidate c = l.part_top[((int64_t)(e / l.n_top) * rows + row) * l.n_top + e % l.n_top];
+        const bool behind = c.x < past_x || (c.x == past_x && c.id > past_id);
+        if (behind && (c.x > x || (c.x == x && c.id < id))) { x = c.x; id = c.id; }
+      }
+      // as one number: logits in the order of integers, ids counted down
+      const int b = __float_as_int(x);
+      long long key = ((long long)(b ^ (int)((uint32_t)(b >> 31) >> 1)) << 32) | (uint32_t)(INT_MAX - id);
+      key = over_block(key, lds_l, [](long long a, long long b) { return a > b ? a : b; });
+      const int kb = (int)(key >> 32);
+      past_x = __int_as_float(kb ^ (int)((uint32_t)(kb >> 31) >> 1));
+      past_id = INT_MAX - (int)(uint32_t)key;
+      if (threadIdx.x == 0) {
+        const bool some = past_id != INT_MAX;
+        p.top_id[row * l.n_top + k] = some ? past_id : -1;
+        p.top_logprob[row * l.n_top + k] = some ? (past_x - m) - log_s : -__builtin_inff();
+      }
+    }
+  }
+}
+
+// Rows gathered side by side, zeros from the last listed one on.
+__global__ __launch_bounds__(256) void gather_rows_kernel(const __bf16* x, int64_t ld_x, const int32_t* idx, const int32_t* count, int T,
+                                                          int max_rows, int d, __bf16* out) {
+  const int n = count == nullptr ? max_rows : *count;
+  const int per_row = d / 8;
+  const int64_t all = (int64_t)max_rows * per_row;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
+    const int64_t j = e / per_row;
+    const int c = (int)(e - j * per_row) * 8;
+    bf16x8_t v = {};
+    if (j < n) {
+      int64_t t = idx == nullptr ? j : idx[j];
+      t = t < 0 ? 0 : (t > T - 1 ? T - 1 : t);
+      v = *reinterpret_cast<const bf16x8_t*>(x + t * ld_x + c);
+    }
+    *reinterpret_cast<bf16x8_t*>(out + j * d + c) = v;
+  }
+}
+
+int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Where 32-bit offsets reach all hidden rows they are gathered as they are copied, else beforehand.
+bool far_rows(int64_t T, int64_t ld_h) { return T * ld_h * 2 > (int64_t)kOutside; }
+
+struct Space { int64_t lists, m, s, t, top, target, rows, total; };
+Space space_of(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t n_top) {
+  // of halves of parts and rows: up to kMostUnits units, at most kMostSplits parts, and one part whatever the rows
+  const int64_t tile = max_rows <= 64 ? 64 : max_rows <= 128 ? 128 : 256;
+  const int64_t most = (int64_t)kMostSplits * max_rows < kMostUnits * tile ? (int64_t)kMostSplits * max_rows : kMostUnits * tile;
+  const int64_t entries = 2 * (most > max_rows ? most : max_rows);
+  Space s;
+  s.lists = 0;
+  s.m = n_top > 0 ? (int64_t)kCus * 8 * (tile / 4) * kListRoom * (int64_t)sizeof(Candidate) : 0;
+  s.s = s.m + padded(4 * entries);
+  s.t = s.s + padded(4 * entries);
+  s.top = s.t + padded(4 * entries);
+  s.target = s.top + padded((int64_t)sizeof(Candidate) * entries * n_top);
+  s.rows = s.target + padded(4 * max_rows);
+  s.total = s.rows + (far_rows(T, ld_h) ? 2 * max_rows * d : 0);
+  return s;
+}
+
+}  // namespace
+
+int64_t logprob_workspace_bytes(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, int32_t n_top) {
+  (void)V;
+  return space_of(T, ld_h, max_rows, d, n_top).total;
+}
+
+int launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
+  const Space at = space_of(a.T, a.ld_h, a.max_rows, a.d, a.n_top);
+  char* ws = static_cast<char*>(a.workspace);
+  LogitParams p = {};
+  p.w = static_cast<const char*>(a.w);
+  p.x = static_cast<const char*>(a.hidden);
+  p.ld_w = a.ld_w * 2;
+  p.ld_x = a.ld_h * 2;
+  p.idx = a.idx;
+  p.count = a.count;
+  p.targets = a.targets;
+  p.T = (int32_t)a.T;
+  p.max_rows = (int32_t)a.max_rows;
+  p.V = a.V;
+  p.d = a.d;
+  p.n_top = a.n_top;
+  p.part_m = reinterpret_cast<float*>(ws + at.m);
+  p.part_s = reinterpret_cast<float*>(ws + at.s);
+  p.part_t = reinterpret_cast<float*>(ws + at.t);
+  p.part_top = reinterpret_cast<Candidate*>(ws + at.top);
+  p.target_logit = reinterpret_cast<float*>(ws + at.target);
+  p.lists = a.n_top > 0 ? reinterpret_cast<Candidate*>(ws + at.lists) : nullptr;
+  if (a.idx != nullptr && far_rows(a.T, a.ld_h)) {
+    __bf16* rows = reinterpret_cast<__bf16*>(ws + at.rows);
+    const int64_t pieces = a.max_rows * (a.d / 8);
+    if (launch_kernel(gather_rows_kernel, dim3((unsigned)((pieces + 255) / 256 < 65536 ? (pieces + 255) / 256 : 65536)), dim3(256),
+                      stream, static_cast<const __bf16*>(a.hidden), a.ld_h, a.idx, a.count, (int)a.T, (int)a.max_rows, a.d, rows) != 0)
+      return -1;
+    p.x = reinterpret_cast<const char*>(rows);
+    p.ld_x = (int64_t)a.d * 2;
+    p.idx = nullptr;
+  }
+  if (launch_kernel(logprob_kernel, dim3(kCus), dim3(kThreads), stream, p) != 0) return -1;
+  JoinParams j = {};
+  j.l = p;
+  j.out_logprob = a.out_logprob;
+  j.out_entropy = a.out_entropy;
+  j.out_lse = a.out_lse;
+  j.top_logprob = a.top_logprob;
+  j.top_id = a.top_id;
+  const int64_t blocks = a.max_rows < 8192 ? a.max_rows : 8192;
+  return launch_kernel(logprob_join_kernel, dim3((unsigned)blocks), dim3(kJoinThreads), stream, j);
+}
+
+}  // namespace mosaic

@@ -3,6 +3,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "mosaic_arguments.h"
 #include "mosaic_tokens_internal.h"
 
@@ -47,6 +49,15 @@ mosaic::DropoutArgs dropout_args(int64_t T, int32_t d, float p, uint64_t seed, i
   a.key_high = (uint32_t)(seed >> 32);
   a.site = (uint32_t)site + 1;
   return a;
+}
+
+// The sizes of a list of rows; rows are asked for only where there are some.
+int check_list_sizes(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V) {
+  MOSAIC_RETURN_IF(check_sizes(T, d, MOSAIC_MAX_ROW));
+  MOSAIC_RETURN_IF(check_vocab(V));
+  if (max_rows < 0) return MOSAIC_ERR_INVALID_ARG;
+  if (max_rows >= kMaxRows || ld_h < d || ld_h % 8 != 0 || ld_h > kMaxStride) return MOSAIC_ERR_UNSUPPORTED_SHAPE;
+  return MOSAIC_OK;
 }
 
 }  // namespace
@@ -145,6 +156,51 @@ int mosaic_dropout_backward(const void* dout, int32_t stream_type, int64_t ld_do
   a.ld_x = ld_dout;
   a.ld_out = ld_dx;
   return launched(mosaic::launch_dropout(a, stream_type == MOSAIC_F32, false, static_cast<hipStream_t>(stream)));
+}
+
+int64_t mosaic_masked_logprobs_workspace_bytes(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, int32_t n_top) {
+  if (check_list_sizes(T, ld_h, max_rows, d, V) != MOSAIC_OK || n_top < 0 || n_top > MOSAIC_MAX_TOP) return 0;
+  return mosaic::logprob_workspace_bytes(T, ld_h, max_rows, d, V, n_top);
+}
+
+int mosaic_masked_logprobs(const void* hidden, int64_t ld_h, int64_t T, int32_t d, const void* w, int64_t ld_w, int32_t V,
+                           const int32_t* idx, const int32_t* count, int64_t max_rows, const int32_t* targets,
+                           float* out_logprob, float* out_entropy, float* out_lse, int32_t n_top, int32_t* top_id,
+                           float* top_logprob, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (n_top < 0 || n_top > MOSAIC_MAX_TOP || (idx == nullptr) != (count == nullptr)) return MOSAIC_ERR_INVALID_ARG;
+  MOSAIC_RETURN_IF(check_list_sizes(T, ld_h, max_rows, d, V));
+  if (idx == nullptr && max_rows != T) return MOSAIC_ERR_INVALID_ARG;
+  if (T == 0 || max_rows == 0) return MOSAIC_OK;
+  if ((out_logprob == nullptr && out_entropy == nullptr && out_lse == nullptr && n_top == 0) ||
+      (out_logprob != nullptr && targets == nullptr) || (n_top > 0 && (top_id == nullptr || top_logprob == nullptr)))
+    return MOSAIC_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)idx, (const void*)count, (const void*)targets, (const void*)out_logprob, (const void*)out_entropy,
+                        (const void*)out_lse, (const void*)top_id, (const void*)top_logprob})
+    if (misaligned(p, 4)) return MOSAIC_ERR_INVALID_ARG;
+  MOSAIC_RETURN_IF(check_matrix(hidden, ld_h, d));
+  MOSAIC_RETURN_IF(check_matrix(w, ld_w, d));
+  if (workspace == nullptr || misaligned(workspace)) return MOSAIC_ERR_INVALID_ARG;
+  if (workspace_bytes < mosaic_masked_logprobs_workspace_bytes(T, ld_h, max_rows, d, V, n_top)) return MOSAIC_ERR_WORKSPACE_TOO_SMALL;
+  mosaic::LogprobArgs a = {};
+  a.hidden = hidden;
+  a.w = w;
+  a.idx = idx;
+  a.count = count;
+  a.targets = out_logprob != nullptr ? targets : nullptr;
+  a.out_logprob = out_logprob;
+  a.out_entropy = out_entropy;
+  a.out_lse = out_lse;
+  a.top_id = top_id;
+  a.top_logprob = top_logprob;
+  a.workspace = workspace;
+  a.ld_h = ld_h;
+  a.ld_w = ld_w;
+  a.T = T;
+  a.max_rows = max_rows;
+  a.d = d;
+  a.V = V;
+  a.n_top = n_top;
+  return launched(mosaic::launch_logprobs(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

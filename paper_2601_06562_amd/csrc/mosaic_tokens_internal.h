@@ -57,5 +57,24 @@ struct DropoutArgs {
 };
 int launch_dropout(const DropoutArgs& a, bool x_f32, bool out_f32, hipStream_t stream);
 
+// ---- log probabilities of given tokens (mosaic_logprob.hip)
+struct LogprobArgs {
+  const void* hidden;
+  const void* w;
+  const int32_t* idx;       // or nullptr: row j is row j
+  const int32_t* count;     // or nullptr: max_rows of them
+  const int32_t* targets;   // or nullptr
+  float* out_logprob;       // or nullptr, as the next ones
+  float* out_entropy;
+  float* out_lse;
+  int32_t* top_id;
+  float* top_logprob;
+  void* workspace;
+  int64_t ld_h, ld_w, T, max_rows;   // strides in elements
+  int32_t d, V, n_top;
+};
+int64_t logprob_workspace_bytes(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, int32_t n_top);
+int launch_logprobs(const LogprobArgs& a, hipStream_t stream);
+
 }  // namespace mosaic
 #endif
