@@ -112,6 +112,33 @@ int mosaic_masked_logprobs(const void *hidden, int64_t ld_h, int64_t T, int32_t 
                            float *out_logprob, float *out_entropy, float *out_lse, int32_t n_top, int32_t *top_id,
                            float *top_logprob, void *workspace, int64_t workspace_bytes, void *stream);
 
+/*
+ * Its gradients, from those of out_logprob (g) and out_entropy (h); the logits are computed again, a part of the vocabulary at a
+ * time.  With p[j, v] and the entropy H[j] as above:
+ *   dl[j, v] = g[j] ([v == targets[j]] - p[j, v]) - h[j] p[j, v] (log p[j, v] + H[j])       (g[j] = 0 without a target)
+ *   dx[j]    = sum_v dl[j, v] w[v]                              the gradient at the listed row hidden[idx[j]]
+ *   dw[v]    = sum_j dl[j, v] hidden[idx[j]]                    [+ what dw holds, if accumulate]
+ * dl is rounded to bf16 for the matrix cores (up to 2^-8 relative per term; up to 32 rows with what that leaves over in a
+ * second number each), but for the target's entries, which outweigh the others: those go into both sums in 32 bits.
+ *   hidden .. targets   as for the forward pass
+ *   logprob, entropy, lse   dev float[max_rows], what the forward pass gave: lse always, logprob with dlogprob, entropy with dentropy
+ *   dlogprob   dev float[max_rows], or NULL (then targets and logprob are not looked at);  dentropy: the same, or NULL; not both NULL
+ *   dx         bf16 [max_rows, d] or NULL; rows from M on are left as they were.  A program whose listed rows are all different
+ *              scatters them itself; mosaic_embedding_backward with idx as the tokens does it also where they are not
+ *   dw         [V, d] by `dw_type`, row stride ld_dw, or NULL; not both NULL.  Every row is written
+ *   accumulate nonzero: dw is added to (32-bit only), so that a batch can be taken in parts
+ *   workspace  dev, 16-byte aligned: the listed rows, 32-bit sums of dx, the targets' terms of dw (6 and 4 max_rows d bytes and
+ *              more for few rows), and dl of as many ids as the rest holds, 2 max_rows bytes each, at least 256.  The query answers for
+ *              at most budget_bytes where that is enough, 0 or less: dl of up to 256 MiB.  The sums' last bits follow from the size
+ * Every row of the bound costs what a listed one does: a close max_rows is worth its while.
+ */
+int64_t mosaic_masked_logprobs_backward_workspace_bytes(int64_t max_rows, int32_t d, int32_t V, int64_t budget_bytes);
+int mosaic_masked_logprobs_backward(const void *hidden, int64_t ld_h, int64_t T, int32_t d, const void *w, int64_t ld_w, int32_t V,
+                                    const int32_t *idx, const int32_t *count, int64_t max_rows, const int32_t *targets,
+                                    const float *logprob, const float *entropy, const float *lse, const float *dlogprob,
+                                    const float *dentropy, void *dx, int64_t ld_dx, void *dw, int32_t dw_type, int64_t ld_dw,
+                                    int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -46,6 +46,7 @@ LAYER_EXPORTS = (   # include/mosaic_layer.h
 TOKEN_EXPORTS = (   # include/mosaic_tokens.h
     "mosaic_embedding_forward", "mosaic_embedding_backward_workspace_bytes", "mosaic_embedding_backward",
     "mosaic_dropout_forward", "mosaic_dropout_backward", "mosaic_masked_logprobs_workspace_bytes", "mosaic_masked_logprobs",
+    "mosaic_masked_logprobs_backward_workspace_bytes", "mosaic_masked_logprobs_backward",
 )
 MAX_TOP = 16                         # alternatives a row that mosaic_masked_logprobs gives at most
 BF16, F32 = 0, 1                     # mosaic_type
@@ -594,6 +595,11 @@ def _tokens():
         L.mosaic_masked_logprobs_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32]
         L.mosaic_masked_logprobs.restype = ctypes.c_int
         L.mosaic_masked_logprobs.argtypes = [p, i64, i64, i32, p, i64, i32, p, p, i64, p, p, p, p, i32, p, p, p, i64, p]
+        L.mosaic_masked_logprobs_backward_workspace_bytes.restype = i64
+        L.mosaic_masked_logprobs_backward_workspace_bytes.argtypes = [i64, i32, i32, i64]
+        L.mosaic_masked_logprobs_backward.restype = ctypes.c_int
+        L.mosaic_masked_logprobs_backward.argtypes = [p, i64, i64, i32, p, i64, i32, p, p, i64, p, p, p, p, p, p, p, i64, p, i32,
+                                                      i64, i32, p, i64, p]
         _token_lib = L
     return _token_lib
 
@@ -701,6 +707,28 @@ def mosaic_masked_logprobs(hidden, w, idx, count, max_rows, targets, out_logprob
         _per_row(out_lse, "out_lse", max_rows), n_top, _dev_ptr(top_id, "top_id", torch.int32),
         _dev_ptr(top_logprob, "top_logprob", torch.float32), *_workspace_args(workspace), _stream_ptr(stream)),
         "mosaic_masked_logprobs")
+
+
+def mosaic_masked_logprobs_backward_workspace_bytes(max_rows, d, V, budget_bytes=0) -> int:
+    return int(_tokens().mosaic_masked_logprobs_backward_workspace_bytes(max_rows, d, V, budget_bytes))
+
+
+def mosaic_masked_logprobs_backward(hidden, w, idx, count, max_rows, targets, logprob, entropy, lse, dlogprob, dentropy, dx, dw,
+                                    workspace, accumulate=False, stream=None):
+    """Gradients of mosaic_masked_logprobs from those of its log probabilities and entropies (float32, either may be None) and
+    what it gave (lse; logprob with dlogprob; entropy with dentropy): dx bf16 [max_rows, d], row j that of the listed row
+    hidden[idx[j]], and dw bf16 or float32 [V, d] (added to what it holds if accumulate; float32 only); either may be None."""
+    p_h, ld_h, T, d, p_w, ld_w, V, p_idx, p_count = _list_args(hidden, w, idx, count, max_rows)
+    if dx is not None and (dx.dim() != 2 or dx.shape[0] < max_rows):
+        raise ValueError("dx must be [max_rows, d]")
+    p_dx, ld_dx = _rows(dx, "dx", dx.shape[0] if dx is not None else 0, d, torch.bfloat16)
+    p_dw, ld_dw = _rows(dw, "dw", V, d)
+    vectors = [_per_row(t, name, max_rows, torch.int32 if name == "targets" else torch.float32) for t, name in (
+        (targets, "targets"), (logprob, "logprob"), (entropy, "entropy"), (lse, "lse"), (dlogprob, "dlogprob"), (dentropy, "dentropy"))]
+    _check(_tokens().mosaic_masked_logprobs_backward(
+        p_h, ld_h, T, d, p_w, ld_w, V, p_idx, p_count, max_rows, *vectors, p_dx, ld_dx, p_dw,
+        _type_of(dw, "dw") if dw is not None else BF16, ld_dw, int(bool(accumulate)), *_workspace_args(workspace),
+        _stream_ptr(stream)), "mosaic_masked_logprobs_backward")
 
 
 class VmmWorkspace:

@@ -46,6 +46,9 @@ struct GemmArgs {
   int64_t ld_out0, ld_out1;
   int64_t low;         // kRecompute: from a row of dg | du to that of its low halves, bytes; 0: none are wanted
   int32_t repeat;      // kDw: rows of x there are where K, one step then, takes them twice; else 0
+  const int32_t* slot; // kOneDw: for each output row the row of `extra` that is added to it, or -1; nullptr: none
+  const float* extra;
+  int64_t ld_extra;    // elements
 };
 
 __device__ __forceinline__ float sigmoid(float z) {
@@ -77,8 +80,8 @@ __device__ __forceinline__ void activate(float g, float& a, float& slope) {
 // stored.
 template <int MODE, int TP, int TQ, int SP, int SQ, int ACT>
 __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int block, int blocks) {
-  constexpr bool kGated = gated_mode(MODE);
-  constexpr bool kRowP = !kGated, kRowQ = MODE == kDw;
+  constexpr bool kGated = gated_mode(MODE), kIsDx = MODE == kDx || MODE == kOneDx, kIsDw = MODE == kDw || MODE == kOneDw;
+  constexpr bool kRowP = !kGated, kRowQ = kIsDw;
   constexpr int kTileP = TP, kTileQ = TQ, kBlocksP = TP / 32, QB = TQ / 64;   // blocks of a wave
   constexpr int kBytesP = kTileP * kStepK * 2, kBytesQ = kTileQ * kStepK * 2;
   using CopierP = Copier<kTileP, kRowP>;
@@ -127,7 +130,7 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
       p_base1 = MODE == kDx ? a.p1 + (int64_t)p_row * 2 : p_base0;
     }
     q_base = kRowQ ? a.q + q_row * 2 : a.q + q_row * a.ld_q;
-    cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, kStepK, MODE == kDw ? a.repeat : 0);
+    cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, kStepK, kIsDw ? a.repeat : 0);
     cq.place(wave, lane, a.ld_q, a.rows_q - q_row, kStepK);
     placed_p = placed_q = kStepK;
     step0 = (int)((int64_t)all_steps * split / a.splits);
@@ -172,7 +175,7 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
       placed_p = left;
       cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, left);
     }
-    const int rows = MODE == kDw && a.repeat != 0 && left != 0 ? a.repeat : left;   // across K: there are behind the base
+    const int rows = kIsDw && a.repeat != 0 && left != 0 ? a.repeat : left;   // across K: there are behind the base
     walk_p.from = buffer_from((seg ? p_base1 : p_base0) + (kRowP ? k * a.ld_p : k * 2),
                               kRowP ? rows * (uint32_t)a.ld_p : left == 0 ? 0 : kOutside);
   };
@@ -226,7 +229,7 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
   // of d 4096 x F 12288, both orders in turn on one card, forward in 2280 us for 2330, dx 2270 for 2314.  (dw, which reads both
   // operands by transposing, would spill 117 registers: eight times slower.)
   // fq: a step's Q fragments; fp: those of two pairs of P blocks.
-  constexpr bool kPaired = TP == 256 && TQ == 256 && MODE != kDw;
+  constexpr bool kPaired = TP == 256 && TQ == 256 && !kIsDw;
   static_assert(!kPaired || (kSplit && SQ == 2 && 2 * kCopiesP <= (kBlocksP / 2 - 1) * QB - 2 && kCopiesQ <= QB + 1),
                 "P's copies before the meeting of a step, Q's behind it");
   bf16x8_t fq[2 * QB], fp[2][2][2];
@@ -375,9 +378,20 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
           if (in && a.out0 != nullptr) store_quads(a.out0 + q * a.ld_out0, f, a.rows_p, o);
         } else {
           char* row;
-          if constexpr (MODE == kDx) row = a.out0 + ((int64_t)done_split * a.rows_q + q) * a.ld_out0;
+          if constexpr (kIsDx) row = a.out0 + ((int64_t)done_split * a.rows_q + q) * a.ld_out0;
+          else if constexpr (MODE == kOneDw) row = a.out0 + q * a.ld_out0;
           else row = q < a.F ? a.out0 + q * a.ld_out0 : a.out1 + (q - a.F) * a.ld_out0;
           const int c0 = done_p + wp * (kTileP / 2);
+          if constexpr (MODE == kOneDw) {
+            const int at = in && a.slot != nullptr ? a.slot[q] : -1;
+            if (at >= 0) {
+#pragma unroll
+              for (int i = 0; i < kBlocksP; ++i) {
+                const int c = c0 + i * 16 + sub;
+                if (c < a.rows_p) acc[i][j] += *reinterpret_cast<const f32x4_t*>(a.extra + at * a.ld_extra + c);
+              }
+            }
+          }
           if (a.f32) {
 #pragma unroll
             for (int i = 0; i < kBlocksP; ++i) {
@@ -714,6 +728,52 @@ int launch_gated_ffn_forward(const FfnForwardArgs& f, hipStream_t stream) {
   }
   return 0;
 }
+
+ProductPlan plan_row_product(int64_t rows, int32_t cols, int64_t depth) {
+  const int64_t steps = tiles(depth, kStepK);
+  ProductPlan best = {1, 0.0};
+  for (int32_t s = 1; s == 1 || (s <= kMostParts && s * rows <= kPartRows && s * 4 <= steps); ++s) {
+    const double us = choose_tile(kOneDx, cols, rows, steps, s).us + (double)(rows * cols) * 8.0 * s / kJoinBytesPerUs;
+    if (s == 1 || us < best.us) best = {s, us};
+  }
+  return best;
+}
+
+namespace {
+GemmArgs product_args(const ProductArgs& f) {
+  GemmArgs a = {};
+  a.p0 = a.p1 = static_cast<const char*>(f.p);
+  a.q = static_cast<const char*>(f.q);
+  a.ld_p = f.ld_p * 2;
+  a.ld_q = f.ld_q * 2;
+  a.rows_q = f.rows;
+  a.rows_p = f.cols;
+  a.depth = f.depth;
+  a.splits = f.splits;
+  a.f32 = f.f32;
+  a.accumulate = f.accumulate;
+  a.out0 = static_cast<char*>(f.out);
+  a.ld_out0 = f.ld_out * (f.f32 ? 4 : 2);
+  a.repeat = f.repeat;
+  a.slot = f.slot;
+  a.extra = f.extra;
+  a.ld_extra = f.ld_extra;
+  return a;
+}
+}  // namespace
+
+int launch_row_product(const ProductArgs& f, hipStream_t stream) {
+  GemmArgs a = product_args(f);
+  for (int64_t t = 0; t < f.rows; t += kLaunchRows) {   // (parts only where all rows are in one launch)
+    a.rows_q = f.rows - t < kLaunchRows ? f.rows - t : kLaunchRows;
+    a.q = static_cast<const char*>(f.q) + t * a.ld_q;
+    a.out0 = static_cast<char*>(f.out) + t * a.ld_out0;
+    if (launch_gemm<kOneDx, 0>(a, stream) != 0) return -1;
+  }
+  return 0;
+}
+
+int launch_column_product(const ProductArgs& f, hipStream_t stream) { return launch_gemm<kOneDw, 0>(product_args(f), stream); }
 
 int launch_gated_ffn_backward(const FfnBackwardArgs& f, hipStream_t stream) {
   const int64_t ld_grads = (int64_t)f.F * 4;

@@ -15,7 +15,8 @@ namespace ffn {
 constexpr int kStepK = 64;
 constexpr int kCus = 256;
 
-enum { kForward, kRecompute, kDx, kDw };
+// kOneDx, kOneDw: the gradients' products of a single weight matrix (the LM head's; mosaic_layer_internal.h).
+enum { kForward, kRecompute, kDx, kDw, kOneDx, kOneDw };
 constexpr bool gated_mode(int mode) { return mode == kForward || mode == kRecompute; }
 
 inline int64_t tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }

@@ -75,6 +75,25 @@ int64_t ffn_gradient_rows(int64_t T);
 int64_t ffn_partial_rows(int64_t T);
 int launch_gated_ffn_backward(const FfnBackwardArgs& a, hipStream_t stream);
 
+// The two products of a matrix's gradients, on the block's tiles.
+//   row product      out[r, c] = sum_k q[r, k] p[k, c]      rows r of q along K; parts of K, `splits` of them, go to [splits, rows, cols]
+//   column product   out[r, c] = sum_k q[k, r] p[k, c]  [+ extra[slot[r], c]]      r a column of q, at most 2^18 of them
+struct ProductArgs {
+  const void* p;   // bf16 [depth, cols]
+  const void* q;   // bf16 [rows, depth], or [depth, rows]
+  void* out;       // bf16, or 32-bit: then added to what it holds where `accumulate` says so
+  const int32_t* slot;   // column product: or nullptr
+  const float* extra;
+  int64_t ld_p, ld_q, ld_out, ld_extra;   // elements
+  int64_t rows, depth;
+  int32_t cols, splits, f32, accumulate;
+  int32_t repeat;        // column product: rows of p that there are where K, at most 64 then, takes them twice; else 0
+};
+struct ProductPlan { int32_t splits; double us; };
+ProductPlan plan_row_product(int64_t rows, int32_t cols, int64_t depth);
+int launch_row_product(const ProductArgs& a, hipStream_t stream);
+int launch_column_product(const ProductArgs& a, hipStream_t stream);
+
 #ifdef __HIPCC__
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4_t;

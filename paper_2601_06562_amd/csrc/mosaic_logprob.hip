@@ -42,7 +42,13 @@ struct LogitParams {
   Candidate* part_top;       // n_top each
   float* target_logit;       // [max_rows]
   Candidate* lists;          // of every block's waves and rows, kListRoom each
+  // gradients: of V ids from `first_id` on, for max_rows rows (zeros from the last listed one on)
+  const float *lse, *entropy, *dlogprob, *dentropy;   // the last three each with what needs them, else nullptr
+  char* dl;                  // bf16 [max_rows, ld_dl]
+  int64_t ld_dl, low;        // bytes; low: from a row to what its rounding left over, 0: not wanted
+  int32_t first_id, all_ids;
 };
+enum { kStatistics, kGradients };
 
 __device__ __forceinline__ int rows_found(const LogitParams& p) {
   if (p.count == nullptr) return p.max_rows;
@@ -277,9 +283,58 @@ __device__ __forceinline__ void reduce_tile(const LogitParams& p, f32x4_t (&acc)
   st.m = m;
 }
 
+// The gradient at a finished tile's logits, in 16 bits, as the matrix products behind take it:
+//   dl[v] = - p[v] (g + h (log p[v] + H))      g, h: the gradients of the row's log probability and entropy H
+// with 0 at the target, whose one-hot term outweighs the others; the target's whole term goes past the 16 bits (target_terms_kernel).
+template <int QB>
+__device__ __forceinline__ void gradient_tile(const LogitParams& p, f32x4_t (&acc)[8][QB], int64_t v0, int row0, int found) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, run = first_of<4>(lane);
+  const int64_t end = ((int64_t)p.V + 7) / 8 * 8;
+#pragma unroll
+  for (int j = 0; j < QB; ++j) {
+    const int row = row0 + 16 * j + l16;
+    const bool in = row < p.max_rows, listed = row < found;
+    const float lse = listed ? p.lse[row] : 0.f;
+    const int target = listed && p.targets != nullptr ? p.targets[row] : -1;
+    const float g = (uint32_t)target < (uint32_t)p.all_ids ? p.dlogprob[row] : 0.f;
+    const float h = listed && p.dentropy != nullptr ? p.dentropy[row] : 0.f;
+    const float entropy = listed && p.dentropy != nullptr ? p.entropy[row] : 0.f;
+    const int64_t from = (int64_t)target - p.first_id - v0;
+    const int rel = target >= 0 && from >= 0 && from < kHalf ? (int)from - 4 * g4 : -kHalf;   // from this lane's first id
+    const int there = p.V - v0 < kHalf ? (int)(p.V - v0) - 4 * g4 : kHalf;                     // ids there are from there on
+#pragma unroll
+    for (int b = 0; b < 8; b += 4) {
+      Quad o[4], low[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int at = 16 * (b + k) + r;
+          const float logp = acc[b + k][j][r] - lse;
+          const float prob = __builtin_amdgcn_exp2f(logp * kLog2e);
+          const float d = -prob * (p.dentropy != nullptr ? g + h * (logp + entropy) : g);
+          v[r] = listed && rel != at && at < there ? d : 0.f;
+        }
+        pack(o[k], v);
+        if constexpr (QB == 1) pack_low(low[k], o[k], v);
+      }
+      gather(o);
+      const int c = (int)(v0 + 16 * b) + run;
+      if (in) store_quads(p.dl + row * p.ld_dl, c, (int)end, o);
+      if constexpr (QB == 1) {   // the tiles that few rows take
+        if (p.low != 0) {
+          gather(low);
+          if (in) store_quads(p.dl + p.low + row * p.ld_dl, c, (int)end, low);
+        }
+      }
+    }
+  }
+}
+
 // All units of this block, in tiles of TQ rows.
-template <int TQ, int SP, int SQ>
-__device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int rows) {
+template <int MODE, int TQ, int SP, int SQ>
+__device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int rows, int found) {
   constexpr int QB = TQ / 64, kBytesP = kVocab * kTileK * 2, kBytesQ = TQ * kTileK * 2;
   constexpr int kCopiesP = 4, kCopiesQ = QB, kBlocksP = 8;
   constexpr bool kSplit = SP != SQ;
@@ -446,32 +501,36 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
     if (done_vt >= 0) {
       const int64_t v = (int64_t)done_vt * kVocab;
       const int q0 = done_row0 + wq * 16 * QB, g = lane >> 4;
-      reduce_tile<QB>(p, acc, st, v + wp * kHalf + 4 * g, q0, rows, v + kVocab > p.V, lists);
-      ++done_tiles;
-      const int64_t row = q0 + 16 * g + (lane & 15), of_half = 2 * done_part + wp;
-      const bool owner = g < QB && row < rows;
-      if (p.n_top > 0) {
-        const bool now = done_last || (done_tiles & (done_tiles - 1)) == 0 || __any(owner && st.n > kListRoom - kHalf);
-        if (now) {
-          __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // the list's entries were stored by other lanes
-          if (owner) {
-            Candidate* list = lists + (16 * g + (lane & 15)) * kListRoom;
-            Candidate* to = done_last ? p.part_top + (of_half * rows + row) * p.n_top : list;
-            if (p.n_top <= 4) keep_best<4>(st, list, to, p.n_top);
-            else if (p.n_top <= 8) keep_best<8>(st, list, to, p.n_top);
-            else keep_best<16>(st, list, to, p.n_top);
+      if constexpr (MODE == kGradients) {
+        gradient_tile<QB>(p, acc, v + wp * kHalf, q0, found);
+      } else {
+        reduce_tile<QB>(p, acc, st, v + wp * kHalf + 4 * g, q0, rows, v + kVocab > p.V, lists);
+        ++done_tiles;
+        const int64_t row = q0 + 16 * g + (lane & 15), of_half = 2 * done_part + wp;
+        const bool owner = g < QB && row < rows;
+        if (p.n_top > 0) {
+          const bool now = done_last || (done_tiles & (done_tiles - 1)) == 0 || __any(owner && st.n > kListRoom - kHalf);
+          if (now) {
+            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // the list's entries were stored by other lanes
+            if (owner) {
+              Candidate* list = lists + (16 * g + (lane & 15)) * kListRoom;
+              Candidate* to = done_last ? p.part_top + (of_half * rows + row) * p.n_top : list;
+              if (p.n_top <= 4) keep_best<4>(st, list, to, p.n_top);
+              else if (p.n_top <= 8) keep_best<8>(st, list, to, p.n_top);
+              else keep_best<16>(st, list, to, p.n_top);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");
           }
-          __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");
         }
-      }
-      if (done_last) {
-        if (owner) {
-          p.part_m[of_half * rows + row] = st.m;
-          p.part_s[of_half * rows + row] = st.s;
-          p.part_t[of_half * rows + row] = st.t;
+        if (done_last) {
+          if (owner) {
+            p.part_m[of_half * rows + row] = st.m;
+            p.part_s[of_half * rows + row] = st.s;
+            p.part_t[of_half * rows + row] = st.t;
+          }
+          st = RowState{kNeg, 0.f, 0.f, kNeg, 0};
+          done_tiles = 0;
         }
-        st = RowState{kNeg, 0.f, 0.f, kNeg, 0};
-        done_tiles = 0;
       }
     }
     if (!more) break;
@@ -553,9 +612,14 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(const LogitParams p) 
   const int rows = rows_found(p);
   if (rows <= 0) return;
   const int tile = tile_rows(rows);
-  if (tile == 256) run_units<256, 3, 2>(p, smem, rows);
-  else if (tile == 128) run_units<128, 3, 3>(p, smem, rows);
-  else run_units<64, 4, 4>(p, smem, rows);
+  if (tile == 256) run_units<kStatistics, 256, 3, 2>(p, smem, rows, rows);
+  else if (tile == 128) run_units<kStatistics, 128, 3, 3>(p, smem, rows, rows);
+  else run_units<kStatistics, 64, 4, 4>(p, smem, rows, rows);
+}
+template <int TQ, int SP, int SQ>
+__global__ __launch_bounds__(kThreads) void logit_gradient_kernel(const LogitParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem[ring_bytes(kVocab, TQ, SP, SQ)];
+  run_units<kGradients, TQ, SP, SQ>(p, smem, p.max_rows, rows_found(p));
 }
 
 // Joins a row's parts: a block a row, a thread every 256th part.
@@ -655,6 +719,71 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const __bf16* x, int64
   }
 }
 
+// What a row's target adds beside the products of dl: coef[j] = g (1 - p) - h p (log p + H), p = exp(logprob[j]).
+struct TermParams {
+  const int32_t *targets, *count;
+  const float *logprob, *entropy, *dlogprob, *dentropy;
+  float* coef;
+  int32_t max_rows, V;
+};
+__global__ __launch_bounds__(256) void target_terms_kernel(const TermParams p) {
+  const int found = p.count == nullptr ? p.max_rows : *p.count;
+  for (int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x; j < p.max_rows; j += (int64_t)gridDim.x * 256) {
+    float c = 0.f;
+    if (j < found) {
+      const int target = p.targets[j];
+      if ((uint32_t)target < (uint32_t)p.V) {
+        const float logp = p.logprob[j], prob = expf(logp);
+        c = p.dlogprob[j] * -expm1f(logp);
+        if (p.dentropy != nullptr) c -= p.dentropy[j] * prob * (logp + p.entropy[j]);
+      }
+    }
+    p.coef[j] = c;
+  }
+}
+
+// dx[j] = the parts' sums (of both halves where dl had two) + coef[j] w[targets[j]], rounded once.
+struct RowsOutParams {
+  const float* parts;
+  const __bf16* w;
+  const int32_t *targets, *count;   // targets: or nullptr
+  const float* coef;
+  __bf16* dx;
+  int64_t ld_w, ld_dx;
+  int32_t n_parts, max_rows, d, V;
+};
+__global__ __launch_bounds__(256) void rows_out_kernel(const RowsOutParams p) {
+  constexpr int kAtOnce = 4;
+  const int n = p.count == nullptr ? p.max_rows : *p.count;
+  const int64_t rows = n < p.max_rows ? n : p.max_rows, per_row = p.d / 8, all = rows * per_row;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
+    const int64_t j = e / per_row;
+    const int c = (int)(e - j * per_row) * 8;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int target = p.targets != nullptr ? p.targets[j] : -1;
+    if ((uint32_t)target < (uint32_t)p.V) {
+      const float coef = p.coef[j];
+      load8(p.w + target * p.ld_w + c, s);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] *= coef;
+    }
+    for (int k = 0; k < p.n_parts; k += kAtOnce) {
+      float v[kAtOnce][8];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[i][x] = 0.f;
+        if (k + i < p.n_parts) load8(p.parts + ((int64_t)(k + i) * p.max_rows + j) * p.d + c, v[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) s[x] += v[i][x];
+    }
+    store8(p.dx + j * p.ld_dx + c, s);
+  }
+}
+
 int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // Where 32-bit offsets reach all hidden rows they are gathered as they are copied, else beforehand.
@@ -727,6 +856,173 @@ int launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
   j.top_id = a.top_id;
   const int64_t blocks = a.max_rows < 8192 ? a.max_rows : 8192;
   return launch_kernel(logprob_join_kernel, dim3((unsigned)blocks), dim3(kJoinThreads), stream, j);
+}
+
+// ---- gradients.  Per part of the vocabulary: dl of its ids, then both products of it.
+namespace {
+
+constexpr int64_t kDlBytes = (int64_t)256 << 20;   // of dl, where the caller sets no other bound
+constexpr int64_t kLowRows = 32;                   // up to here dl carries what its rounding leaves over, as the feed-forward block's
+
+struct GradientSpace {
+  int64_t rows, coef, sort, sums, extra, slot, parts, dl, least;   // offsets; least: bytes for one tile of ids
+  int64_t dl_rows;
+  int32_t splits;
+};
+GradientSpace gradient_space(int64_t max_rows, int32_t d, int32_t V) {
+  GradientSpace s;
+  const bool low = max_rows <= kLowRows;
+  s.dl_rows = low ? 2 * max_rows : max_rows;
+  s.splits = plan_row_product(s.dl_rows, d, V < 65536 ? V : 65536).splits;
+  s.rows = 0;
+  s.coef = s.rows + padded(2 * max_rows * d);
+  s.sort = s.coef + padded(4 * max_rows);
+  s.sums = s.sort + padded(sort_tokens_bytes(max_rows, V));
+  s.extra = s.sums + padded(4 * token_sum_partials(max_rows) * d);
+  s.slot = s.extra + padded(4 * max_rows * d);
+  s.parts = s.slot + padded(4 * (int64_t)V);
+  s.dl = s.parts + padded(4 * s.splits * s.dl_rows * d);
+  s.least = s.dl + 2 * s.dl_rows * kVocab;
+  return s;
+}
+// Ids at a time with so many bytes for dl, evenly, in whole tiles.
+constexpr int64_t kMostIds = (int64_t)1 << 18;
+int64_t ids_at_once(int64_t dl_rows, int32_t V, int64_t bytes) {
+  int64_t most = bytes / (2 * dl_rows) / kVocab * kVocab;
+  if (most > kMostIds) most = kMostIds;
+  if (most < kVocab) most = kVocab;
+  const int64_t parts = ((int64_t)V + most - 1) / most;
+  return (((int64_t)V + parts - 1) / parts + kVocab - 1) / kVocab * kVocab;
+}
+
+template <int TQ, int SP, int SQ>
+int launch_gradient_tiles(const LogitParams& p, hipStream_t stream) {
+  return launch_kernel(logit_gradient_kernel<TQ, SP, SQ>, dim3(kCus), dim3(kThreads), stream, p);
+}
+
+}  // namespace
+
+int64_t logprob_backward_workspace_bytes(int64_t max_rows, int32_t d, int32_t V, int64_t budget_bytes) {
+  const GradientSpace at = gradient_space(max_rows, d, V);
+  const int64_t room = budget_bytes > 0 ? budget_bytes - at.dl : kDlBytes;
+  return at.dl + 2 * at.dl_rows * ids_at_once(at.dl_rows, V, room);
+}
+int64_t logprob_backward_least_bytes(int64_t max_rows, int32_t d, int32_t V) { return gradient_space(max_rows, d, V).least; }
+
+int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
+  const GradientSpace at = gradient_space(a.max_rows, a.d, a.V);
+  char* ws = static_cast<char*>(a.workspace);
+  __bf16* rows = reinterpret_cast<__bf16*>(ws + at.rows);
+  float* coef = reinterpret_cast<float*>(ws + at.coef);
+  float* extra = reinterpret_cast<float*>(ws + at.extra);
+  int32_t* slot = reinterpret_cast<int32_t*>(ws + at.slot);
+  float* parts = reinterpret_cast<float*>(ws + at.parts);
+  const int64_t pieces = (a.max_rows * (a.d / 8) + 255) / 256;
+  const dim3 grid((unsigned)(pieces < 65536 ? pieces : 65536));
+  if (launch_kernel(gather_rows_kernel, grid, dim3(256), stream, static_cast<const __bf16*>(a.hidden), a.ld_h, a.idx, a.count, (int)a.T,
+                    (int)a.max_rows, a.d, rows) != 0)
+    return -1;
+  // the targets' own terms: for dw summed by target
+  const bool dw = a.dw != nullptr;
+  if (a.targets != nullptr) {
+    TermParams t = {a.targets, a.count, a.logprob, a.entropy, a.dlogprob, a.dentropy, coef, (int32_t)a.max_rows, a.V};
+    const int64_t blocks = (a.max_rows + 255) / 256;
+    if (launch_kernel(target_terms_kernel, dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(256), stream, t) != 0) return -1;
+    if (dw) {
+      TokenSumArgs sum = {};
+      if (launch_sort_tokens(a.targets, a.max_rows, a.count, a.V, ws + at.sort, &sum.sorted, stream) != 0) return -1;
+      sum.rows = rows;
+      sum.weights = coef;
+      sum.partials = reinterpret_cast<float*>(ws + at.sums);
+      sum.sums = extra;
+      sum.first = slot;
+      sum.n = a.max_rows;
+      sum.ld_rows = sum.ld_sums = a.d;
+      sum.V = a.V;
+      sum.d = a.d;
+      sum.scale = 1.f;
+      if (launch_token_sums(sum, false, true, stream) != 0) return -1;
+    }
+  }
+  const int64_t each = ids_at_once(at.dl_rows, a.V, a.workspace_bytes - at.dl);
+  const bool low = a.max_rows <= kLowRows;
+  LogitParams p = {};
+  p.x = reinterpret_cast<const char*>(rows);
+  p.ld_w = a.ld_w * 2;
+  p.ld_x = (int64_t)a.d * 2;
+  p.count = a.count;
+  p.targets = a.targets;
+  p.T = (int32_t)a.T;
+  p.max_rows = (int32_t)a.max_rows;
+  p.d = a.d;
+  p.lse = a.lse;
+  p.entropy = a.entropy;
+  p.dlogprob = a.dlogprob;
+  p.dentropy = a.dentropy;
+  p.dl = ws + at.dl;
+  p.ld_dl = each * 2;
+  p.low = low ? a.max_rows * p.ld_dl : 0;
+  p.all_ids = a.V;
+  for (int64_t v = 0; v < a.V; v += each) {
+    const int64_t n = a.V - v < each ? a.V - v : each;
+    p.w = static_cast<const char*>(a.w) + v * p.ld_w;
+    p.V = (int32_t)n;
+    p.first_id = (int32_t)v;
+    const int tile = tile_rows(a.max_rows);
+    const int rc = tile == 256 ? launch_gradient_tiles<256, 3, 2>(p, stream)
+                   : tile == 128 ? launch_gradient_tiles<128, 3, 3>(p, stream) : launch_gradient_tiles<64, 4, 4>(p, stream);
+    if (rc != 0) return -1;
+    if (a.dx != nullptr) {
+      ProductArgs x = {};
+      x.p = p.w;
+      x.q = p.dl;
+      x.out = parts;
+      x.ld_p = a.ld_w;
+      x.ld_q = each;
+      x.ld_out = a.d;
+      x.rows = at.dl_rows;
+      x.depth = n;
+      x.cols = a.d;
+      x.splits = at.splits;
+      x.f32 = 1;
+      x.accumulate = v > 0;
+      if (launch_row_product(x, stream) != 0) return -1;
+    }
+    if (dw) {
+      ProductArgs w = {};
+      w.p = rows;
+      w.q = p.dl;
+      w.out = static_cast<char*>(a.dw) + v * a.ld_dw * (a.dw_f32 ? 4 : 2);
+      w.slot = a.targets != nullptr ? slot + v : nullptr;
+      w.extra = extra;
+      w.ld_p = w.ld_extra = a.d;
+      w.ld_q = each;
+      w.ld_out = a.ld_dw;
+      w.rows = n;
+      w.depth = at.dl_rows;
+      w.cols = a.d;
+      w.splits = 1;
+      w.f32 = a.dw_f32;
+      w.accumulate = a.accumulate;
+      w.repeat = low ? (int32_t)a.max_rows : 0;
+      if (launch_column_product(w, stream) != 0) return -1;
+    }
+  }
+  if (a.dx == nullptr) return 0;
+  RowsOutParams o = {};
+  o.parts = parts;
+  o.w = static_cast<const __bf16*>(a.w);
+  o.targets = a.targets;
+  o.count = a.count;
+  o.coef = coef;
+  o.dx = static_cast<__bf16*>(a.dx);
+  o.ld_w = a.ld_w;
+  o.ld_dx = a.ld_dx;
+  o.n_parts = at.splits * (low ? 2 : 1);
+  o.max_rows = (int32_t)a.max_rows;
+  o.d = a.d;
+  o.V = a.V;
+  return launch_kernel(rows_out_kernel, grid, dim3(256), stream, o);
 }
 
 }  // namespace mosaic

@@ -203,4 +203,71 @@ int mosaic_masked_logprobs(const void* hidden, int64_t ld_h, int64_t T, int32_t 
   return launched(mosaic::launch_logprobs(a, static_cast<hipStream_t>(stream)));
 }
 
+int64_t mosaic_masked_logprobs_backward_workspace_bytes(int64_t max_rows, int32_t d, int32_t V, int64_t budget_bytes) {
+  if (check_list_sizes(0, d, max_rows, d, V) != MOSAIC_OK || max_rows == 0) return 0;
+  return mosaic::logprob_backward_workspace_bytes(max_rows, d, V, budget_bytes);
+}
+
+int mosaic_masked_logprobs_backward(const void* hidden, int64_t ld_h, int64_t T, int32_t d, const void* w, int64_t ld_w, int32_t V,
+                                    const int32_t* idx, const int32_t* count, int64_t max_rows, const int32_t* targets,
+                                    const float* logprob, const float* entropy, const float* lse, const float* dlogprob,
+                                    const float* dentropy, void* dx, int64_t ld_dx, void* dw, int32_t dw_type, int64_t ld_dw,
+                                    int32_t accumulate, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!known_type(dw_type) || (accumulate != 0 && dw != nullptr && dw_type != MOSAIC_F32) || (idx == nullptr) != (count == nullptr))
+    return MOSAIC_ERR_INVALID_ARG;
+  MOSAIC_RETURN_IF(check_list_sizes(T, ld_h, max_rows, d, V));
+  if (idx == nullptr && max_rows != T) return MOSAIC_ERR_INVALID_ARG;
+  MOSAIC_RETURN_IF(check_optional(dw, ld_dw, d));
+  const bool some = T > 0 && max_rows > 0;
+  if (some) {
+    if ((dx == nullptr && dw == nullptr) || (dlogprob == nullptr && dentropy == nullptr) || lse == nullptr ||
+        (dlogprob != nullptr && (targets == nullptr || logprob == nullptr)) || (dentropy != nullptr && entropy == nullptr))
+      return MOSAIC_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)idx, (const void*)count, (const void*)targets, (const void*)logprob, (const void*)entropy,
+                          (const void*)lse, (const void*)dlogprob, (const void*)dentropy})
+      if (misaligned(p, 4)) return MOSAIC_ERR_INVALID_ARG;
+    MOSAIC_RETURN_IF(check_matrix(hidden, ld_h, d));
+    MOSAIC_RETURN_IF(check_matrix(w, ld_w, d));
+    MOSAIC_RETURN_IF(check_optional(dx, ld_dx, d));
+    if (workspace == nullptr || misaligned(workspace)) return MOSAIC_ERR_INVALID_ARG;
+    if (workspace_bytes < mosaic::logprob_backward_least_bytes(max_rows, d, V)) return MOSAIC_ERR_WORKSPACE_TOO_SMALL;
+  }
+  hipStream_t on = static_cast<hipStream_t>(stream);
+  if (!some) {   // no rows: dw is cleared
+    if (dw == nullptr || accumulate != 0) return MOSAIC_OK;
+    mosaic::TokenSumArgs none = {};
+    none.sums = dw;
+    none.ld_sums = ld_dw;
+    none.V = V;
+    none.d = d;
+    return launched(mosaic::launch_token_sums(none, false, dw_type == MOSAIC_F32, on));
+  }
+  mosaic::LogprobBackwardArgs a = {};
+  a.hidden = hidden;
+  a.w = w;
+  a.idx = idx;
+  a.count = count;
+  a.targets = dlogprob != nullptr ? targets : nullptr;
+  a.logprob = logprob;
+  a.entropy = entropy;
+  a.lse = lse;
+  a.dlogprob = dlogprob;
+  a.dentropy = dentropy;
+  a.dx = dx;
+  a.dw = dw;
+  a.workspace = workspace;
+  a.ld_h = ld_h;
+  a.ld_w = ld_w;
+  a.ld_dx = ld_dx;
+  a.ld_dw = ld_dw;
+  a.T = T;
+  a.max_rows = max_rows;
+  a.workspace_bytes = workspace_bytes;
+  a.d = d;
+  a.V = V;
+  a.dw_f32 = dw_type == MOSAIC_F32;
+  a.accumulate = accumulate != 0;
+  return launched(mosaic::launch_logprobs_backward(a, on));
+}
+
 }  // extern "C"

@@ -76,5 +76,22 @@ struct LogprobArgs {
 int64_t logprob_workspace_bytes(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, int32_t n_top);
 int launch_logprobs(const LogprobArgs& a, hipStream_t stream);
 
+struct LogprobBackwardArgs {
+  const void* hidden;
+  const void* w;
+  const int32_t* idx;        // or nullptr
+  const int32_t* count;      // or nullptr
+  const int32_t* targets;    // with dlogprob and logprob, or nullptr
+  const float *logprob, *entropy, *lse, *dlogprob, *dentropy;   // entropy and dentropy: or nullptr
+  void* dx;                  // bf16, or nullptr
+  void* dw;                  // or nullptr
+  void* workspace;
+  int64_t ld_h, ld_w, ld_dx, ld_dw, T, max_rows, workspace_bytes;
+  int32_t d, V, dw_f32, accumulate;
+};
+int64_t logprob_backward_workspace_bytes(int64_t max_rows, int32_t d, int32_t V, int64_t budget_bytes);
+int64_t logprob_backward_least_bytes(int64_t max_rows, int32_t d, int32_t V);
+int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream);
+
 }  // namespace mosaic
 #endif
