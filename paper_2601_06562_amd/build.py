@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmosaic.so")
 SOURCES = ["mosaic_api.hip", "mosaic_compact.hip", "mosaic_logits.hip", "mosaic_unmask.hip", "mosaic_probe.hip", "mosaic_vmm.hip",
            "mosaic_plan.cpp", "mosaic_graph.cpp", "mosaic_layer_api.hip", "mosaic_norm.hip", "mosaic_ffn.hip", "mosaic_tokens_api.hip",
-           "mosaic_embed.hip", "mosaic_logprob.hip"]
+           "mosaic_embed.hip", "mosaic_logprob.hip", "mosaic_logprob_w4.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,7 +1,8 @@
 #!/usr/bin/env python3
 """Generates mosaic_w4_tile.inc (greedy) and mosaic_w4_tile_sample.inc (sampling): one vocabulary tile of the 4-wave
 fused kernel as one inline-asm statement, the hand-scheduled K-loop followed by the tile's vocabulary reduction, for
-each width of the row tile (32*NB tokens, NB = 1..8, chosen by `if constexpr`).
+each width of the row tile (32*NB tokens, NB = 1..8, chosen by `if constexpr`); mosaic_w4_products.inc, the K-loop alone, and
+mosaic_w4_columns.inc, the logits it leaves in the accumulators (log probabilities of given tokens, mosaic_logprob_w4.hip).
 
 The K-loop covers the nk K-tiles of the vocabulary tile.  Per K-tile (step g) a wave issues 16*nb
 v_mfma_f32_16x16x32_bf16: its 128 vocabulary ids (8 blocks) against its half of the tokens (nb blocks), both K-halves of
@@ -1060,11 +1061,14 @@ def build_pairs():
     e("s_mov_b32 %[hsrc_hi], s99")
 
 
-def write_statement(f, blocks, sample):
+def write_statement(f, blocks, sample, products=False):
     SHAPE["nb"] = blocks
     lines.clear()
-    uid[0] = 2000 if sample else 1000
-    if sample:
+    uid[0] = 3000 if products else 2000 if sample else 1000
+    if products:                                      # the K-loop alone: its results are the accumulators, 32 a vector
+        build_pairs() if pairs() else build()
+        outs = [f'"={{a[{32 * k}:{32 * k + 31}]}}"(acc[{k}])' for k in range(blocks)]
+    elif sample:
         build_tile_sample()
         outs = []
         for tb in range(blocks):
@@ -1093,8 +1097,11 @@ def write_statement(f, blocks, sample):
     for name in ("total", "nk", "wwrap", "hwrap"):
         ins.append(f'[{name}] "s"(st_{name})')
     clob = ['"s94"', '"s95"', '"s96"', '"s97"', '"s98"', '"s99"', '"vcc"', '"scc"', '"m0"', '"memory"']
-    ins += ['[vb] "v"(vb)', '[first] "s"(st_first)', '[nt] "n"(STREAM ? 1 : 0)']
-    clob = [f'"a{i}"' for i in range(32 * blocks)] + [f'"s{i}"' for i in range(88, 94)] + clob
+    if not products:
+        ins += ['[vb] "v"(vb)', '[first] "s"(st_first)']
+    ins.append('[nt] "n"(STREAM ? 1 : 0)')
+    if not products:
+        clob = [f'"a{i}"' for i in range(32 * blocks)] + [f'"s{i}"' for i in range(88, 94)] + clob
     if sample:
         ins += [f'[pos{tb}] "v"(pos[{tb}])' for tb in range(blocks)]
         ins += ['[rb] "s"(row_best)', '[rl] "s"(last_row)']
@@ -1111,6 +1118,20 @@ def write_statement(f, blocks, sample):
     f.write("    : " + ",\n      ".join(outs) + "\n")
     f.write("    : " + ",\n      ".join(ins) + "\n")
     f.write("    : " + ", ".join(clob) + ");\n}\n")
+
+
+def write_columns(f, blocks):
+    """the 32 logits of column `j` of a finished tile, out of the accumulators, which stay where the K-loop's statement left
+    them: both name the same registers"""
+    SHAPE["nb"] = blocks
+    f.write(f"if constexpr (NB == {blocks}) {{\nswitch (j) {{\n")
+    for j in range(blocks):
+        f.write(f"case {j}: asm volatile(\n")
+        for el in range(32):
+            f.write(f'    "v_accvgpr_read_b32 %{el}, {acc_reg(el // 4, j, el % 4)}\\n"\n')
+        f.write("    : " + ", ".join(f'"=&v"(x[{el}])' for el in range(32)) + "\n")
+        f.write("    : " + ", ".join(f'"{{a[{32 * k}:{32 * k + 31}]}}"(acc[{k}])' for k in range(blocks)) + "); break;\n")
+    f.write("}\n}\n")
 
 
 def write_pieces(f):
@@ -1133,6 +1154,15 @@ def main(folder):
                     f"{'sampling' if sample else 'greedy'} 4-wave kernel, K-loop and vocabulary reduction, per width.\n")
             for blocks in range(1, 9):
                 write_statement(f, blocks, sample)
+    with open(os.path.join(folder, "mosaic_w4_products.inc"), "w") as f:
+        f.write("// GENERATED by gen_w4_loop.py -- do not edit.  One vocabulary tile of the 4-wave kernels that work on the logits "
+                "themselves, the K-loop alone, per width.\n")
+        for blocks in range(1, 9):
+            write_statement(f, blocks, False, products=True)
+    with open(os.path.join(folder, "mosaic_w4_columns.inc"), "w") as f:
+        f.write("// GENERATED by gen_w4_loop.py -- do not edit.  A column of the tile that mosaic_w4_products.inc makes, per width.\n")
+        for blocks in range(1, 9):
+            write_columns(f, blocks)
     with open(os.path.join(folder, "mosaic_w4_pieces.inc"), "w") as f:
         write_pieces(f)
 

@@ -8,53 +8,15 @@
 #include <limits.h>
 #include <stdint.h>
 
-#include "mosaic_tile.h"
-#include "mosaic_tokens_internal.h"
+#include "mosaic_logprob_rows.h"
 
 namespace mosaic {
 namespace {
 
-using namespace tile;
+using namespace logprob;
 
-constexpr int kCus = 256;
-constexpr int kVocab = 256;            // ids of a tile
-constexpr int kHalf = kVocab / 2;      // ids of a wave's half
 constexpr int kMostSplits = 256;       // parts of the vocabulary
 constexpr int kMostUnits = 512;        // units, where there is more than one part
-constexpr float kNeg = -0x1p100f;      // "minus infinity" that survives subtraction
-constexpr float kLog2e = 1.4426950408889634f;
-// A wave's list of candidates for a row's alternatives: what a compression leaves, and all that one tile can add.
-constexpr int kMostTop = MOSAIC_MAX_TOP;
-constexpr int kListRoom = kHalf + kMostTop;
-
-struct Candidate { float x; int32_t id; };
-
-struct LogitParams {
-  const char* w;
-  const char* x;
-  int64_t ld_w, ld_x;        // bytes
-  const int32_t* idx;        // or nullptr: x holds the listed rows side by side
-  const int32_t* count;      // or nullptr
-  const int32_t* targets;    // or nullptr
-  int32_t T, max_rows, V, d, n_top;
-  // statistics: of the halves of every part of the vocabulary, rows side by side
-  float *part_m, *part_s, *part_t;
-  Candidate* part_top;       // n_top each
-  float* target_logit;       // [max_rows]
-  Candidate* lists;          // of every block's waves and rows, kListRoom each
-  // gradients: of V ids from `first_id` on, for max_rows rows (zeros from the last listed one on)
-  const float *lse, *entropy, *dlogprob, *dentropy;   // the last three each with what needs them, else nullptr
-  char* dl;                  // bf16 [max_rows, ld_dl]
-  int64_t ld_dl, low;        // bytes; low: from a row to what its rounding left over, 0: not wanted
-  int32_t first_id, all_ids;
-};
-enum { kStatistics, kGradients };
-
-__device__ __forceinline__ int rows_found(const LogitParams& p) {
-  if (p.count == nullptr) return p.max_rows;
-  const int n = *p.count;
-  return n < 0 ? 0 : n < p.max_rows ? n : p.max_rows;
-}
 
 // Rows of a tile for so many rows, by what a step of 64 k takes: 256 rows 1.50 us, 128 rows 0.92.
 __host__ __device__ inline int tile_rows(int64_t rows) {
@@ -106,232 +68,6 @@ struct RowCopier {
   }
 };
 
-// Over the four lanes that hold one row (16 apart).
-__device__ __forceinline__ float row_max(float x) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float row_min(float x) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  const float y = fminf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
-  return fminf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float row_sum(float x) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  const float y = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
-// The largest number below x (of those that are no denormals).
-__device__ __forceinline__ float below(float x) {
-  const int b = __float_as_int(x);
-  if (__builtin_fabsf(x) < 0x1p-125f) return -0x1p-125f;
-  return __int_as_float(b > 0 ? b - 1 : b + 1);
-}
-
-// What a lane holds between tiles, of one row of its wave: of column block g = lane / 16 (with QB column blocks, g % QB).
-//   m, s, t   the largest logit, sum e^(x - m), sum (x - m) e^(x - m)
-//   tau       ids of later tiles with a logit of tau or less are none of the n_top best of this half
-//   n         candidates in the list
-struct RowState { float m, s, t, tau; int n; };
-
-// Sorts a row's candidates and keeps the n best, in `to`: by logit, then by id.  A lane takes a row.
-template <int N>
-__device__ __forceinline__ void keep_best(RowState& st, const Candidate* list, Candidate* to, int n) {
-  float x[N];
-  int id[N];
-#pragma unroll
-  for (int k = 0; k < N; ++k) { x[k] = -__builtin_inff(); id[k] = INT_MAX; }
-  for (int e = 0; e < st.n; e += 4) {
-    Candidate c[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = list[e + i < st.n ? e + i : e];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float cx = e + i < st.n ? c[i].x : -__builtin_inff();
-      int ci = e + i < st.n ? c[i].id : INT_MAX;
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const bool first = cx > x[k] || (cx == x[k] && ci < id[k]);
-        const float ox = x[k];
-        const int oi = id[k];
-        x[k] = first ? cx : ox;
-        id[k] = first ? ci : oi;
-        cx = first ? ox : cx;
-        ci = first ? oi : ci;
-      }
-    }
-  }
-  float last = kNeg;
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    if (k < n) {
-      to[k] = Candidate{x[k], id[k]};
-      last = x[k];
-    }
-  }
-  if (st.n >= n) {
-    st.n = n;
-    st.tau = fmaxf(last, kNeg);
-  }
-}
-
-// Reduces a finished tile into the rows' states.  v0: the id of this lane's first accumulator; row0: the first row of column
-// block 0 of its wave.
-template <int QB>
-__device__ __forceinline__ void reduce_tile(const LogitParams& p, f32x4_t (&acc)[8][QB], RowState& st, int64_t v0, int row0, int rows,
-                                            bool ragged, Candidate* lists) {
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, mine = g % QB;
-  int target[QB];
-#pragma unroll
-  for (int j = 0; j < QB; ++j) {
-    const int row = row0 + 16 * j + l16;
-    target[j] = p.targets != nullptr && row < rows ? p.targets[row] : -1;
-  }
-  if (ragged) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int j = 0; j < QB; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (v0 + 16 * i + r >= p.V) acc[i][j][r] = kNeg;
-  }
-  float own_m = 0.f, own_s = 0.f, own_t = 0.f;
-#pragma unroll
-  for (int j = 0; j < QB; ++j) {
-    float most[4];   // of quarters of the lane's ids
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float m = fmaxf(acc[2 * k][j][0], acc[2 * k + 1][j][0]);
-#pragma unroll
-      for (int r = 1; r < 4; ++r) m = fmaxf(fmaxf(m, acc[2 * k][j][r]), acc[2 * k + 1][j][r]);
-      most[k] = m;
-    }
-    const float lane_m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-    const float m = row_max(lane_m);
-    float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-#pragma unroll
-      for (int r = 0; r < 4; r += 2) {
-        const float u0 = acc[i][j][r] - m, u1 = acc[i][j][r + 1] - m;
-        const float e0 = __builtin_amdgcn_exp2f(u0 * kLog2e), e1 = __builtin_amdgcn_exp2f(u1 * kLog2e);
-        s0 += e0;
-        s1 += e1;
-        t0 = __builtin_fmaf(u0, e0, t0);
-        t1 = __builtin_fmaf(u1, e1, t1);
-      }
-    }
-    const float s = row_sum(s0 + s1), t = row_sum(t0 + t1);
-    own_m = mine == j ? m : own_m;
-    own_s = mine == j ? s : own_s;
-    own_t = mine == j ? t : own_t;
-
-    // the target's logit, in the one lane that holds it
-    const int64_t rel64 = target[j] - v0;
-    const bool here = target[j] >= 0 && target[j] < p.V && rel64 >= 0 && rel64 < kHalf && (rel64 & 15) < 4;
-    if (__any(here)) {
-      const int rel = here ? (int)rel64 : -1;
-      float x = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x = rel == 16 * i + r ? acc[i][j][r] : x;
-      if (here) p.target_logit[row0 + 16 * j + l16] = x;
-    }
-
-    if (p.n_top > 0) {
-      // Of n_top sets of ids the least of the sets' largest is no more than the n_top-th largest of all: 4, 8 or 16 sets.
-      float bound = lane_m;
-      if (p.n_top > 4) bound = fminf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-      if (p.n_top > 8) bound = fminf(fminf(most[0], most[1]), fminf(most[2], most[3]));
-      bound = row_min(bound);
-      const int from = 16 * j + l16;
-      float tau = fmaxf(__shfl(st.tau, from, 64), below(fmaxf(bound, kNeg)));
-      tau = row0 + from < rows ? fmaxf(tau, kNeg) : __builtin_inff();
-      int n = __shfl(st.n, from, 64);
-      if (__any(lane_m > tau)) {
-        Candidate* list = lists + from * kListRoom;
-        const uint64_t of_row = (uint64_t)0x0001000100010001 << l16, lower = ((uint64_t)1 << lane) - 1;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float most4 = fmaxf(fmaxf(acc[i][j][0], acc[i][j][1]), fmaxf(acc[i][j][2], acc[i][j][3]));
-          if (__any(most4 > tau)) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const bool hit = acc[i][j][r] > tau;
-              const uint64_t hits = __ballot(hit) & of_row;
-              const int at = n + __popcll(hits & lower);
-              if (hit && at < kListRoom) list[at] = Candidate{acc[i][j][r], (int32_t)(v0 + 16 * i + r)};
-              n += __popcll(hits);
-            }
-          }
-        }
-      }
-      st.n = mine == j ? n : st.n;
-    }
-  }
-  const float m = fmaxf(st.m, own_m);
-  const float a = __builtin_amdgcn_exp2f((st.m - m) * kLog2e), b = __builtin_amdgcn_exp2f((own_m - m) * kLog2e);
-  st.t = a * (st.t + st.s * (st.m - m)) + b * (own_t + own_s * (own_m - m));
-  st.s = a * st.s + b * own_s;
-  st.m = m;
-}
-
-// The gradient at a finished tile's logits, in 16 bits, as the matrix products behind take it:
-//   dl[v] = - p[v] (g + h (log p[v] + H))      g, h: the gradients of the row's log probability and entropy H
-// with 0 at the target, whose one-hot term outweighs the others; the target's whole term goes past the 16 bits (target_terms_kernel).
-template <int QB>
-__device__ __forceinline__ void gradient_tile(const LogitParams& p, f32x4_t (&acc)[8][QB], int64_t v0, int row0, int found) {
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, run = first_of<4>(lane);
-  const int64_t end = ((int64_t)p.V + 7) / 8 * 8;
-#pragma unroll
-  for (int j = 0; j < QB; ++j) {
-    const int row = row0 + 16 * j + l16;
-    const bool in = row < p.max_rows, listed = row < found;
-    const float lse = listed ? p.lse[row] : 0.f;
-    const int target = listed && p.targets != nullptr ? p.targets[row] : -1;
-    const float g = (uint32_t)target < (uint32_t)p.all_ids ? p.dlogprob[row] : 0.f;
-    const float h = listed && p.dentropy != nullptr ? p.dentropy[row] : 0.f;
-    const float entropy = listed && p.dentropy != nullptr ? p.entropy[row] : 0.f;
-    const int64_t from = (int64_t)target - p.first_id - v0;
-    const int rel = target >= 0 && from >= 0 && from < kHalf ? (int)from - 4 * g4 : -kHalf;   // from this lane's first id
-    const int there = p.V - v0 < kHalf ? (int)(p.V - v0) - 4 * g4 : kHalf;                     // ids there are from there on
-#pragma unroll
-    for (int b = 0; b < 8; b += 4) {
-      Quad o[4], low[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float v[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int at = 16 * (b + k) + r;
-          const float logp = acc[b + k][j][r] - lse;
-          const float prob = __builtin_amdgcn_exp2f(logp * kLog2e);
-          const float d = -prob * (p.dentropy != nullptr ? g + h * (logp + entropy) : g);
-          v[r] = listed && rel != at && at < there ? d : 0.f;
-        }
-        pack(o[k], v);
-        if constexpr (QB == 1) pack_low(low[k], o[k], v);
-      }
-      gather(o);
-      const int c = (int)(v0 + 16 * b) + run;
-      if (in) store_quads(p.dl + row * p.ld_dl, c, (int)end, o);
-      if constexpr (QB == 1) {   // the tiles that few rows take
-        if (p.low != 0) {
-          gather(low);
-          if (in) store_quads(p.dl + p.low + row * p.ld_dl, c, (int)end, low);
-        }
-      }
-    }
-  }
-}
-
 // All units of this block, in tiles of TQ rows.
 template <int MODE, int TQ, int SP, int SQ>
 __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int rows, int found) {
@@ -355,10 +91,10 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
   if (unit >= end) return;
   const int panel = row_tiles < 8 ? row_tiles : 8;
 
-  Candidate* const lists = p.lists == nullptr ? nullptr : p.lists + ((int64_t)blockIdx.x * 8 + wave) * (16 * QB) * kListRoom;
+  Candidate* const lists = p.lists == nullptr ? nullptr : p.lists + ((int64_t)blockIdx.x * 8 + wave) * (64 * QB) * kListRoom;
 
   // Of the tile whose copies are issued.
-  int part = 0, row0 = 0, vt = 0, vt_end = 0, turned = 0;
+  int part = 0, row0 = 0, vt = 0, vt_begin = 0, vt_end = 0, turned = 0;
   RowCopier<kCopiesP> cp;
   RowCopier<kCopiesQ> cq;
   cp.past = cq.past = 0;
@@ -371,7 +107,7 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
     const int deep = row_tiles - pn * panel < panel ? row_tiles - pn * panel : panel;
     part = in / deep;
     row0 = (pn * panel + in % deep) * TQ;
-    vt = (int)((int64_t)vocab_tiles * part / parts);
+    vt = vt_begin = (int)((int64_t)vocab_tiles * part / parts);
     vt_end = (int)((int64_t)vocab_tiles * (part + 1) / parts);
     if (p.idx == nullptr) q_base = p.x + (int64_t)row0 * p.ld_x;
 #pragma unroll
@@ -473,9 +209,20 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
     slot_q = to_q;
   };
 
-  RowState st = {kNeg, 0.f, 0.f, kNeg, 0};
-  int done_vt = -1, done_row0 = 0, done_part = 0, done_tiles = 0;   // the tile whose logits are in the accumulators
-  bool done_last = false, fresh = true;                              // the last of its unit; fresh: a unit is to be begun
+  if (MODE == kStatistics && blockIdx.x == 0 && threadIdx.x == 0) {
+    p.found[0] = 2 * parts;
+    p.found[1] = rows;
+  }
+  Rows<QB> st;
+  st.clear();
+  int done_vt = -1, done_row0 = 0, done_part = 0, done_tiles = 0, unit_tiles = 0;   // the tile whose logits are in the accumulators
+  bool done_last = false, fresh = true;                                             // the last of its unit; fresh: a unit is to be begun
+  auto load = [&](int j, float (&x)[32]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[4 * i + r] = acc[i][j][r];
+  };
   for (;;) {
     const bool more = unit < end;
     if (more) {
@@ -499,36 +246,33 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
       }
     }
     if (done_vt >= 0) {
-      const int64_t v = (int64_t)done_vt * kVocab;
+      const int64_t v = (int64_t)done_vt * kVocab + wp * kHalf;
       const int q0 = done_row0 + wq * 16 * QB, g = lane >> 4;
       if constexpr (MODE == kGradients) {
-        gradient_tile<QB>(p, acc, v + wp * kHalf, q0, found);
+        gradient_tile<QB, false>(load, v, q0, found);
       } else {
-        reduce_tile<QB>(p, acc, st, v + wp * kHalf + 4 * g, q0, rows, v + kVocab > p.V, lists);
+        const int own_row = q0 + 16 * g + (lane & 15);
+        const int target[1] = {g < QB && p.targets != nullptr && own_row < rows ? p.targets[own_row] : -1};
+        const int64_t of_half = (int64_t)(2 * done_part + wp) * rows;
+        auto place = [&](int k, bool& in) __attribute__((always_inline)) {
+          const int row = q0 + 16 * (4 * k + g) + (lane & 15);
+          in = in && row < rows;
+          const Arguments a = arguments_again();
+        return a->part_top + (of_half + (in ? row : 0)) * a->n_top;
+        };
         ++done_tiles;
-        const int64_t row = q0 + 16 * g + (lane & 15), of_half = 2 * done_part + wp;
-        const bool owner = g < QB && row < rows;
-        if (p.n_top > 0) {
-          const bool now = done_last || (done_tiles & (done_tiles - 1)) == 0 || __any(owner && st.n > kListRoom - kHalf);
-          if (now) {
-            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // the list's entries were stored by other lanes
-            if (owner) {
-              Candidate* list = lists + (16 * g + (lane & 15)) * kListRoom;
-              Candidate* to = done_last ? p.part_top + (of_half * rows + row) * p.n_top : list;
-              if (p.n_top <= 4) keep_best<4>(st, list, to, p.n_top);
-              else if (p.n_top <= 8) keep_best<8>(st, list, to, p.n_top);
-              else keep_best<16>(st, list, to, p.n_top);
-            }
-            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");
-          }
-        }
+        reduce_tile<QB, false>(load, st, v + 4 * g, 0, p.V, target, q0, rows, lists, sort_now(done_tiles, unit_tiles), place);
         if (done_last) {
-          if (owner) {
-            p.part_m[of_half * rows + row] = st.m;
-            p.part_s[of_half * rows + row] = st.s;
-            p.part_t[of_half * rows + row] = st.t;
+#pragma unroll
+          for (int k = 0; k < Rows<QB>::kOwn; ++k) {
+            const int row = q0 + 16 * (4 * k + g) + (lane & 15);
+            if (4 * k + g < QB && row < rows) {
+              p.part_e[of_half + row] = st.e[k];
+              p.part_s[of_half + row] = st.s[k];
+              p.part_t[of_half + row] = st.t[k];
+            }
           }
-          st = RowState{kNeg, 0.f, 0.f, kNeg, 0};
+          st.clear();
           done_tiles = 0;
         }
       }
@@ -599,6 +343,7 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
     done_vt = vt;
     done_row0 = row0;
     done_part = part;
+    unit_tiles = vt_end - vt_begin;
     done_last = fresh = ++vt == vt_end;
     if (fresh) unit += stride;
   }
@@ -628,6 +373,7 @@ struct JoinParams {
   LogitParams l;
   float *out_logprob, *out_entropy, *out_lse, *top_logprob;
   int32_t* top_id;
+  int64_t entries;   // of the parts' arrays
 };
 template <typename T, typename F>
 __device__ __forceinline__ T over_block(T v, T* lds, F f) {
@@ -647,30 +393,34 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(const JoinPa
   __shared__ long long lds_l[kJoinThreads / 64];
   const LogitParams& l = p.l;
   const int rows = rows_found(l);
-  const int tile = tile_rows(rows);
-  const int vocab_tiles = (int)(((int64_t)l.V + kVocab - 1) / kVocab);
-  const int halves = rows > 0 ? 2 * choose_parts((rows + tile - 1) / tile, vocab_tiles, (l.d + kTileK - 1) / kTileK) : 0;
+  if (rows <= 0) return;
+  const int stride = l.found[1];
+  // (whatever another call on the same workspace left there, nobody is to be led beyond the arrays)
+  const int halves = stride >= rows && l.found[0] > 0 && (int64_t)l.found[0] * stride <= p.entries ? l.found[0] : 0;
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-    float m = kNeg;
-    for (int h = threadIdx.x; h < halves; h += kJoinThreads) m = fmaxf(m, l.part_m[(int64_t)h * rows + row]);
-    m = over_block(m, lds_f, [](float a, float b) { return fmaxf(a, b); });
+    float e = kNegExponent;
+    for (int h = threadIdx.x; h < halves; h += kJoinThreads) e = fmaxf(e, l.part_e[(int64_t)h * stride + row]);
+    e = over_block(e, lds_f, [](float a, float b) { return fmaxf(a, b); });
     double s = 0.0, t = 0.0;
     for (int h = threadIdx.x; h < halves; h += kJoinThreads) {
-      const int64_t at = (int64_t)h * rows + row;
-      const float pm = l.part_m[at], ps = l.part_s[at];
-      const float scale = __builtin_amdgcn_exp2f((pm - m) * kLog2e);
-      s += (double)scale * ps;
-      t += (double)scale * ((double)l.part_t[at] + (double)ps * (pm - m));
+      const int64_t at = (int64_t)h * stride + row;
+      const float by = l.part_e[at] - e, scale = __builtin_amdgcn_exp2f(by), part = l.part_s[at];
+      s += (double)(scale * part);
+      t += (double)scale * ((double)l.part_t[at] + (double)part * by);
     }
     s = over_block(s, lds_d, [](double a, double b) { return a + b; });
     t = over_block(t, lds_d, [](double a, double b) { return a + b; });
-    const float log_s = logf((float)s);
+    // back from powers of two, by the factor that the exponents were made with
+    const double log_s = log2(s), lse = ((double)e + log_s) / (double)kLog2e;
     if (threadIdx.x == 0) {
-      if (p.out_lse != nullptr) p.out_lse[row] = m + log_s;
-      if (p.out_entropy != nullptr) p.out_entropy[row] = log_s - (float)(t / s);
+      if (p.out_lse != nullptr) p.out_lse[row] = (float)lse;
+      // an entropy is never below zero, a log probability never above it, whatever the last bits of a certain row's sums say
+      const float entropy = (float)((log_s - t / s) / (double)kLog2e);
+      if (p.out_entropy != nullptr) p.out_entropy[row] = entropy < 0.f ? 0.f : entropy;
       if (p.out_logprob != nullptr) {
         const int target = l.targets[row];
-        p.out_logprob[row] = (uint32_t)target < (uint32_t)l.V ? (l.target_logit[row] - m) - log_s : 0.f;
+        const float logp = (uint32_t)target < (uint32_t)l.V ? (float)((double)l.target_logit[row] - lse) : 0.f;
+        p.out_logprob[row] = logp > 0.f ? 0.f : logp;
       }
     }
     // The best n_top of the parts' best: each time the first behind the one before, by logit, then by id.
@@ -679,10 +429,10 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(const JoinPa
     for (int k = 0; k < l.n_top; ++k) {
       float x = -__builtin_inff();
       int id = INT_MAX;
-      for (int e = threadIdx.x; e < halves * l.n_top; e += kJoinThreads) {
-        const Candidate c = l.part_top[((int64_t)(e / l.n_top) * rows + row) * l.n_top + e % l.n_top];
-        const bool behind = c.x < past_x || (c.x == past_x && c.id > past_id);
-        if (behind && (c.x > x || (c.x == x && c.id < id))) { x = c.x; id = c.id; }
+      for (int c = threadIdx.x; c < halves * l.n_top; c += kJoinThreads) {
+        const Candidate other = l.part_top[((int64_t)(c / l.n_top) * stride + row) * l.n_top + c % l.n_top];
+        const bool behind = other.x < past_x || (other.x == past_x && other.id > past_id);
+        if (behind && (other.x > x || (other.x == x && other.id < id))) { x = other.x; id = other.id; }
       }
       // as one number: logits in the order of integers, ids counted down
       const int b = __float_as_int(x);
@@ -694,7 +444,8 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(const JoinPa
       if (threadIdx.x == 0) {
         const bool some = past_id != INT_MAX;
         p.top_id[row * l.n_top + k] = some ? past_id : -1;
-        p.top_logprob[row * l.n_top + k] = some ? (past_x - m) - log_s : -__builtin_inff();
+        const float logp = some ? (float)((double)past_x - lse) : -__builtin_inff();
+        p.top_logprob[row * l.n_top + k] = logp > 0.f ? 0.f : logp;
       }
     }
   }
@@ -789,19 +540,30 @@ int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 // Where 32-bit offsets reach all hidden rows they are gathered as they are copied, else beforehand.
 bool far_rows(int64_t T, int64_t ld_h) { return T * ld_h * 2 > (int64_t)kOutside; }
 
-struct Space { int64_t lists, m, s, t, top, target, rows, total; };
-Space space_of(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t n_top) {
-  // of halves of parts and rows: up to kMostUnits units, at most kMostSplits parts, and one part whatever the rows
-  const int64_t tile = max_rows <= 64 ? 64 : max_rows <= 128 ? 128 : 256;
-  const int64_t most = (int64_t)kMostSplits * max_rows < kMostUnits * tile ? (int64_t)kMostSplits * max_rows : kMostUnits * tile;
-  const int64_t entries = 2 * (most > max_rows ? most : max_rows);
+struct Space { int64_t found, lists, e, s, t, top, target, rows, total, entries, slots; };
+Space space_of(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, int32_t n_top) {
   Space s;
-  s.lists = 0;
-  s.m = n_top > 0 ? (int64_t)kCus * 8 * (tile / 4) * kListRoom * (int64_t)sizeof(Candidate) : 0;
-  s.s = s.m + padded(4 * entries);
-  s.t = s.s + padded(4 * entries);
-  s.top = s.t + padded(4 * entries);
-  s.target = s.top + padded((int64_t)sizeof(Candidate) * entries * n_top);
+  const int64_t tile = max_rows <= 64 ? 64 : max_rows <= 128 ? 128 : 256;
+  int64_t lists;
+  if (w4_takes(d, V)) {   // as many parts as fill the chip at the bound; fewer rows have room for more
+    const int64_t row_tiles = (max_rows + 255) / 256;
+    s.slots = row_tiles * 256 * choose_vocab_splits(row_tiles, ((int64_t)V + kVocab - 1) / kVocab, kCus);
+    s.entries = 2 * s.slots;
+    lists = w4_list_bytes(max_rows);
+  } else {
+    // up to kMostUnits units, at most kMostSplits parts, and one part whatever the rows
+    const int64_t most = (int64_t)kMostSplits * max_rows < kMostUnits * tile ? (int64_t)kMostSplits * max_rows : kMostUnits * tile;
+    s.slots = most > max_rows ? most : max_rows;
+    s.entries = 2 * s.slots;
+    lists = (int64_t)kCus * 8 * tile * kListRoom * (int64_t)sizeof(Candidate);
+  }
+  s.found = 0;
+  s.lists = 256;
+  s.e = s.lists + (n_top > 0 ? lists : 0);
+  s.s = s.e + padded(4 * s.entries);
+  s.t = s.s + padded(4 * s.entries);
+  s.top = s.t + padded(4 * s.entries);
+  s.target = s.top + padded((int64_t)sizeof(Candidate) * s.entries * n_top);
   s.rows = s.target + padded(4 * max_rows);
   s.total = s.rows + (far_rows(T, ld_h) ? 2 * max_rows * d : 0);
   return s;
@@ -810,12 +572,11 @@ Space space_of(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t n_t
 }  // namespace
 
 int64_t logprob_workspace_bytes(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, int32_t n_top) {
-  (void)V;
-  return space_of(T, ld_h, max_rows, d, n_top).total;
+  return space_of(T, ld_h, max_rows, d, V, n_top).total;
 }
 
 int launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
-  const Space at = space_of(a.T, a.ld_h, a.max_rows, a.d, a.n_top);
+  const Space at = space_of(a.T, a.ld_h, a.max_rows, a.d, a.V, a.n_top);
   char* ws = static_cast<char*>(a.workspace);
   LogitParams p = {};
   p.w = static_cast<const char*>(a.w);
@@ -830,7 +591,8 @@ int launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
   p.V = a.V;
   p.d = a.d;
   p.n_top = a.n_top;
-  p.part_m = reinterpret_cast<float*>(ws + at.m);
+  p.found = reinterpret_cast<int32_t*>(ws + at.found);
+  p.part_e = reinterpret_cast<float*>(ws + at.e);
   p.part_s = reinterpret_cast<float*>(ws + at.s);
   p.part_t = reinterpret_cast<float*>(ws + at.t);
   p.part_top = reinterpret_cast<Candidate*>(ws + at.top);
@@ -846,8 +608,14 @@ int launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
     p.ld_x = (int64_t)a.d * 2;
     p.idx = nullptr;
   }
-  if (launch_kernel(logprob_kernel, dim3(kCus), dim3(kThreads), stream, p) != 0) return -1;
+  if (w4_takes(a.d, a.V)) {
+    p.sched.slots64 = (uint32_t)(at.slots / 64 < INT32_MAX ? at.slots / 64 : INT32_MAX);
+    if (launch_logprob_w4(p, stream) != 0) return -1;
+  } else if (launch_kernel(logprob_kernel, dim3(kCus), dim3(kThreads), stream, p) != 0) {
+    return -1;
+  }
   JoinParams j = {};
+  j.entries = at.entries;
   j.l = p;
   j.out_logprob = a.out_logprob;
   j.out_entropy = a.out_entropy;
@@ -895,9 +663,29 @@ int64_t ids_at_once(int64_t dl_rows, int32_t V, int64_t bytes) {
   return (((int64_t)V + parts - 1) / parts + kVocab - 1) / kVocab * kVocab;
 }
 
-template <int TQ, int SP, int SQ>
 int launch_gradient_tiles(const LogitParams& p, hipStream_t stream) {
-  return launch_kernel(logit_gradient_kernel<TQ, SP, SQ>, dim3(kCus), dim3(kThreads), stream, p);
+  const int tile = tile_rows(p.max_rows);
+  if (tile == 256) return launch_kernel(logit_gradient_kernel<256, 3, 2>, dim3(kCus), dim3(kThreads), stream, p);
+  if (tile == 128) return launch_kernel(logit_gradient_kernel<128, 3, 3>, dim3(kCus), dim3(kThreads), stream, p);
+  return launch_kernel(logit_gradient_kernel<64, 4, 4>, dim3(kCus), dim3(kThreads), stream, p);
+}
+
+// dl of `n` ids from v on: whole tiles of ids on the 4-wave kernel where it takes them.
+int launch_dl(LogitParams p, int64_t v, int64_t n, hipStream_t stream) {
+  const int64_t whole = w4_takes(p.d, kVocab) ? n / kVocab * kVocab : 0;
+  const char* w = p.w + v * p.ld_w;
+  char* dl = p.dl;
+  const int64_t parts[2][2] = {{0, whole}, {whole, n - whole}};
+  for (int k = 0; k < 2; ++k) {
+    if (parts[k][1] == 0) continue;
+    p.w = w + parts[k][0] * p.ld_w;
+    p.dl = dl + parts[k][0] * 2;
+    p.V = (int32_t)parts[k][1];
+    p.dl_ids = (p.V + 7) / 8 * 8;
+    p.first_id = (int32_t)(v + parts[k][0]);
+    if ((k == 0 ? launch_logit_gradients_w4(p, stream) : launch_gradient_tiles(p, stream)) != 0) return -1;
+  }
+  return 0;
 }
 
 }  // namespace
@@ -947,6 +735,7 @@ int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
   const int64_t each = ids_at_once(at.dl_rows, a.V, a.workspace_bytes - at.dl);
   const bool low = a.max_rows <= kLowRows;
   LogitParams p = {};
+  p.w = static_cast<const char*>(a.w);
   p.x = reinterpret_cast<const char*>(rows);
   p.ld_w = a.ld_w * 2;
   p.ld_x = (int64_t)a.d * 2;
@@ -965,16 +754,10 @@ int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
   p.all_ids = a.V;
   for (int64_t v = 0; v < a.V; v += each) {
     const int64_t n = a.V - v < each ? a.V - v : each;
-    p.w = static_cast<const char*>(a.w) + v * p.ld_w;
-    p.V = (int32_t)n;
-    p.first_id = (int32_t)v;
-    const int tile = tile_rows(a.max_rows);
-    const int rc = tile == 256 ? launch_gradient_tiles<256, 3, 2>(p, stream)
-                   : tile == 128 ? launch_gradient_tiles<128, 3, 3>(p, stream) : launch_gradient_tiles<64, 4, 4>(p, stream);
-    if (rc != 0) return -1;
+    if (launch_dl(p, v, n, stream) != 0) return -1;
     if (a.dx != nullptr) {
       ProductArgs x = {};
-      x.p = p.w;
+      x.p = p.w + v * p.ld_w;
       x.q = p.dl;
       x.out = parts;
       x.ld_p = a.ld_w;

@@ -1,0 +1,389 @@
+// What the kernels that make logits tile by tile do with them (mosaic_logprob.hip, mosaic_logprob_w4.hip): statistics of rows,
+// candidates for their most probable ids, gradients at the logits.  Device code.
+//
+// In both kernels a wave holds 128 ids of a tile by 16 QB rows, in blocks of 16 x 16: lane l has ids 16 i + 4 (l / 16) + r, i < 8,
+// r < 4, of rows 16 j + l % 16, j < QB ("columns").  A row of a wave lies in four lanes, 16 apart; what is kept of it between tiles
+// one of them holds, its owner: of column j lane group j % 4.  `load(j, x)` gives a column's 32 elements, x[4 i + r].  ROLLED:
+// columns are taken in a loop, so that the code is there once; where the compiler holds the accumulators it needs them unrolled.
+#ifndef MOSAIC_LOGPROB_ROWS_H_
+#define MOSAIC_LOGPROB_ROWS_H_
+
+#include <hip/hip_runtime.h>
+#include <limits.h>
+#include <stdint.h>
+
+#include "mosaic_schedule.h"
+#include "mosaic_tile.h"
+#include "mosaic_tokens_internal.h"
+
+namespace mosaic {
+namespace logprob {
+
+using namespace tile;
+
+constexpr int kCus = 256;
+constexpr int kVocab = 256;            // ids of a tile
+constexpr int kHalf = kVocab / 2;      // ids of a wave's half
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNeg = -0x1p100f;      // "minus infinity" that survives subtraction; a power of two, so that
+constexpr float kNegExponent = kNeg * kLog2e;   // this is exact
+constexpr int kMostTop = MOSAIC_MAX_TOP;
+constexpr int kListRoom = 16;          // candidates a lane keeps of a row until they are sorted in
+
+struct Candidate { float x; int32_t id; };
+
+struct LogitParams {
+  const char* w;
+  const char* x;
+  int64_t ld_w, ld_x;        // bytes
+  const int32_t* idx;        // or nullptr: x holds the listed rows side by side
+  const int32_t* count;      // or nullptr
+  const int32_t* targets;    // or nullptr
+  int32_t T, max_rows, V, d, n_top;
+  // statistics: of the halves of every part of the vocabulary (`found` says how many parts, and the rows of one)
+  float *part_e, *part_s, *part_t;
+  Candidate* part_top;       // n_top each
+  float* target_logit;       // [max_rows]
+  Candidate* lists;          // of every block's waves: kListRoom x columns x 64 lanes
+  int32_t* found;
+  ScheduleInput sched;       // mosaic_logprob_w4.hip
+  // gradients: of V ids from `first_id` on, for max_rows rows (zeros from the last listed one on)
+  const float *lse, *entropy, *dlogprob, *dentropy;   // the last three each with what needs them, else nullptr
+  char* dl;                  // bf16 [max_rows, ld_dl]
+  int64_t ld_dl, low;        // bytes; low: from a row to what its rounding left over, 0: not wanted
+  int32_t first_id, all_ids;
+  int32_t dl_ids;            // ids that dl holds, a multiple of 8
+};
+enum { kStatistics, kGradients };
+
+// A kernel's arguments, read where they are used: what is made of a tile uses many, and kept from one tile to the next they would
+// take the scalar registers that the products need.
+typedef const __attribute__((address_space(4))) LogitParams* Arguments;
+__device__ __forceinline__ Arguments arguments_again() {
+  auto at = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return (Arguments)at;
+}
+
+__device__ __forceinline__ int rows_found(const LogitParams& p) {
+  if (p.count == nullptr) return p.max_rows;
+  const int n = *p.count;
+  return n < 0 ? 0 : n < p.max_rows ? n : p.max_rows;
+}
+
+// Over the four lanes that hold one row.
+template <typename F>
+__device__ __forceinline__ float over_row(float x, F f) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float y = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float row_max(float x) { return over_row(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float row_min(float x) { return over_row(x, [](float a, float b) { return fminf(a, b); }); }
+__device__ __forceinline__ float row_sum(float x) { return over_row(x, [](float a, float b) { return a + b; }); }
+
+// The largest number below x (of those that are no denormals).
+__device__ __forceinline__ float below(float x) {
+  const int b = __float_as_int(x);
+  if (__builtin_fabsf(x) < 0x1p-125f) return -0x1p-125f;
+  return __int_as_float(b > 0 ? b - 1 : b + 1);
+}
+
+// What a lane holds between tiles, of rows 16 (4 k + lane / 16) + lane % 16 of its wave, k < kOwn.  With u = x log2 e - e, e a whole
+// number, so that a change of e only ever scales s by a power of two and u is rounded once:
+//   s, t   sum 2^u, sum u 2^u        (log-sum-exp: (e + log2 s) / log2 e;  entropy: (log2 s - t / s) / log2 e)
+//   tau    ids of later tiles with a logit of tau or less are none of the n_top best of this half
+//   n      candidates that are sorted in
+template <int QB>
+struct Rows {
+  static constexpr int kOwn = (QB + 3) / 4;
+  float e[kOwn], s[kOwn], t[kOwn], tau[kOwn];
+  int n[kOwn];
+  uint32_t listed[kOwn];   // of columns 4 k .. 4 k + 3, a byte each: candidates in this lane's own lists
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) { e[k] = kNegExponent; s[k] = t[k] = 0.f; tau[k] = kNeg; n[k] = 0; listed[k] = 0; }
+  }
+};
+
+// Element k of an array of one or two, k the same in all lanes.
+template <typename T, int N>
+__device__ __forceinline__ T pick(const T (&a)[N], int k) {
+  if constexpr (N == 1) return a[0];
+  else return k == 0 ? a[0] : a[1];
+}
+template <typename T, int N>
+__device__ __forceinline__ void put(T (&a)[N], int k, bool own, T v) {
+  a[0] = own && k == 0 ? v : a[0];
+  if constexpr (N > 1) a[1] = own && k == 1 ? v : a[1];
+}
+
+// Sorts the candidates of this lane's own row k into the n best of before, in part_top at `to`: by logit, then by id.
+template <int N, int QB>
+__device__ __forceinline__ void sort_in(Rows<QB>& st, int k, const Candidate* lists, Candidate* to, bool owner, int n) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const uint32_t own_lists = pick(st.listed, k);
+  int here[4], most = 0;   // of the row's four lanes
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    here[q] = __shfl((int)own_lists, l16 + 16 * q, 64) >> (8 * g) & 255;
+    most = here[q] > most ? here[q] : most;
+  }
+  const int before = pick(st.n, k);
+  int all = before;
+  float last = kNeg;
+  if (owner) {
+    const Candidate* from = lists + (int64_t)(4 * k + g) * kListRoom * 64 + l16;
+    float x[N];
+    int id[N];
+#pragma unroll
+    for (int m = 0; m < N; ++m) {
+      const Candidate c = to[m < before ? m : 0];
+      x[m] = m < before ? c.x : -__builtin_inff();
+      id[m] = m < before ? c.id : INT_MAX;
+    }
+    constexpr int kAtOnce = 4;   // of each lane's list
+#pragma unroll 1
+    for (int e = 0; e < most; e += kAtOnce) {
+      Candidate c[kAtOnce][4];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) c[i][q] = from[(e + i < kListRoom ? e + i : 0) * 64 + 16 * q];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bool in = e + i < here[q];
+          all += in ? 1 : 0;
+          float cx = in ? c[i][q].x : -__builtin_inff();
+          int ci = in ? c[i][q].id : INT_MAX;
+#pragma unroll
+          for (int m = 0; m < N; ++m) {
+            const bool first = cx > x[m] || (cx == x[m] && ci < id[m]);
+            const float ox = x[m];
+            const int oi = id[m];
+            x[m] = first ? cx : ox;
+            id[m] = first ? ci : oi;
+            cx = first ? ox : cx;
+            ci = first ? oi : ci;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < N; ++m) {
+      if (m < n) {
+        to[m] = Candidate{x[m], id[m]};
+        last = x[m];
+      }
+    }
+  }
+  put(st.n, k, owner, all < n ? all : n);
+  put(st.tau, k, owner && all >= n, fmaxf(last, kNeg));
+}
+
+// All own rows.  place(k, in): where the candidates of own row k go, and whether there is such a row.
+template <int QB, class Place>
+__device__ __forceinline__ void sort_all_in(Rows<QB>& st, const Candidate* lists, int n, Place place) {
+  const int g = (threadIdx.x & 63) >> 4;
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // the lists' entries were stored by other lanes
+#pragma unroll 1
+  for (int k = 0; k < Rows<QB>::kOwn; ++k) {
+    bool in = 4 * k + g < QB;
+    Candidate* to = place(k, in);
+    if (n <= 8) sort_in<8, QB>(st, k, lists, to, in, n);
+    else sort_in<16, QB>(st, k, lists, to, in, n);
+    put(st.listed, k, true, 0u);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // and are free for others
+}
+
+template <bool ROLLED, int N, class F>
+__device__ __forceinline__ void each_column(F f) {
+  if constexpr (ROLLED) {
+#pragma unroll 1
+    for (int j = 0; j < N; ++j) f(j);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f(j);
+  }
+}
+
+// Works a finished tile into the rows' states.  v0: the id of this lane's first element; ids below `from` and from `end` on are
+// not counted; target: of the own rows, less than 0: none.  place(k, in): where the candidates of own row k go.  now: whether the
+// candidates so far are sorted in at the end.
+template <int QB, bool ROLLED, class Load, class Place>
+__device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0, int64_t from, int64_t end,
+                                            const int (&target)[Rows<QB>::kOwn], int row0, int rows, Candidate* lists, bool now, Place place) {
+  constexpr int kOwn = Rows<QB>::kOwn;
+  const Arguments p = arguments_again();
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const bool whole = v0 - 4 * g >= from && v0 - 4 * g + kHalf <= end;      // (the same in all lanes)
+  const int lo = from > v0 ? (int)(from - v0) : 0, hi = end < v0 + kHalf ? (int)(end - v0) : kHalf;
+  float tau[kOwn];         // of the own rows: what candidates of this tile have to pass
+  uint32_t next[kOwn];     // of columns 4 k .., a byte each: the first quad of this lane that is still to be looked at
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) { tau[k] = 0.f; next[k] = 0; }
+  for (bool again = false;; again = true) {
+    bool full = false;
+    each_column<ROLLED, QB>([&](int j) __attribute__((always_inline)) {
+      const int k = j >> 2, at = 8 * (j & 3), owner = 16 * (j & 3) + l16;
+      const bool own = g == (j & 3);
+      float x[32];
+      load(j, x);
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[4 * i + r] = 16 * i + r >= lo && 16 * i + r < hi ? x[4 * i + r] : kNeg;
+      }
+      if (!again) {
+        float most[4];   // of quarters of the lane's ids
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          most[m] = x[8 * m];
+#pragma unroll
+          for (int r = 1; r < 8; ++r) most[m] = fmaxf(most[m], x[8 * m + r]);
+        }
+        const float lane_m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+        const float e = __builtin_ceilf(fmaxf(row_max(lane_m), kNeg) * kLog2e);
+        float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const float u = __builtin_fmaf(x[i], kLog2e, -e), z = __builtin_amdgcn_exp2f(u);
+          s[i & 3] += z;
+          t[i & 3] = __builtin_fmaf(u, z, t[i & 3]);
+        }
+        const float row_s = row_sum((s[0] + s[1]) + (s[2] + s[3])), row_t = row_sum((t[0] + t[1]) + (t[2] + t[3]));
+        const float old_e = pick(st.e, k), old_s = pick(st.s, k), to = fmaxf(old_e, e);
+        const float a = __builtin_amdgcn_exp2f(old_e - to), b = __builtin_amdgcn_exp2f(e - to);
+        put(st.t, k, own, a * (pick(st.t, k) + old_s * (old_e - to)) + b * (row_t + row_s * (e - to)));
+        put(st.s, k, own, a * old_s + b * row_s);
+        put(st.e, k, own, to);
+
+        // the target's logit, in the one lane that holds it
+        const int wanted = __shfl(pick(target, k), owner, 64);
+        const int64_t rel64 = wanted - v0;
+        const bool here = wanted >= 0 && rel64 >= lo && rel64 < hi && (rel64 & 15) < 4;
+        if (__any(here)) {
+          const int rel = here ? (int)rel64 : -1;
+          float logit = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) logit = rel == 16 * i + r ? x[4 * i + r] : logit;
+          if (here) p->target_logit[row0 + 16 * j + l16] = logit;
+        }
+        if (p->n_top > 0) {
+          // Of n_top sets of ids the least of the sets' largest is no more than the n_top-th largest of all: 4, 8 or 16 sets.
+          float bound = lane_m;
+          if (p->n_top > 4) bound = fminf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+          if (p->n_top > 8) bound = fminf(fminf(most[0], most[1]), fminf(most[2], most[3]));
+          bound = fmaxf(row_min(bound), kNeg);
+          const float known = __shfl(pick(st.tau, k), owner, 64);
+          put(tau, k, own, row0 + 16 * j + l16 < rows ? fmaxf(fmaxf(known, below(bound)), kNeg) : __builtin_inff());
+        }
+      }
+      if (p->n_top == 0) return;
+      // Candidates go to this lane's own list of the column.  Where it is full the lane stops at the quad that does not fit, and goes
+      // on there once all have been sorted in.
+      const float pass = __shfl(pick(tau, k), owner, 64);
+      int done = (int)(pick(next, k) >> at & 255), n = (int)(pick(st.listed, k) >> at & 255);
+      bool stopped = false;
+      Candidate* list = lists + (int64_t)j * kListRoom * 64 + lane;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool want = fmaxf(fmaxf(x[4 * i], x[4 * i + 1]), fmaxf(x[4 * i + 2], x[4 * i + 3])) > pass && i >= done && !stopped;
+        if (__any(want)) {
+          stopped = stopped || (want && n > kListRoom - 4);
+          done = want && stopped ? i : done;
+          if (want && !stopped) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              if (x[4 * i + r] > pass) {
+                list[n * 64] = Candidate{x[4 * i + r], (int32_t)(v0 + 16 * i + r)};
+                ++n;
+              }
+            }
+          }
+        }
+      }
+      full = full || stopped;
+      put(next, k, true, (pick(next, k) & ~(255u << at)) | (uint32_t)(stopped ? done : 8) << at);
+      put(st.listed, k, true, (pick(st.listed, k) & ~(255u << at)) | (uint32_t)n << at);
+    });
+    const bool more = __any(full);
+    if (p->n_top > 0 && (more || now)) sort_all_in(st, lists, p->n_top, place);
+    if (!more) return;
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) tau[k] = fmaxf(tau[k], below(st.tau[k]));   // an id of this tile may equal the n_top-th best and come before it
+  }
+}
+
+// Whether the candidates of a unit's `tiles` tiles so far are sorted in now: after 1, 2, 4, 8, ... of them, of a long unit, and at its
+// end.
+__device__ __forceinline__ bool sort_now(int tiles, int of) { return tiles == of || (of > 2 && (tiles & (tiles - 1)) == 0); }
+
+// The gradient at a finished tile's logits, in 16 bits, as the matrix products behind take it:
+//   dl[v] = - p[v] (g + h (log p[v] + H))      g, h: the gradients of the row's log probability and entropy H
+// with 0 at the target, whose one-hot term outweighs the others; the target's whole term goes past the 16 bits.
+// v0: the first id of the wave.
+template <int QB, bool ROLLED, class Load>
+__device__ __forceinline__ void gradient_tile(Load load, int64_t v0, int row0, int found) {
+  const Arguments p = arguments_again();
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, run = first_of<4>(lane);
+  const int there = p->V - v0 < kHalf ? (int)(p->V - v0) - 4 * g4 : kHalf;   // ids there are from this lane's first on
+  each_column<ROLLED, QB>([&](int j) __attribute__((always_inline)) {
+    const int row = row0 + 16 * j + l16;
+    const bool in = row < p->max_rows, listed = row < found;
+    const float lse = listed ? p->lse[row] : 0.f;
+    const int target = listed && p->targets != nullptr ? p->targets[row] : -1;
+    const float g = (uint32_t)target < (uint32_t)p->all_ids ? p->dlogprob[row] : 0.f;
+    const float h = listed && p->dentropy != nullptr ? p->dentropy[row] : 0.f;
+    const float entropy = listed && p->dentropy != nullptr ? p->entropy[row] : 0.f;
+    const int64_t from = (int64_t)target - p->first_id - v0;
+    const int rel = target >= 0 && from >= 0 && from < kHalf ? (int)from - 4 * g4 : -kHalf;
+    float x[32];
+    load(j, x);
+#pragma unroll
+    for (int b = 0; b < 8; b += 4) {
+      Quad o[4], low[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int at = 16 * (b + k) + r;
+          const float logp = x[4 * (b + k) + r] - lse;
+          const float prob = __builtin_amdgcn_exp2f(logp * kLog2e);
+          const float d = -prob * (p->dentropy != nullptr ? g + h * (logp + entropy) : g);
+          v[r] = listed && rel != at && at < there ? d : 0.f;
+        }
+        pack(o[k], v);
+        if constexpr (QB == 1) pack_low(low[k], o[k], v);
+      }
+      gather(o);
+      const int c = (int)(v0 + 16 * b) + run;
+      if (in) store_quads(p->dl + row * p->ld_dl, c, p->dl_ids, o);
+      if constexpr (QB == 1) {   // the tiles that few rows take
+        if (p->low != 0) {
+          gather(low);
+          if (in) store_quads(p->dl + p->low + row * p->ld_dl, c, p->dl_ids, low);
+        }
+      }
+    }
+  });
+}
+
+// mosaic_logprob_w4.hip: whether its kernels take these sizes, and their launches.
+bool w4_takes(int32_t d, int32_t V);
+int launch_logprob_w4(const LogitParams& p, hipStream_t stream);
+int launch_logit_gradients_w4(const LogitParams& p, hipStream_t stream);
+int64_t w4_list_bytes(int64_t max_rows);
+
+}  // namespace logprob
+}  // namespace mosaic
+#endif
