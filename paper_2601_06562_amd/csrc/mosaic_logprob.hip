@@ -214,7 +214,6 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
     p.found[1] = rows;
   }
   Rows<QB> st;
-  st.clear();
   int done_vt = -1, done_row0 = 0, done_part = 0, done_tiles = 0, unit_tiles = 0;   // the tile whose logits are in the accumulators
   bool done_last = false, fresh = true;                                             // the last of its unit; fresh: a unit is to be begun
   auto load = [&](int j, float (&x)[32]) __attribute__((always_inline)) {
@@ -251,6 +250,7 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
       if constexpr (MODE == kGradients) {
         gradient_tile<QB, false>(load, v, q0, found);
       } else {
+        if (done_tiles == 0) st.clear(q0, rows);
         const int own_row = q0 + 16 * g + (lane & 15);
         const int target[1] = {g < QB && p.targets != nullptr && own_row < rows ? p.targets[own_row] : -1};
         const int64_t of_half = (int64_t)(2 * done_part + wp) * rows;
@@ -261,7 +261,7 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
         return a->part_top + (of_half + (in ? row : 0)) * a->n_top;
         };
         ++done_tiles;
-        reduce_tile<QB, false>(load, st, v + 4 * g, 0, p.V, target, q0, rows, lists, sort_now(done_tiles, unit_tiles), place);
+        reduce_tile<QB, false>(load, st, v + 4 * g, 0, p.V, target, q0, lists, done_tiles == 1, sort_now(done_tiles, unit_tiles), place);
         if (done_last) {
 #pragma unroll
           for (int k = 0; k < Rows<QB>::kOwn; ++k) {
@@ -272,7 +272,6 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
               p.part_t[of_half + row] = st.t[k];
             }
           }
-          st.clear();
           done_tiles = 0;
         }
       }

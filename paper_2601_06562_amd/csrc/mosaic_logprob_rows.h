@@ -102,9 +102,17 @@ struct Rows {
   int n[kOwn];
   uint32_t listed[kOwn];   // of columns 4 k .. 4 k + 3, a byte each: candidates in this lane's own lists
 
-  __device__ __forceinline__ void clear() {
+  // row0: the wave's first row.  Rows past the last have no candidates.
+  __device__ __forceinline__ void clear(int row0, int rows) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) { e[k] = kNegExponent; s[k] = t[k] = 0.f; tau[k] = kNeg; n[k] = 0; listed[k] = 0; }
+    for (int k = 0; k < kOwn; ++k) {
+      e[k] = kNegExponent;
+      s[k] = t[k] = 0.f;
+      tau[k] = row0 + 64 * k + lane < rows ? kNeg : __builtin_inff();
+      n[k] = 0;
+      listed[k] = 0;
+    }
   }
 };
 
@@ -212,26 +220,134 @@ __device__ __forceinline__ void each_column(F f) {
   }
 }
 
+// Sorts N = 2, 4, 8, ... numbers that first fall and then rise, or the reverse, largest first.
+template <int N>
+__device__ __forceinline__ void sort_bitonic(float* v) {
+#pragma unroll
+  for (int half = N / 2; half >= 1; half /= 2) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if ((i & half) != 0) continue;
+      const float a = v[i], b = v[i + half];
+      v[i] = fmaxf(a, b);
+      v[i + half] = fminf(a, b);
+    }
+  }
+}
+// Sorts any eight, largest first.
+__device__ __forceinline__ void sort_eight(float (&v)[8]) {
+#pragma unroll
+  for (int n = 2; n <= 8; n *= 2) {
+#pragma unroll
+    for (int i = 0; i < 8; i += n) {   // every other run the other way round
+      if (n < 8 && (i & n) != 0) {
+#pragma unroll
+        for (int k = 0; k < n; ++k) v[i + k] = -v[i + k];
+      }
+#pragma unroll
+      for (int half = n / 2; half >= 1; half /= 2) {
+#pragma unroll
+        for (int k = 0; k < n; ++k) {
+          if ((k & half) != 0) continue;
+          const float x = v[i + k], y = v[i + k + half];
+          v[i + k] = fmaxf(x, y);
+          v[i + k + half] = fminf(x, y);
+        }
+      }
+      if (n < 8 && (i & n) != 0) {
+#pragma unroll
+        for (int k = 0; k < n; ++k) v[i + k] = -v[i + k];
+      }
+    }
+  }
+}
+// A number that at least n of a row's ids of this tile reach: the n-th largest (for n > 8 the 16th) of the largest of 32 sets of
+// four, q, eight of which lie in each of the row's lanes.  About 5.4, 9 and 22 of 128 ids reach it for n = 5, 8 and 16.
+__device__ __forceinline__ float reached_by(const float (&q)[8], int n) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = q[i];
+  sort_eight(v);
+  // with the lane 16 away: of both lanes' sorted lists, one reversed, the larger of each two are the eight largest
+  float lo[8], hi[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+    lo[i] = __uint_as_float(r[0]);
+    hi[i] = __uint_as_float(r[1]);
+  }
+  float first[16];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    first[i] = fmaxf(lo[i], hi[7 - i]);
+    first[8 + i] = fminf(lo[i], hi[7 - i]);
+  }
+  sort_bitonic<8>(first);
+  float bound;
+  if (n <= 8) {
+    float top[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(first[i]), __float_as_uint(first[i]), false, false);
+      lo[i] = __uint_as_float(r[0]);
+      hi[i] = __uint_as_float(r[1]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top[i] = fmaxf(lo[i], hi[7 - i]);
+    sort_bitonic<8>(top);
+    bound = top[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) bound = i < n ? top[i] : bound;
+  } else {
+    sort_bitonic<8>(first + 8);
+    float low[16], high[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(first[i]), __float_as_uint(first[i]), false, false);
+      low[i] = __uint_as_float(r[0]);
+      high[i] = __uint_as_float(r[1]);
+    }
+    bound = fmaxf(low[0], high[15]);
+#pragma unroll
+    for (int i = 1; i < 16; ++i) bound = fminf(bound, fmaxf(low[i], high[15 - i]));
+  }
+  return bound;
+}
+
 // Works a finished tile into the rows' states.  v0: the id of this lane's first element; ids below `from` and from `end` on are
-// not counted; target: of the own rows, less than 0: none.  place(k, in): where the candidates of own row k go.  now: whether the
-// candidates so far are sorted in at the end.
+// not counted; target: of the own rows, less than 0: none.  begins: the first tile of its unit.  now: whether the candidates so far
+// are sorted in at the end.  place(k, in): where the candidates of own row k go.
 template <int QB, bool ROLLED, class Load, class Place>
 __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0, int64_t from, int64_t end,
-                                            const int (&target)[Rows<QB>::kOwn], int row0, int rows, Candidate* lists, bool now, Place place) {
+                                            const int (&target)[Rows<QB>::kOwn], int row0, Candidate* lists, bool begins, bool now,
+                                            Place place) {
   constexpr int kOwn = Rows<QB>::kOwn;
   const Arguments p = arguments_again();
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const int n_top = p->n_top;
   const bool whole = v0 - 4 * g >= from && v0 - 4 * g + kHalf <= end;      // (the same in all lanes)
   const int lo = from > v0 ? (int)(from - v0) : 0, hi = end < v0 + kHalf ? (int)(end - v0) : kHalf;
+  int wanted[kOwn];        // of the own rows: where the target lies in the half, from its first id on, or -1
+  bool some = false;
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {
+    const int64_t at = (int64_t)target[k] - (v0 - 4 * g);
+    wanted[k] = target[k] >= 0 && at >= 0 && at < kHalf ? (int)at : -1;
+    some = some || wanted[k] >= 0;
+  }
+  some = __any(some);
+  float tile_e[kOwn], tile_s[kOwn], tile_t[kOwn];
   float tau[kOwn];         // of the own rows: what candidates of this tile have to pass
   uint32_t next[kOwn];     // of columns 4 k .., a byte each: the first quad of this lane that is still to be looked at
 #pragma unroll
-  for (int k = 0; k < kOwn; ++k) { tau[k] = 0.f; next[k] = 0; }
+  for (int k = 0; k < kOwn; ++k) { tile_e[k] = kNegExponent; tile_s[k] = tile_t[k] = 0.f; tau[k] = st.tau[k]; next[k] = 0; }
   for (bool again = false;; again = true) {
     bool full = false;
     each_column<ROLLED, QB>([&](int j) __attribute__((always_inline)) {
       const int k = j >> 2, at = 8 * (j & 3), owner = 16 * (j & 3) + l16;
       const bool own = g == (j & 3);
+      float pass = 0.f;
+      if (n_top > 0) pass = __shfl(pick(tau, k), owner, 64);
       float x[32];
       load(j, x);
       if (!whole) {
@@ -240,15 +356,11 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
 #pragma unroll
           for (int r = 0; r < 4; ++r) x[4 * i + r] = 16 * i + r >= lo && 16 * i + r < hi ? x[4 * i + r] : kNeg;
       }
+      float most[8];       // of quads
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most[i] = fmaxf(fmaxf(fmaxf(x[4 * i], x[4 * i + 1]), x[4 * i + 2]), x[4 * i + 3]);
       if (!again) {
-        float most[4];   // of quarters of the lane's ids
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          most[m] = x[8 * m];
-#pragma unroll
-          for (int r = 1; r < 8; ++r) most[m] = fmaxf(most[m], x[8 * m + r]);
-        }
-        const float lane_m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+        const float lane_m = fmaxf(fmaxf(fmaxf(fmaxf(most[0], most[1]), most[2]), fmaxf(fmaxf(most[3], most[4]), most[5])), fmaxf(most[6], most[7]));
         const float e = __builtin_ceilf(fmaxf(row_max(lane_m), kNeg) * kLog2e);
         float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -257,46 +369,39 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
           s[i & 3] += z;
           t[i & 3] = __builtin_fmaf(u, z, t[i & 3]);
         }
-        const float row_s = row_sum((s[0] + s[1]) + (s[2] + s[3])), row_t = row_sum((t[0] + t[1]) + (t[2] + t[3]));
-        const float old_e = pick(st.e, k), old_s = pick(st.s, k), to = fmaxf(old_e, e);
-        const float a = __builtin_amdgcn_exp2f(old_e - to), b = __builtin_amdgcn_exp2f(e - to);
-        put(st.t, k, own, a * (pick(st.t, k) + old_s * (old_e - to)) + b * (row_t + row_s * (e - to)));
-        put(st.s, k, own, a * old_s + b * row_s);
-        put(st.e, k, own, to);
-
-        // the target's logit, in the one lane that holds it
-        const int wanted = __shfl(pick(target, k), owner, 64);
-        const int64_t rel64 = wanted - v0;
-        const bool here = wanted >= 0 && rel64 >= lo && rel64 < hi && (rel64 & 15) < 4;
-        if (__any(here)) {
-          const int rel = here ? (int)rel64 : -1;
+        put(tile_e, k, own, e);
+        put(tile_s, k, own, row_sum((s[0] + s[1]) + (s[2] + s[3])));
+        put(tile_t, k, own, row_sum((t[0] + t[1]) + (t[2] + t[3])));
+        if (some) {        // the target's logit, in the one lane that holds it
+          const int rel = __shfl(pick(wanted, k), owner, 64) - 4 * g;
           float logit = 0.f;
+          bool here = false;
 #pragma unroll
           for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) logit = rel == 16 * i + r ? x[4 * i + r] : logit;
-          if (here) p->target_logit[row0 + 16 * j + l16] = logit;
-        }
-        if (p->n_top > 0) {
-          // Of n_top sets of ids the least of the sets' largest is no more than the n_top-th largest of all: 4, 8 or 16 sets.
-          float bound = lane_m;
-          if (p->n_top > 4) bound = fminf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-          if (p->n_top > 8) bound = fminf(fminf(most[0], most[1]), fminf(most[2], most[3]));
-          bound = fmaxf(row_min(bound), kNeg);
-          const float known = __shfl(pick(st.tau, k), owner, 64);
-          put(tau, k, own, row0 + 16 * j + l16 < rows ? fmaxf(fmaxf(known, below(bound)), kNeg) : __builtin_inff());
+            for (int r = 0; r < 4; ++r) {
+              const bool it = rel == 16 * i + r;
+              logit = it ? x[4 * i + r] : logit;
+              here = here || it;
+            }
+          if (here && rel >= lo && rel < hi) p->target_logit[row0 + 16 * j + l16] = logit;
         }
       }
-      if (p->n_top == 0) return;
+      if (n_top == 0) return;
+      if (begins && !again) {
+        const float bound = below(fmaxf(reached_by(most, n_top), kNeg));
+        pass = fmaxf(fmaxf(pass, bound), kNeg);
+        put(tau, k, own, pass);
+      }
       // Candidates go to this lane's own list of the column.  Where it is full the lane stops at the quad that does not fit, and goes
       // on there once all have been sorted in.
-      const float pass = __shfl(pick(tau, k), owner, 64);
       int done = (int)(pick(next, k) >> at & 255), n = (int)(pick(st.listed, k) >> at & 255);
       bool stopped = false;
-      Candidate* list = lists + (int64_t)j * kListRoom * 64 + lane;
+      char* const list = reinterpret_cast<char*>(lists) + j * (kListRoom * 64 * (int)sizeof(Candidate));
+      uint32_t to = (uint32_t)(n * 64 + lane) * (uint32_t)sizeof(Candidate);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const bool want = fmaxf(fmaxf(x[4 * i], x[4 * i + 1]), fmaxf(x[4 * i + 2], x[4 * i + 3])) > pass && i >= done && !stopped;
+        const bool want = most[i] > pass && i >= done && !stopped;
         if (__any(want)) {
           stopped = stopped || (want && n > kListRoom - 4);
           done = want && stopped ? i : done;
@@ -304,7 +409,8 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               if (x[4 * i + r] > pass) {
-                list[n * 64] = Candidate{x[4 * i + r], (int32_t)(v0 + 16 * i + r)};
+                *reinterpret_cast<Candidate*>(list + to) = Candidate{x[4 * i + r], (int32_t)(v0 + 16 * i + r)};
+                to += 64 * (uint32_t)sizeof(Candidate);
                 ++n;
               }
             }
@@ -316,7 +422,16 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
       put(st.listed, k, true, (pick(st.listed, k) & ~(255u << at)) | (uint32_t)n << at);
     });
     const bool more = __any(full);
-    if (p->n_top > 0 && (more || now)) sort_all_in(st, lists, p->n_top, place);
+    if (n_top > 0 && (more || now)) sort_all_in(st, lists, n_top, place);
+    if (!again) {
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) {
+        const float to = fmaxf(st.e[k], tile_e[k]), a = __builtin_amdgcn_exp2f(st.e[k] - to), b = __builtin_amdgcn_exp2f(tile_e[k] - to);
+        st.t[k] = a * (st.t[k] + st.s[k] * (st.e[k] - to)) + b * (tile_t[k] + tile_s[k] * (tile_e[k] - to));
+        st.s[k] = a * st.s[k] + b * tile_s[k];
+        st.e[k] = to;
+      }
+    }
     if (!more) return;
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) tau[k] = fmaxf(tau[k], below(st.tau[k]));   // an id of this tile may equal the n_top-th best and come before it

@@ -86,7 +86,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
   const uint32_t w_dst = (uint32_t)wave * 64u * kRowBytes, h_dst = (uint32_t)(wave * 8 * NB) * kRowBytes;
 
   Candidate* const lists =
-      MODE == kGradients || p.lists == nullptr ? nullptr : p.lists + ((int64_t)blockIdx.x * 4 + wave) * (64 * NB) * kListRoom;
+      MODE == kGradients || p.lists == nullptr ? nullptr : p.lists + ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(wave)) * (64 * NB) * kListRoom;
 
   for (int u = first; u < n_units; u += G) {
     int pnl = u / full_panel_units;
@@ -200,7 +200,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
     uint32_t st_g = 0;
 
     Rows<NB> st;
-    st.clear();
+    st.clear(first_row, rows);
     const int64_t of_half = (int64_t)(2 * sp + wv) * sched.stride;
     auto place = [&](int k, bool& in) __attribute__((always_inline)) {
       const int row = first_row + 16 * (4 * k + q) + l16;
@@ -241,7 +241,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
         gradient_tile<NB, true>(load, v, first_row, found);
       } else {
         const int64_t from = vt0 + n == ragged_tile ? (int64_t)ragged_tile * kVocab : 0;
-        reduce_tile<NB, true>(load, st, v + 4 * q, from, p.V, target, first_row, rows, lists, sort_now(n + 1, ntile), place);
+        reduce_tile<NB, true>(load, st, v + 4 * q, from, p.V, target, first_row, lists, n == 0, sort_now(n + 1, ntile), place);
       }
     }
     if constexpr (MODE == kStatistics) {
