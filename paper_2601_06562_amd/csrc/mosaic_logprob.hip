@@ -91,7 +91,7 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
   if (unit >= end) return;
   const int panel = row_tiles < 8 ? row_tiles : 8;
 
-  Candidate* const lists = p.lists == nullptr ? nullptr : p.lists + ((int64_t)blockIdx.x * 8 + wave) * (64 * QB) * kListRoom;
+  Entry* const lists = p.lists == nullptr ? nullptr : p.lists + ((int64_t)blockIdx.x * 8 + wave) * (64 * QB) * kListRoom;
 
   // Of the tile whose copies are issued.
   int part = 0, row0 = 0, vt = 0, vt_begin = 0, vt_end = 0, turned = 0;
@@ -257,8 +257,7 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
         auto place = [&](int k, bool& in) __attribute__((always_inline)) {
           const int row = q0 + 16 * (4 * k + g) + (lane & 15);
           in = in && row < rows;
-          const Arguments a = arguments_again();
-        return a->part_top + (of_half + (in ? row : 0)) * a->n_top;
+          return p.part_top + (of_half + (in ? row : 0)) * p.n_top;
         };
         ++done_tiles;
         reduce_tile<QB, false>(load, st, v + 4 * g, 0, p.V, target, q0, lists, done_tiles == 1, sort_now(done_tiles, unit_tiles), place);
@@ -366,8 +365,8 @@ __global__ __launch_bounds__(kThreads) void logit_gradient_kernel(const LogitPar
   run_units<kGradients, TQ, SP, SQ>(p, smem, p.max_rows, rows_found(p));
 }
 
-// Joins a row's parts: a block a row, a thread every 256th part.
-constexpr int kJoinThreads = 256;
+// Joins a row's parts, a wave a row: a lane takes every 64th half.
+constexpr int kJoinWaves = 4;
 struct JoinParams {
   LogitParams l;
   float *out_logprob, *out_entropy, *out_lse, *top_logprob;
@@ -375,43 +374,55 @@ struct JoinParams {
   int64_t entries;   // of the parts' arrays
 };
 template <typename T, typename F>
-__device__ __forceinline__ T over_block(T v, T* lds, F f) {
+__device__ __forceinline__ T over_wave(T v, F f) {
 #pragma unroll
   for (int x = 32; x >= 1; x >>= 1) v = f(v, __shfl_xor(v, x, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = lds[0];
-#pragma unroll
-  for (int w = 1; w < kJoinThreads / 64; ++w) v = f(v, lds[w]);
   return v;
 }
-__global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(const JoinParams p) {
-  __shared__ double lds_d[kJoinThreads / 64];
-  __shared__ float lds_f[kJoinThreads / 64];
-  __shared__ long long lds_l[kJoinThreads / 64];
+__global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(const JoinParams p) {
+  constexpr int kHeld = 2 * kMostSplits / 64;   // halves of a lane, at most
   const LogitParams& l = p.l;
-  const int rows = rows_found(l);
+  const int rows = rows_found(l), lane = threadIdx.x & 63;
   if (rows <= 0) return;
   const int stride = l.found[1];
   // (whatever another call on the same workspace left there, nobody is to be led beyond the arrays)
-  const int halves = stride >= rows && l.found[0] > 0 && (int64_t)l.found[0] * stride <= p.entries ? l.found[0] : 0;
-  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+  const int halves = stride >= rows && l.found[0] > 0 && l.found[0] <= 2 * kMostSplits && (int64_t)l.found[0] * stride <= p.entries ? l.found[0] : 0;
+  const int held = (halves + 63) / 64;
+  for (int64_t row = (int64_t)blockIdx.x * kJoinWaves + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * kJoinWaves) {
+    float pe[kHeld], ps[kHeld], pt[kHeld];
+    Candidate head[kHeld];
+    int taken[kHeld];
     float e = kNegExponent;
-    for (int h = threadIdx.x; h < halves; h += kJoinThreads) e = fmaxf(e, l.part_e[(int64_t)h * stride + row]);
-    e = over_block(e, lds_f, [](float a, float b) { return fmaxf(a, b); });
-    double s = 0.0, t = 0.0;
-    for (int h = threadIdx.x; h < halves; h += kJoinThreads) {
-      const int64_t at = (int64_t)h * stride + row;
-      const float by = l.part_e[at] - e, scale = __builtin_amdgcn_exp2f(by), part = l.part_s[at];
-      s += (double)(scale * part);
-      t += (double)scale * ((double)l.part_t[at] + (double)part * by);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int h = lane + 64 * i;
+      pe[i] = kNegExponent;
+      ps[i] = pt[i] = 0.f;
+      head[i] = 0;
+      taken[i] = 0;
+      if (i < held && h < halves) {
+        const int64_t at = (int64_t)h * stride + row;
+        pe[i] = l.part_e[at];
+        ps[i] = l.part_s[at];
+        pt[i] = l.part_t[at];
+        if (l.n_top > 0) head[i] = l.part_top[at * l.n_top];
+      }
     }
-    s = over_block(s, lds_d, [](double a, double b) { return a + b; });
-    t = over_block(t, lds_d, [](double a, double b) { return a + b; });
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) e = fmaxf(e, pe[i]);
+    e = over_wave(e, [](float a, float b) { return fmaxf(a, b); });
+    double s = 0.0, t = 0.0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const float by = pe[i] - e, scale = __builtin_amdgcn_exp2f(by);
+      s += (double)(scale * ps[i]);
+      t += (double)scale * ((double)pt[i] + (double)ps[i] * by);
+    }
+    s = over_wave(s, [](double a, double b) { return a + b; });
+    t = over_wave(t, [](double a, double b) { return a + b; });
     // back from powers of two, by the factor that the exponents were made with
     const double log_s = log2(s), lse = ((double)e + log_s) / (double)kLog2e;
-    if (threadIdx.x == 0) {
+    if (lane == 0) {
       if (p.out_lse != nullptr) p.out_lse[row] = (float)lse;
       // an entropy is never below zero, a log probability never above it, whatever the last bits of a certain row's sums say
       const float entropy = (float)((log_s - t / s) / (double)kLog2e);
@@ -422,28 +433,23 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(const JoinPa
         p.out_logprob[row] = logp > 0.f ? 0.f : logp;
       }
     }
-    // The best n_top of the parts' best: each time the first behind the one before, by logit, then by id.
-    float past_x = __builtin_inff();
-    int past_id = -1;
+    // The best n_top of the halves' best: a lane holds the first candidates of its halves and, each time the best of all is its own,
+    // looks at the next of that half.
     for (int k = 0; k < l.n_top; ++k) {
-      float x = -__builtin_inff();
-      int id = INT_MAX;
-      for (int c = threadIdx.x; c < halves * l.n_top; c += kJoinThreads) {
-        const Candidate other = l.part_top[((int64_t)(c / l.n_top) * stride + row) * l.n_top + c % l.n_top];
-        const bool behind = other.x < past_x || (other.x == past_x && other.id > past_id);
-        if (behind && (other.x > x || (other.x == x && other.id < id))) { x = other.x; id = other.id; }
+      Candidate best = 0;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) best = head[i] > best ? head[i] : best;
+      best = over_wave((unsigned long long)best, [](unsigned long long a, unsigned long long b) { return a > b ? a : b; });
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        if (best != 0 && head[i] == best) {   // (ids differ, so it is one lane's)
+          ++taken[i];
+          head[i] = taken[i] < l.n_top ? l.part_top[((int64_t)(lane + 64 * i) * stride + row) * l.n_top + taken[i]] : 0;
+        }
       }
-      // as one number: logits in the order of integers, ids counted down
-      const int b = __float_as_int(x);
-      long long key = ((long long)(b ^ (int)((uint32_t)(b >> 31) >> 1)) << 32) | (uint32_t)(INT_MAX - id);
-      key = over_block(key, lds_l, [](long long a, long long b) { return a > b ? a : b; });
-      const int kb = (int)(key >> 32);
-      past_x = __int_as_float(kb ^ (int)((uint32_t)(kb >> 31) >> 1));
-      past_id = INT_MAX - (int)(uint32_t)key;
-      if (threadIdx.x == 0) {
-        const bool some = past_id != INT_MAX;
-        p.top_id[row * l.n_top + k] = some ? past_id : -1;
-        const float logp = some ? (float)((double)past_x - lse) : -__builtin_inff();
+      if (lane == 0) {
+        const float logp = best != 0 ? (float)((double)logit_of(best) - lse) : -__builtin_inff();
+        p.top_id[row * l.n_top + k] = best != 0 ? id_of(best) : -1;
         p.top_logprob[row * l.n_top + k] = logp > 0.f ? 0.f : logp;
       }
     }
@@ -554,7 +560,7 @@ Space space_of(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, 
     const int64_t most = (int64_t)kMostSplits * max_rows < kMostUnits * tile ? (int64_t)kMostSplits * max_rows : kMostUnits * tile;
     s.slots = most > max_rows ? most : max_rows;
     s.entries = 2 * s.slots;
-    lists = (int64_t)kCus * 8 * tile * kListRoom * (int64_t)sizeof(Candidate);
+    lists = (int64_t)kCus * 8 * tile * kListRoom * (int64_t)sizeof(Entry);
   }
   s.found = 0;
   s.lists = 256;
@@ -596,7 +602,7 @@ int launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
   p.part_t = reinterpret_cast<float*>(ws + at.t);
   p.part_top = reinterpret_cast<Candidate*>(ws + at.top);
   p.target_logit = reinterpret_cast<float*>(ws + at.target);
-  p.lists = a.n_top > 0 ? reinterpret_cast<Candidate*>(ws + at.lists) : nullptr;
+  p.lists = a.n_top > 0 ? reinterpret_cast<Entry*>(ws + at.lists) : nullptr;
   if (a.idx != nullptr && far_rows(a.T, a.ld_h)) {
     __bf16* rows = reinterpret_cast<__bf16*>(ws + at.rows);
     const int64_t pieces = a.max_rows * (a.d / 8);
@@ -621,8 +627,8 @@ int launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
   j.out_lse = a.out_lse;
   j.top_logprob = a.top_logprob;
   j.top_id = a.top_id;
-  const int64_t blocks = a.max_rows < 8192 ? a.max_rows : 8192;
-  return launch_kernel(logprob_join_kernel, dim3((unsigned)blocks), dim3(kJoinThreads), stream, j);
+  const int64_t blocks = (a.max_rows + kJoinWaves - 1) / kJoinWaves;
+  return launch_kernel(logprob_join_kernel, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(64 * kJoinWaves), stream, j);
 }
 
 // ---- gradients.  Per part of the vocabulary: dl of its ids, then both products of it.

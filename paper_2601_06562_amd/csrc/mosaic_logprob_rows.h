@@ -30,7 +30,20 @@ constexpr float kNegExponent = kNeg * kLog2e;   // this is exact
 constexpr int kMostTop = MOSAIC_MAX_TOP;
 constexpr int kListRoom = 16;          // candidates a lane keeps of a row until they are sorted in
 
-struct Candidate { float x; int32_t id; };
+// A candidate for a row's most probable ids: a number that is the larger the earlier it comes, by logit, then by the lower id.  0: none.
+typedef uint64_t Candidate;
+__host__ __device__ __forceinline__ Candidate candidate_of(float x, int32_t id) {
+  const float y = x + 0.f;   // -0 as 0
+  const uint32_t b = __builtin_bit_cast(uint32_t, y), up = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+  return (uint64_t)up << 32 | (uint32_t)~id;
+}
+__host__ __device__ __forceinline__ float logit_of(Candidate c) {
+  const uint32_t up = (uint32_t)(c >> 32);
+  return __builtin_bit_cast(float, up ^ ((up & 0x80000000u) != 0 ? 0x80000000u : 0xffffffffu));
+}
+__host__ __device__ __forceinline__ int32_t id_of(Candidate c) { return (int32_t)~(uint32_t)c; }
+
+struct Entry { float x; int32_t id; };   // of a lane's own list
 
 struct LogitParams {
   const char* w;
@@ -44,7 +57,7 @@ struct LogitParams {
   float *part_e, *part_s, *part_t;
   Candidate* part_top;       // n_top each
   float* target_logit;       // [max_rows]
-  Candidate* lists;          // of every block's waves: kListRoom x columns x 64 lanes
+  Entry* lists;              // of every block's waves: kListRoom x columns x 64 lanes
   int32_t* found;
   ScheduleInput sched;       // mosaic_logprob_w4.hip
   // gradients: of V ids from `first_id` on, for max_rows rows (zeros from the last listed one on)
@@ -69,6 +82,17 @@ __device__ __forceinline__ int rows_found(const LogitParams& p) {
   if (p.count == nullptr) return p.max_rows;
   const int n = *p.count;
   return n < 0 ? 0 : n < p.max_rows ? n : p.max_rows;
+}
+
+// A pointer among them points into device memory, which the compiler cannot tell of one that it did not see passed in.
+template <typename T>
+__device__ __forceinline__ __attribute__((address_space(1))) T* in_memory(T* x) { return (__attribute__((address_space(1))) T*)x; }
+// The same number, of which the compiler does not know that it is the same from one turn of a loop to the next: left alone it makes a
+// loop of its own for every such condition (a width's code 60 KB, which no instruction cache holds).
+__device__ __forceinline__ int opaque(int x) {
+  x = __builtin_amdgcn_readfirstlane(x);
+  asm volatile("" : "+s"(x));
+  return x;
 }
 
 // Over the four lanes that hold one row.
@@ -130,7 +154,7 @@ __device__ __forceinline__ void put(T (&a)[N], int k, bool own, T v) {
 
 // Sorts the candidates of this lane's own row k into the n best of before, in part_top at `to`: by logit, then by id.
 template <int N, int QB>
-__device__ __forceinline__ void sort_in(Rows<QB>& st, int k, const Candidate* lists, Candidate* to, bool owner, int n) {
+__device__ __forceinline__ void sort_in(Rows<QB>& st, int k, const Entry* lists, Candidate* to, bool owner, int n) {
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
   const uint32_t own_lists = pick(st.listed, k);
   int here[4], most = 0;   // of the row's four lanes
@@ -143,49 +167,44 @@ __device__ __forceinline__ void sort_in(Rows<QB>& st, int k, const Candidate* li
   int all = before;
   float last = kNeg;
   if (owner) {
-    const Candidate* from = lists + (int64_t)(4 * k + g) * kListRoom * 64 + l16;
-    float x[N];
-    int id[N];
+    const Entry* from = lists + (int64_t)(4 * k + g) * kListRoom * 64 + l16;
+    Candidate best[N];
 #pragma unroll
     for (int m = 0; m < N; ++m) {
       const Candidate c = to[m < before ? m : 0];
-      x[m] = m < before ? c.x : -__builtin_inff();
-      id[m] = m < before ? c.id : INT_MAX;
+      best[m] = m < before ? c : 0;
     }
-    constexpr int kAtOnce = 4;   // of each lane's list
+    // one entry of each lane's list at a time, the next ones under way
+    Entry ahead[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) ahead[q] = from[16 * q];
 #pragma unroll 1
-    for (int e = 0; e < most; e += kAtOnce) {
-      Candidate c[kAtOnce][4];
+    for (int e = 0; e < most; ++e) {
+      Entry c[4];
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i)
+      for (int q = 0; q < 4; ++q) {
+        c[q] = ahead[q];
+        ahead[q] = from[(e + 1 < kListRoom ? e + 1 : 0) * 64 + 16 * q];
+      }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) c[i][q] = from[(e + i < kListRoom ? e + i : 0) * 64 + 16 * q];
+      for (int q = 0; q < 4; ++q) {
+        const bool in = e < here[q];
+        all += in ? 1 : 0;
+        Candidate x = in ? candidate_of(c[q].x, c[q].id) : 0;
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const bool in = e + i < here[q];
-          all += in ? 1 : 0;
-          float cx = in ? c[i][q].x : -__builtin_inff();
-          int ci = in ? c[i][q].id : INT_MAX;
-#pragma unroll
-          for (int m = 0; m < N; ++m) {
-            const bool first = cx > x[m] || (cx == x[m] && ci < id[m]);
-            const float ox = x[m];
-            const int oi = id[m];
-            x[m] = first ? cx : ox;
-            id[m] = first ? ci : oi;
-            cx = first ? ox : cx;
-            ci = first ? oi : ci;
-          }
+        for (int m = 0; m < N; ++m) {
+          const Candidate other = best[m];
+          const bool first = x > other;
+          best[m] = first ? x : other;
+          x = first ? other : x;
         }
       }
     }
 #pragma unroll
     for (int m = 0; m < N; ++m) {
       if (m < n) {
-        to[m] = Candidate{x[m], id[m]};
-        last = x[m];
+        to[m] = best[m];
+        last = best[m] != 0 ? logit_of(best[m]) : kNeg;
       }
     }
   }
@@ -195,7 +214,7 @@ __device__ __forceinline__ void sort_in(Rows<QB>& st, int k, const Candidate* li
 
 // All own rows.  place(k, in): where the candidates of own row k go, and whether there is such a row.
 template <int QB, class Place>
-__device__ __forceinline__ void sort_all_in(Rows<QB>& st, const Candidate* lists, int n, Place place) {
+__device__ __forceinline__ void sort_all_in(Rows<QB>& st, const Entry* lists, int n, Place place) {
   const int g = (threadIdx.x & 63) >> 4;
   __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // the lists' entries were stored by other lanes
 #pragma unroll 1
@@ -261,52 +280,63 @@ __device__ __forceinline__ void sort_eight(float (&v)[8]) {
     }
   }
 }
-// A number that at least n of a row's ids of this tile reach: the n-th largest (for n > 8 the 16th) of the largest of 32 sets of
-// four, q, eight of which lie in each of the row's lanes.  About 5.4, 9 and 22 of 128 ids reach it for n = 5, 8 and 16.
-__device__ __forceinline__ float reached_by(const float (&q)[8], int n) {
-  float v[8];
+template <int N>
+__device__ __forceinline__ void exchange16(const float (&v)[N], float (&lo)[N], float (&hi)[N]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = q[i];
-  sort_eight(v);
-  // with the lane 16 away: of both lanes' sorted lists, one reversed, the larger of each two are the eight largest
-  float lo[8], hi[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < N; ++i) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
     lo[i] = __uint_as_float(r[0]);
     hi[i] = __uint_as_float(r[1]);
   }
-  float first[16];
+}
+template <int N>
+__device__ __forceinline__ void exchange32(const float (&v)[N], float (&lo)[N], float (&hi)[N]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    first[i] = fmaxf(lo[i], hi[7 - i]);
-    first[8 + i] = fminf(lo[i], hi[7 - i]);
+  for (int i = 0; i < N; ++i) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+    lo[i] = __uint_as_float(r[0]);
+    hi[i] = __uint_as_float(r[1]);
   }
-  sort_bitonic<8>(first);
+}
+// A number that at least n of a row's ids of this tile reach: the n-th largest of the largest of 16 sets of eight ids, four of
+// which lie in each of the row's lanes; for n > 8 the 16th of 32 sets of four.  Of two sorted lists, one reversed, the larger of
+// each two are the largest of all.  q: the largest of each quad.  Of 128 ids 3.5, 5.8, 10.6 and 22 reach it for n = 3, 5, 8 and 16.
+__device__ __forceinline__ float reached_by(const float (&q)[8], int n) {
   float bound;
   if (n <= 8) {
-    float top[8];
+    float v[4], lo[4], hi[4], all[8], low[8], high[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = fmaxf(q[2 * i], q[2 * i + 1]);
+    const float a = fmaxf(v[0], v[1]), b = fminf(v[0], v[1]), c = fminf(v[2], v[3]), d = fmaxf(v[2], v[3]);   // falls, then rises
+    v[0] = a; v[1] = b; v[2] = c; v[3] = d;
+    sort_bitonic<4>(v);
+    exchange16(v, lo, hi);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      all[i] = lo[i];
+      all[4 + i] = hi[3 - i];
+    }
+    sort_bitonic<8>(all);
+    exchange32(all, low, high);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) all[i] = fmaxf(low[i], high[7 - i]);
+    sort_bitonic<8>(all);
+    bound = all[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) bound = i < n ? all[i] : bound;
+  } else {
+    float v[8], lo[8], hi[8], all[16], low[16], high[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = q[i];
+    sort_eight(v);
+    exchange16(v, lo, hi);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(first[i]), __float_as_uint(first[i]), false, false);
-      lo[i] = __uint_as_float(r[0]);
-      hi[i] = __uint_as_float(r[1]);
+      all[i] = lo[i];
+      all[8 + i] = hi[7 - i];
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top[i] = fmaxf(lo[i], hi[7 - i]);
-    sort_bitonic<8>(top);
-    bound = top[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) bound = i < n ? top[i] : bound;
-  } else {
-    sort_bitonic<8>(first + 8);
-    float low[16], high[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(first[i]), __float_as_uint(first[i]), false, false);
-      low[i] = __uint_as_float(r[0]);
-      high[i] = __uint_as_float(r[1]);
-    }
+    sort_bitonic<16>(all);
+    exchange32(all, low, high);
     bound = fmaxf(low[0], high[15]);
 #pragma unroll
     for (int i = 1; i < 16; ++i) bound = fminf(bound, fmaxf(low[i], high[15 - i]));
@@ -319,13 +349,13 @@ __device__ __forceinline__ float reached_by(const float (&q)[8], int n) {
 // are sorted in at the end.  place(k, in): where the candidates of own row k go.
 template <int QB, bool ROLLED, class Load, class Place>
 __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0, int64_t from, int64_t end,
-                                            const int (&target)[Rows<QB>::kOwn], int row0, Candidate* lists, bool begins, bool now,
+                                            const int (&target)[Rows<QB>::kOwn], int row0, Entry* lists, bool begins, bool now,
                                             Place place) {
   constexpr int kOwn = Rows<QB>::kOwn;
   const Arguments p = arguments_again();
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
   const int n_top = p->n_top;
-  const bool whole = v0 - 4 * g >= from && v0 - 4 * g + kHalf <= end;      // (the same in all lanes)
+  const bool cut = v0 - 4 * g < from || v0 - 4 * g + kHalf > end;      // (the same in all lanes)
   const int lo = from > v0 ? (int)(from - v0) : 0, hi = end < v0 + kHalf ? (int)(end - v0) : kHalf;
   int wanted[kOwn];        // of the own rows: where the target lies in the half, from its first id on, or -1
   bool some = false;
@@ -335,22 +365,25 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
     wanted[k] = target[k] >= 0 && at >= 0 && at < kHalf ? (int)at : -1;
     some = some || wanted[k] >= 0;
   }
-  some = __any(some);
+  enum { kCut = 1, kTarget = 2, kTop = 4, kBegins = 8, kAgain = 16 };
+  int all_flags = (cut ? kCut : 0) | (__any(some) ? kTarget : 0) | (n_top > 0 ? kTop | (begins ? kBegins : 0) : 0);
   float tile_e[kOwn], tile_s[kOwn], tile_t[kOwn];
   float tau[kOwn];         // of the own rows: what candidates of this tile have to pass
   uint32_t next[kOwn];     // of columns 4 k .., a byte each: the first quad of this lane that is still to be looked at
 #pragma unroll
   for (int k = 0; k < kOwn; ++k) { tile_e[k] = kNegExponent; tile_s[k] = tile_t[k] = 0.f; tau[k] = st.tau[k]; next[k] = 0; }
-  for (bool again = false;; again = true) {
+#pragma unroll 1
+  for (;;) {
     bool full = false;
     each_column<ROLLED, QB>([&](int j) __attribute__((always_inline)) {
       const int k = j >> 2, at = 8 * (j & 3), owner = 16 * (j & 3) + l16;
       const bool own = g == (j & 3);
+      const int flags = opaque(all_flags);
       float pass = 0.f;
-      if (n_top > 0) pass = __shfl(pick(tau, k), owner, 64);
+      if (flags & kTop) pass = __shfl(pick(tau, k), owner, 64);
       float x[32];
       load(j, x);
-      if (!whole) {
+      if (flags & kCut) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -359,7 +392,7 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
       float most[8];       // of quads
 #pragma unroll
       for (int i = 0; i < 8; ++i) most[i] = fmaxf(fmaxf(fmaxf(x[4 * i], x[4 * i + 1]), x[4 * i + 2]), x[4 * i + 3]);
-      if (!again) {
+      if (!(flags & kAgain)) {
         const float lane_m = fmaxf(fmaxf(fmaxf(fmaxf(most[0], most[1]), most[2]), fmaxf(fmaxf(most[3], most[4]), most[5])), fmaxf(most[6], most[7]));
         const float e = __builtin_ceilf(fmaxf(row_max(lane_m), kNeg) * kLog2e);
         float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};
@@ -372,7 +405,7 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
         put(tile_e, k, own, e);
         put(tile_s, k, own, row_sum((s[0] + s[1]) + (s[2] + s[3])));
         put(tile_t, k, own, row_sum((t[0] + t[1]) + (t[2] + t[3])));
-        if (some) {        // the target's logit, in the one lane that holds it
+        if (flags & kTarget) {        // the target's logit, in the one lane that holds it
           const int rel = __shfl(pick(wanted, k), owner, 64) - 4 * g;
           float logit = 0.f;
           bool here = false;
@@ -384,11 +417,11 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
               logit = it ? x[4 * i + r] : logit;
               here = here || it;
             }
-          if (here && rel >= lo && rel < hi) p->target_logit[row0 + 16 * j + l16] = logit;
+          if (here && rel >= lo && rel < hi) in_memory(p->target_logit)[row0 + 16 * j + l16] = logit;
         }
       }
-      if (n_top == 0) return;
-      if (begins && !again) {
+      if (!(flags & kTop)) return;
+      if ((flags & (kBegins | kAgain)) == kBegins) {
         const float bound = below(fmaxf(reached_by(most, n_top), kNeg));
         pass = fmaxf(fmaxf(pass, bound), kNeg);
         put(tau, k, own, pass);
@@ -397,33 +430,36 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
       // on there once all have been sorted in.
       int done = (int)(pick(next, k) >> at & 255), n = (int)(pick(st.listed, k) >> at & 255);
       bool stopped = false;
-      char* const list = reinterpret_cast<char*>(lists) + j * (kListRoom * 64 * (int)sizeof(Candidate));
-      uint32_t to = (uint32_t)(n * 64 + lane) * (uint32_t)sizeof(Candidate);
+      char* const list = reinterpret_cast<char*>(lists) + j * (kListRoom * 64 * (int)sizeof(Entry));
+      uint32_t to = (uint32_t)(n * 64 + lane) * (uint32_t)sizeof(Entry);
+      constexpr uint32_t kFull = (kListRoom - 4) * 64 * (uint32_t)sizeof(Entry);
+      const int id0 = (int)v0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const bool want = most[i] > pass && i >= done && !stopped;
+        const bool want = (most[i] > pass) & (i >= done) & !stopped;
         if (__any(want)) {
-          stopped = stopped || (want && n > kListRoom - 4);
-          done = want && stopped ? i : done;
-          if (want && !stopped) {
+          const bool fits = to < kFull + 64 * (uint32_t)sizeof(Entry);
+          stopped = stopped | (want & !fits);
+          done = want & !fits ? i : done;
+          if (want & fits) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               if (x[4 * i + r] > pass) {
-                *reinterpret_cast<Candidate*>(list + to) = Candidate{x[4 * i + r], (int32_t)(v0 + 16 * i + r)};
-                to += 64 * (uint32_t)sizeof(Candidate);
-                ++n;
+                *reinterpret_cast<Entry*>(list + to) = Entry{x[4 * i + r], id0 + 16 * i + r};
+                to += 64 * (uint32_t)sizeof(Entry);
               }
             }
           }
         }
       }
+      n = (int)(to / (64 * (uint32_t)sizeof(Entry)));
       full = full || stopped;
       put(next, k, true, (pick(next, k) & ~(255u << at)) | (uint32_t)(stopped ? done : 8) << at);
       put(st.listed, k, true, (pick(st.listed, k) & ~(255u << at)) | (uint32_t)n << at);
     });
     const bool more = __any(full);
     if (n_top > 0 && (more || now)) sort_all_in(st, lists, n_top, place);
-    if (!again) {
+    if (!(all_flags & kAgain)) {
 #pragma unroll
       for (int k = 0; k < kOwn; ++k) {
         const float to = fmaxf(st.e[k], tile_e[k]), a = __builtin_amdgcn_exp2f(st.e[k] - to), b = __builtin_amdgcn_exp2f(tile_e[k] - to);
@@ -433,6 +469,7 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
       }
     }
     if (!more) return;
+    all_flags |= kAgain;
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) tau[k] = fmaxf(tau[k], below(st.tau[k]));   // an id of this tile may equal the n_top-th best and come before it
   }
@@ -454,11 +491,11 @@ __device__ __forceinline__ void gradient_tile(Load load, int64_t v0, int row0, i
   each_column<ROLLED, QB>([&](int j) __attribute__((always_inline)) {
     const int row = row0 + 16 * j + l16;
     const bool in = row < p->max_rows, listed = row < found;
-    const float lse = listed ? p->lse[row] : 0.f;
-    const int target = listed && p->targets != nullptr ? p->targets[row] : -1;
-    const float g = (uint32_t)target < (uint32_t)p->all_ids ? p->dlogprob[row] : 0.f;
-    const float h = listed && p->dentropy != nullptr ? p->dentropy[row] : 0.f;
-    const float entropy = listed && p->dentropy != nullptr ? p->entropy[row] : 0.f;
+    const float lse = listed ? in_memory(p->lse)[row] : 0.f;
+    const int target = listed && p->targets != nullptr ? in_memory(p->targets)[row] : -1;
+    const float g = (uint32_t)target < (uint32_t)p->all_ids ? in_memory(p->dlogprob)[row] : 0.f;
+    const float h = listed && p->dentropy != nullptr ? in_memory(p->dentropy)[row] : 0.f;
+    const float entropy = listed && p->dentropy != nullptr ? in_memory(p->entropy)[row] : 0.f;
     const int64_t from = (int64_t)target - p->first_id - v0;
     const int rel = target >= 0 && from >= 0 && from < kHalf ? (int)from - 4 * g4 : -kHalf;
     float x[32];

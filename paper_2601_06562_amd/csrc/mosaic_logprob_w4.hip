@@ -85,7 +85,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
   const uint32_t u_hwrap = (uint32_t)(nk - 1) * 128u;
   const uint32_t w_dst = (uint32_t)wave * 64u * kRowBytes, h_dst = (uint32_t)(wave * 8 * NB) * kRowBytes;
 
-  Candidate* const lists =
+  Entry* const lists =
       MODE == kGradients || p.lists == nullptr ? nullptr : p.lists + ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(wave)) * (64 * NB) * kListRoom;
 
   for (int u = first; u < n_units; u += G) {
@@ -123,14 +123,14 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
 #pragma unroll
       for (int k = 0; k < Rows<NB>::kOwn; ++k) {
         const int row = first_row + 16 * (4 * k + q) + l16;
-        target[k] = 4 * k + q < NB && p.targets != nullptr && row < rows ? p.targets[row] : -1;
+        target[k] = 4 * k + q < NB && p.targets != nullptr && row < rows ? in_memory(p.targets)[row] : -1;
       }
     }
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       int j = tt * kTokens + wave * 8 * NB + 8 * i + sub;
       if (j > rows - 1) j = rows - 1;
-      trow[i] = p.idx != nullptr ? p.idx[j] : j;
+      trow[i] = p.idx != nullptr ? in_memory(p.idx)[j] : j;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) woff[i] = wlane[i & 1] + (uint32_t)(8 * (i ^ turn)) * w_row_bytes;
@@ -205,8 +205,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
     auto place = [&](int k, bool& in) __attribute__((always_inline)) {
       const int row = first_row + 16 * (4 * k + q) + l16;
       in = in && row < rows;
-      const Arguments a = arguments_again();
-      return a->part_top + (of_half + (in ? row : 0)) * a->n_top;
+      return p.part_top + (of_half + (in ? row : 0)) * p.n_top;
     };
 
 #pragma unroll 1
@@ -320,7 +319,7 @@ bool w4_takes(int32_t d, int32_t V) {
 int64_t w4_list_bytes(int64_t max_rows) {
   const int64_t width = max_rows >= 256 ? 8 : (max_rows + 31) / 32;   // row tiles no wider than that
   (void)width;
-  return (int64_t)kCus * 4 * 64 * 8 * kListRoom * (int64_t)sizeof(Candidate);
+  return (int64_t)kCus * 4 * 64 * 8 * kListRoom * (int64_t)sizeof(Entry);
 }
 
 int launch_logprob_w4(const LogitParams& p, hipStream_t stream) { return launch<kStatistics>(p, stream); }
