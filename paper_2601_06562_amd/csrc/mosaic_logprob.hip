@@ -209,7 +209,7 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
     slot_q = to_q;
   };
 
-  if (MODE == kStatistics && blockIdx.x == 0 && threadIdx.x == 0) {
+  if (MODE != kGradients && blockIdx.x == 0 && threadIdx.x == 0) {
     p.found[0] = 2 * parts;
     p.found[1] = rows;
   }
@@ -260,7 +260,7 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
           return p.part_top + (of_half + (in ? row : 0)) * p.n_top;
         };
         ++done_tiles;
-        reduce_tile<QB, false>(load, st, v + 4 * g, 0, p.V, target, q0, lists, done_tiles == 1, sort_now(done_tiles, unit_tiles), place);
+        reduce_tile<QB, false, MODE == kAlternatives>(load, st, v + 4 * g, 0, p.V, target, q0, lists, done_tiles == 1, sort_now(done_tiles, unit_tiles), place);
         if (done_last) {
 #pragma unroll
           for (int k = 0; k < Rows<QB>::kOwn; ++k) {
@@ -350,14 +350,15 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
 constexpr int kLds = 160 * 1024;
 static_assert(ring_bytes(kVocab, 256, 3, 2) <= kLds && ring_bytes(kVocab, 128, 3, 3) <= kLds && ring_bytes(kVocab, 64, 4, 4) <= kLds, "rings");
 
+template <int MODE>
 __global__ __launch_bounds__(kThreads) void logprob_kernel(const LogitParams p) {
   __shared__ __attribute__((aligned(1024))) char smem[kLds];
   const int rows = rows_found(p);
   if (rows <= 0) return;
   const int tile = tile_rows(rows);
-  if (tile == 256) run_units<kStatistics, 256, 3, 2>(p, smem, rows, rows);
-  else if (tile == 128) run_units<kStatistics, 128, 3, 3>(p, smem, rows, rows);
-  else run_units<kStatistics, 64, 4, 4>(p, smem, rows, rows);
+  if (tile == 256) run_units<MODE, 256, 3, 2>(p, smem, rows, rows);
+  else if (tile == 128) run_units<MODE, 128, 3, 3>(p, smem, rows, rows);
+  else run_units<MODE, 64, 4, 4>(p, smem, rows, rows);
 }
 template <int TQ, int SP, int SQ>
 __global__ __launch_bounds__(kThreads) void logit_gradient_kernel(const LogitParams p) {
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(const Joi
       const int h = lane + 64 * i;
       pe[i] = kNegExponent;
       ps[i] = pt[i] = 0.f;
-      head[i] = 0;
+      head[i] = 0.0;
       taken[i] = 0;
       if (i < held && h < halves) {
         const int64_t at = (int64_t)h * stride + row;
@@ -436,20 +437,20 @@ __global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(const Joi
     // The best n_top of the halves' best: a lane holds the first candidates of its halves and, each time the best of all is its own,
     // looks at the next of that half.
     for (int k = 0; k < l.n_top; ++k) {
-      Candidate best = 0;
+      Candidate best = 0.0;
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i) best = head[i] > best ? head[i] : best;
-      best = over_wave((unsigned long long)best, [](unsigned long long a, unsigned long long b) { return a > b ? a : b; });
+      for (int i = 0; i < kHeld; ++i) best = first_of_two(head[i], best);
+      best = over_wave(best, [](double a, double b) { return first_of_two(a, b); });
 #pragma unroll
       for (int i = 0; i < kHeld; ++i) {
-        if (best != 0 && head[i] == best) {   // (ids differ, so it is one lane's)
+        if (best != 0.0 && head[i] == best) {   // (ids differ, so it is one lane's)
           ++taken[i];
-          head[i] = taken[i] < l.n_top ? l.part_top[((int64_t)(lane + 64 * i) * stride + row) * l.n_top + taken[i]] : 0;
+          head[i] = taken[i] < l.n_top ? l.part_top[((int64_t)(lane + 64 * i) * stride + row) * l.n_top + taken[i]] : 0.0;
         }
       }
       if (lane == 0) {
-        const float logp = best != 0 ? (float)((double)logit_of(best) - lse) : -__builtin_inff();
-        p.top_id[row * l.n_top + k] = best != 0 ? id_of(best) : -1;
+        const float logp = best != 0.0 ? (float)((double)logit_of(best) - lse) : -__builtin_inff();
+        p.top_id[row * l.n_top + k] = best != 0.0 ? id_of(best) : -1;
         p.top_logprob[row * l.n_top + k] = logp > 0.f ? 0.f : logp;
       }
     }
@@ -554,7 +555,7 @@ Space space_of(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, 
     const int64_t row_tiles = (max_rows + 255) / 256;
     s.slots = row_tiles * 256 * choose_vocab_splits(row_tiles, ((int64_t)V + kVocab - 1) / kVocab, kCus);
     s.entries = 2 * s.slots;
-    lists = w4_list_bytes(max_rows);
+    lists = w4_list_bytes();
   } else {
     // up to kMostUnits units, at most kMostSplits parts, and one part whatever the rows
     const int64_t most = (int64_t)kMostSplits * max_rows < kMostUnits * tile ? (int64_t)kMostSplits * max_rows : kMostUnits * tile;
@@ -615,8 +616,8 @@ int launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
   }
   if (w4_takes(a.d, a.V)) {
     p.sched.slots64 = (uint32_t)(at.slots / 64 < INT32_MAX ? at.slots / 64 : INT32_MAX);
-    if (launch_logprob_w4(p, stream) != 0) return -1;
-  } else if (launch_kernel(logprob_kernel, dim3(kCus), dim3(kThreads), stream, p) != 0) {
+    if ((a.n_top > 0 ? launch_alternatives_w4(p, stream) : launch_statistics_w4(p, stream)) != 0) return -1;
+  } else if (launch_kernel(a.n_top > 0 ? logprob_kernel<kAlternatives> : logprob_kernel<kStatistics>, dim3(kCus), dim3(kThreads), stream, p) != 0) {
     return -1;
   }
   JoinParams j = {};
@@ -688,7 +689,7 @@ int launch_dl(LogitParams p, int64_t v, int64_t n, hipStream_t stream) {
     p.V = (int32_t)parts[k][1];
     p.dl_ids = (p.V + 7) / 8 * 8;
     p.first_id = (int32_t)(v + parts[k][0]);
-    if ((k == 0 ? launch_logit_gradients_w4(p, stream) : launch_gradient_tiles(p, stream)) != 0) return -1;
+    if ((k == 0 ? launch_gradients_w4(p, stream) : launch_gradient_tiles(p, stream)) != 0) return -1;
   }
   return 0;
 }

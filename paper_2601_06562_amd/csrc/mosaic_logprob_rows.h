@@ -30,18 +30,30 @@ constexpr float kNegExponent = kNeg * kLog2e;   // this is exact
 constexpr int kMostTop = MOSAIC_MAX_TOP;
 constexpr int kListRoom = 16;          // candidates a lane keeps of a row until they are sorted in
 
-// A candidate for a row's most probable ids: a number that is the larger the earlier it comes, by logit, then by the lower id.  0: none.
-typedef uint64_t Candidate;
-__host__ __device__ __forceinline__ Candidate candidate_of(float x, int32_t id) {
-  const float y = x + 0.f;   // -0 as 0
-  const uint32_t b = __builtin_bit_cast(uint32_t, y), up = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-  return (uint64_t)up << 32 | (uint32_t)~id;
+// A candidate for a row's most probable ids: a positive double that is the larger the earlier it comes, by logit, then by the lower id
+// (32 bits of one in the order of unsigned numbers, 31 of the other counted down: no NaN but of a NaN), so that two instructions put
+// two in order, where a comparison of 64-bit whole numbers and the selects behind it are seven.  0: none.
+typedef double Candidate;
+__device__ __forceinline__ Candidate candidate_of(float x, int32_t id) {
+  const uint32_t b = __float_as_uint(x + 0.f), up = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);   // (-0 as 0)
+  return __longlong_as_double((long long)((uint64_t)up << 31 | (0x7fffffffu - (uint32_t)id)));
 }
-__host__ __device__ __forceinline__ float logit_of(Candidate c) {
-  const uint32_t up = (uint32_t)(c >> 32);
-  return __builtin_bit_cast(float, up ^ ((up & 0x80000000u) != 0 ? 0x80000000u : 0xffffffffu));
+__device__ __forceinline__ float logit_of(Candidate c) {
+  const uint32_t up = (uint32_t)((uint64_t)__double_as_longlong(c) >> 31);
+  return __uint_as_float(up ^ ((up & 0x80000000u) != 0 ? 0x80000000u : 0xffffffffu));
 }
-__host__ __device__ __forceinline__ int32_t id_of(Candidate c) { return (int32_t)~(uint32_t)c; }
+__device__ __forceinline__ int32_t id_of(Candidate c) { return (int32_t)(0x7fffffffu - ((uint32_t)__double_as_longlong(c) & 0x7fffffffu)); }
+// The first and the second of two; as statements, since the compiler quiets what it takes for signalling NaNs beforehand.
+__device__ __forceinline__ Candidate first_of_two(Candidate a, Candidate b) {
+  Candidate c;
+  asm("v_max_f64 %0, %1, %2" : "=v"(c) : "v"(a), "v"(b));
+  return c;
+}
+__device__ __forceinline__ Candidate second_of_two(Candidate a, Candidate b) {
+  Candidate c;
+  asm("v_min_f64 %0, %1, %2" : "=v"(c) : "v"(a), "v"(b));
+  return c;
+}
 
 struct Entry { float x; int32_t id; };   // of a lane's own list
 
@@ -67,7 +79,8 @@ struct LogitParams {
   int32_t first_id, all_ids;
   int32_t dl_ids;            // ids that dl holds, a multiple of 8
 };
-enum { kStatistics, kGradients };
+// Alternatives are a kernel's own: without them its code is a quarter, and most of a short call's time goes to fetching code.
+enum { kStatistics, kAlternatives, kGradients };
 
 // A kernel's arguments, read where they are used: what is made of a tile uses many, and kept from one tile to the next they would
 // take the scalar registers that the products need.
@@ -172,31 +185,39 @@ __device__ __forceinline__ void sort_in(Rows<QB>& st, int k, const Entry* lists,
 #pragma unroll
     for (int m = 0; m < N; ++m) {
       const Candidate c = to[m < before ? m : 0];
-      best[m] = m < before ? c : 0;
+      best[m] = m < before ? c : 0.0;
     }
-    // one entry of each lane's list at a time, the next ones under way
-    Entry ahead[4];
+    // four entries of each lane's list at a time, the next ones under way
+    constexpr int kAtOnce = 4;
+    Entry ahead[kAtOnce][4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) ahead[q] = from[16 * q];
+    for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) ahead[i][q] = from[i * 64 + 16 * q];
 #pragma unroll 1
-    for (int e = 0; e < most; ++e) {
-      Entry c[4];
+    for (int e = 0; e < most; e += kAtOnce) {
+      Candidate c[kAtOnce][4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        c[q] = ahead[q];
-        ahead[q] = from[(e + 1 < kListRoom ? e + 1 : 0) * 64 + 16 * q];
+      for (int i = 0; i < kAtOnce; ++i) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bool in = e + i < here[q];
+          all += in ? 1 : 0;
+          c[i][q] = in ? candidate_of(ahead[i][q].x, ahead[i][q].id) : 0.0;
+          ahead[i][q] = from[(e + kAtOnce + i < kListRoom ? e + kAtOnce + i : 0) * 64 + 16 * q];
+        }
       }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const bool in = e < here[q];
-        all += in ? 1 : 0;
-        Candidate x = in ? candidate_of(c[q].x, c[q].id) : 0;
+      for (int i = 0; i < kAtOnce; ++i) {
 #pragma unroll
-        for (int m = 0; m < N; ++m) {
-          const Candidate other = best[m];
-          const bool first = x > other;
-          best[m] = first ? x : other;
-          x = first ? other : x;
+        for (int q = 0; q < 4; ++q) {
+          Candidate x = c[i][q];
+#pragma unroll
+          for (int m = 0; m < N; ++m) {
+            const Candidate other = best[m];
+            best[m] = first_of_two(x, other);
+            x = second_of_two(x, other);
+          }
         }
       }
     }
@@ -204,7 +225,7 @@ __device__ __forceinline__ void sort_in(Rows<QB>& st, int k, const Entry* lists,
     for (int m = 0; m < N; ++m) {
       if (m < n) {
         to[m] = best[m];
-        last = best[m] != 0 ? logit_of(best[m]) : kNeg;
+        last = best[m] != 0.0 ? logit_of(best[m]) : kNeg;
       }
     }
   }
@@ -347,14 +368,14 @@ __device__ __forceinline__ float reached_by(const float (&q)[8], int n) {
 // Works a finished tile into the rows' states.  v0: the id of this lane's first element; ids below `from` and from `end` on are
 // not counted; target: of the own rows, less than 0: none.  begins: the first tile of its unit.  now: whether the candidates so far
 // are sorted in at the end.  place(k, in): where the candidates of own row k go.
-template <int QB, bool ROLLED, class Load, class Place>
+template <int QB, bool ROLLED, bool TOP, class Load, class Place>
 __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0, int64_t from, int64_t end,
                                             const int (&target)[Rows<QB>::kOwn], int row0, Entry* lists, bool begins, bool now,
                                             Place place) {
   constexpr int kOwn = Rows<QB>::kOwn;
   const Arguments p = arguments_again();
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
-  const int n_top = p->n_top;
+  const int n_top = TOP ? p->n_top : 0;
   const bool cut = v0 - 4 * g < from || v0 - 4 * g + kHalf > end;      // (the same in all lanes)
   const int lo = from > v0 ? (int)(from - v0) : 0, hi = end < v0 + kHalf ? (int)(end - v0) : kHalf;
   int wanted[kOwn];        // of the own rows: where the target lies in the half, from its first id on, or -1
@@ -365,8 +386,8 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
     wanted[k] = target[k] >= 0 && at >= 0 && at < kHalf ? (int)at : -1;
     some = some || wanted[k] >= 0;
   }
-  enum { kCut = 1, kTarget = 2, kTop = 4, kBegins = 8, kAgain = 16 };
-  int all_flags = (cut ? kCut : 0) | (__any(some) ? kTarget : 0) | (n_top > 0 ? kTop | (begins ? kBegins : 0) : 0);
+  enum { kCut = 1, kTarget = 2, kBegins = 4, kAgain = 8 };
+  int all_flags = (cut ? kCut : 0) | (__any(some) ? kTarget : 0) | (begins ? kBegins : 0);
   float tile_e[kOwn], tile_s[kOwn], tile_t[kOwn];
   float tau[kOwn];         // of the own rows: what candidates of this tile have to pass
   uint32_t next[kOwn];     // of columns 4 k .., a byte each: the first quad of this lane that is still to be looked at
@@ -380,7 +401,7 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
       const bool own = g == (j & 3);
       const int flags = opaque(all_flags);
       float pass = 0.f;
-      if (flags & kTop) pass = __shfl(pick(tau, k), owner, 64);
+      if constexpr (TOP) pass = __shfl(pick(tau, k), owner, 64);
       float x[32];
       load(j, x);
       if (flags & kCut) {
@@ -420,45 +441,51 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
           if (here && rel >= lo && rel < hi) in_memory(p->target_logit)[row0 + 16 * j + l16] = logit;
         }
       }
-      if (!(flags & kTop)) return;
-      if ((flags & (kBegins | kAgain)) == kBegins) {
-        const float bound = below(fmaxf(reached_by(most, n_top), kNeg));
-        pass = fmaxf(fmaxf(pass, bound), kNeg);
-        put(tau, k, own, pass);
-      }
-      // Candidates go to this lane's own list of the column.  Where it is full the lane stops at the quad that does not fit, and goes
-      // on there once all have been sorted in.
-      int done = (int)(pick(next, k) >> at & 255), n = (int)(pick(st.listed, k) >> at & 255);
-      bool stopped = false;
-      char* const list = reinterpret_cast<char*>(lists) + j * (kListRoom * 64 * (int)sizeof(Entry));
-      uint32_t to = (uint32_t)(n * 64 + lane) * (uint32_t)sizeof(Entry);
-      constexpr uint32_t kFull = (kListRoom - 4) * 64 * (uint32_t)sizeof(Entry);
-      const int id0 = (int)v0;
+      if constexpr (TOP) {
+        if ((flags & (kBegins | kAgain)) == kBegins) {
+          const float bound = below(fmaxf(reached_by(most, n_top), kNeg));
+          pass = fmaxf(fmaxf(pass, bound), kNeg);
+          put(tau, k, own, pass);
+        }
+        // Candidates go to this lane's own list of the column.  Where it is full the lane stops at the quad that does not fit, and goes
+        // on there once all have been sorted in.
+        int done = (int)(pick(next, k) >> at & 255), n = (int)(pick(st.listed, k) >> at & 255);
+        bool stopped = false;
+        char* const list = reinterpret_cast<char*>(lists) + j * (kListRoom * 64 * (int)sizeof(Entry));
+        uint32_t to = (uint32_t)(n * 64 + lane) * (uint32_t)sizeof(Entry);
+        constexpr uint32_t kFull = (kListRoom - 4) * 64 * (uint32_t)sizeof(Entry);
+        const int id0 = (int)v0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const bool want = (most[i] > pass) & (i >= done) & !stopped;
-        if (__any(want)) {
-          const bool fits = to < kFull + 64 * (uint32_t)sizeof(Entry);
-          stopped = stopped | (want & !fits);
-          done = want & !fits ? i : done;
-          if (want & fits) {
+        for (int i = 0; i < 8; ++i) {
+          const bool want = (most[i] > pass) & (i >= done) & !stopped;
+          if (__any(want)) {
+            const bool fits = to < kFull + 64 * (uint32_t)sizeof(Entry);
+            stopped = stopped | (want & !fits);
+            done = (want & !fits) ? i : done;
+            if (want & fits) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              if (x[4 * i + r] > pass) {
-                *reinterpret_cast<Entry*>(list + to) = Entry{x[4 * i + r], id0 + 16 * i + r};
-                to += 64 * (uint32_t)sizeof(Entry);
+              for (int r = 0; r < 4; ++r) {
+                if (x[4 * i + r] > pass) {
+                  *reinterpret_cast<Entry*>(list + to) = Entry{x[4 * i + r], id0 + 16 * i + r};
+                  to += 64 * (uint32_t)sizeof(Entry);
+                }
               }
             }
           }
         }
+        n = (int)(to / (64 * (uint32_t)sizeof(Entry)));
+        full = full || stopped;
+        put(next, k, true, (pick(next, k) & ~(255u << at)) | (uint32_t)(stopped ? done : 8) << at);
+        put(st.listed, k, true, (pick(st.listed, k) & ~(255u << at)) | (uint32_t)n << at);
       }
-      n = (int)(to / (64 * (uint32_t)sizeof(Entry)));
-      full = full || stopped;
-      put(next, k, true, (pick(next, k) & ~(255u << at)) | (uint32_t)(stopped ? done : 8) << at);
-      put(st.listed, k, true, (pick(st.listed, k) & ~(255u << at)) | (uint32_t)n << at);
     });
-    const bool more = __any(full);
-    if (n_top > 0 && (more || now)) sort_all_in(st, lists, n_top, place);
+    bool more = false;
+    if constexpr (TOP) {
+      more = __any(full);
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) st.tau[k] = fmaxf(st.tau[k], tau[k]);   // (what no id of this tile needs to pass none of a later one does)
+      if (more || now) sort_all_in(st, lists, n_top, place);
+    }
     if (!(all_flags & kAgain)) {
 #pragma unroll
       for (int k = 0; k < kOwn; ++k) {
@@ -530,11 +557,12 @@ __device__ __forceinline__ void gradient_tile(Load load, int64_t v0, int row0, i
   });
 }
 
-// mosaic_logprob_w4.hip: whether its kernels take these sizes, and their launches.
+// The 4-wave kernels (mosaic_logprob_w4.h): whether they take these sizes, and their launches.
 bool w4_takes(int32_t d, int32_t V);
-int launch_logprob_w4(const LogitParams& p, hipStream_t stream);
-int launch_logit_gradients_w4(const LogitParams& p, hipStream_t stream);
-int64_t w4_list_bytes(int64_t max_rows);
+int launch_statistics_w4(const LogitParams& p, hipStream_t stream);
+int launch_alternatives_w4(const LogitParams& p, hipStream_t stream);
+int launch_gradients_w4(const LogitParams& p, hipStream_t stream);
+int64_t w4_list_bytes();
 
 }  // namespace logprob
 }  // namespace mosaic

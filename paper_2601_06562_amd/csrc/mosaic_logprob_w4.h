@@ -4,7 +4,11 @@
 // of 32 NB rows and parts of the vocabulary are chosen on the device from the rows found (mosaic_schedule.h), as there.
 //
 // It takes d that is a multiple of 64 and whole tiles of 256 ids, or a last tile over the vocabulary's last 256 ids, of which
-// those of the tile before it are not counted again; mosaic_logprob.hip has the kernel for the rest.
+// those of the tile before it are not counted again; mosaic_logprob.hip has the kernel for the rest.  Each of the three kernels is compiled by itself
+// (mosaic_logprob_w4_*.hip), since one takes about a minute.
+#ifndef MOSAIC_LOGPROB_W4_H_
+#define MOSAIC_LOGPROB_W4_H_
+
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -86,7 +90,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
   const uint32_t w_dst = (uint32_t)wave * 64u * kRowBytes, h_dst = (uint32_t)(wave * 8 * NB) * kRowBytes;
 
   Entry* const lists =
-      MODE == kGradients || p.lists == nullptr ? nullptr : p.lists + ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(wave)) * (64 * NB) * kListRoom;
+      MODE != kAlternatives ? nullptr : p.lists + ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(wave)) * (64 * NB) * kListRoom;
 
   for (int u = first; u < n_units; u += G) {
     int pnl = u / full_panel_units;
@@ -119,7 +123,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
     const int first_row = tt * kTokens + wt * (kTokens / 2);   // this wave's rows
     int trow[NB];
     [[maybe_unused]] int target[Rows<NB>::kOwn];
-    if constexpr (MODE == kStatistics) {
+    if constexpr (MODE != kGradients) {
 #pragma unroll
       for (int k = 0; k < Rows<NB>::kOwn; ++k) {
         const int row = first_row + 16 * (4 * k + q) + l16;
@@ -240,10 +244,10 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
         gradient_tile<NB, true>(load, v, first_row, found);
       } else {
         const int64_t from = vt0 + n == ragged_tile ? (int64_t)ragged_tile * kVocab : 0;
-        reduce_tile<NB, true>(load, st, v + 4 * q, from, p.V, target, first_row, lists, n == 0, sort_now(n + 1, ntile), place);
+        reduce_tile<NB, true, MODE == kAlternatives>(load, st, v + 4 * q, from, p.V, target, first_row, lists, n == 0, sort_now(n + 1, ntile), place);
       }
     }
-    if constexpr (MODE == kStatistics) {
+    if constexpr (MODE != kGradients) {
 #pragma unroll
       for (int k = 0; k < Rows<NB>::kOwn; ++k) {
         const int row = first_row + 16 * (4 * k + q) + l16;
@@ -276,16 +280,16 @@ __device__ __forceinline__ void w4_units_of(const LogitParams& p, const Schedule
 template <int MODE>
 __global__ __launch_bounds__(kW4Threads) void logprob_kernel_w4(const LogitParams p, int stream_w) {
   __shared__ __attribute__((aligned(1024))) char smem[kLdsBytes];
-  const int found = rows_found(p), rows = MODE == kStatistics ? found : p.max_rows;
+  const int found = rows_found(p), rows = MODE == kGradients ? p.max_rows : found;
   if (rows <= 0) return;
   const Schedule sched = choose_schedule_wave(p.sched, rows);
-  if (MODE == kStatistics && blockIdx.x == 0 && threadIdx.x == 0) {
+  if (MODE != kGradients && blockIdx.x == 0 && threadIdx.x == 0) {
     p.found[0] = 2 * sched.splits;
     p.found[1] = sched.stride;
   }
   const int units = sched.row_tiles * sched.splits, first = first_unit((int)blockIdx.x, (int)p.sched.grid, units);
   if (first >= units) return;
-  if constexpr (MODE == kStatistics) {
+  if constexpr (MODE != kGradients) {
     if (stream_w != 0 && sched.row_tiles == 1) {
       w4_units_of<MODE, true>(p, sched, rows, found, first, smem);
       return;
@@ -307,28 +311,5 @@ int launch(LogitParams p, hipStream_t stream) {
 }
 
 }  // namespace
-
-namespace logprob {
-
-constexpr int kRaggedKTiles = 5;   // as the mask-only pass
-
-bool w4_takes(int32_t d, int32_t V) {
-  return d % kTileK == 0 && V >= kVocab && (V % kVocab == 0 || d / kTileK >= kRaggedKTiles) && (int64_t)kVocab * d * 2 < (int64_t)1 << 32;
-}
-
-int64_t w4_list_bytes(int64_t max_rows) {
-  const int64_t width = max_rows >= 256 ? 8 : (max_rows + 31) / 32;   // row tiles no wider than that
-  (void)width;
-  return (int64_t)kCus * 4 * 64 * 8 * kListRoom * (int64_t)sizeof(Entry);
-}
-
-int launch_logprob_w4(const LogitParams& p, hipStream_t stream) { return launch<kStatistics>(p, stream); }
-
-int launch_logit_gradients_w4(const LogitParams& p, hipStream_t stream) {
-  LogitParams g = p;
-  g.sched.slots64 = INT32_MAX;
-  return launch<kGradients>(g, stream);
-}
-
-}  // namespace logprob
 }  // namespace mosaic
+#endif
