@@ -17,11 +17,62 @@ __device__ __forceinline__ int64_t rows_of(int64_t T, const int32_t* count) {
   return n < 0 ? 0 : n < T ? n : T;
 }
 
+// A block's lanes take eight columns of a stripe each: eight side by side or, so that a store of a wave fills whole lines where
+// the output has 32 bits, four and four more half a stripe on.
+template <typename O>
+struct Columns {
+  static constexpr bool kSplit = sizeof(O) == 4;
+  static constexpr int kSecond = kSplit ? kStripe / 2 : 4;   // from the first four to the others
+  static __device__ __forceinline__ int first(int stripe) { return stripe * kStripe + (int)threadIdx.x * (kSplit ? 4 : 8); }
+};
+__device__ __forceinline__ void load4(const __bf16* p, float* v) {
+  const bf16x4_t t = *reinterpret_cast<const bf16x4_t*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (float)t[i];
+}
+__device__ __forceinline__ void load4(const float* p, float* v) {
+  const f32x4_t t = *reinterpret_cast<const f32x4_t*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = t[i];
+}
+// The lane's columns of a row; c: the first.  (d is a multiple of 8, so a group of four is there or not.)
+template <typename O, typename S>
+__device__ __forceinline__ void load_columns(const S* row, int c, int d, float (&v)[8]) {
+  if constexpr (Columns<O>::kSplit) {
+    if (c < d) load4(row + c, v);
+    if (c + Columns<O>::kSecond < d) load4(row + c + Columns<O>::kSecond, v + 4);
+  } else {
+    if (c < d) load8(row + c, v);
+  }
+}
+// PAST: past the caches; what is written once and is larger than they are only takes the room of what is read.
+template <bool PAST>
+__device__ __forceinline__ void store_columns(float* row, int c, int d, const float (&v)[8]) {
+  const f32x4_t a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+  f32x4_t *const at = reinterpret_cast<f32x4_t*>(row + c), *const then = reinterpret_cast<f32x4_t*>(row + c + Columns<float>::kSecond);
+  if constexpr (PAST) {
+    if (c < d) __builtin_nontemporal_store(a, at);
+    if (c + Columns<float>::kSecond < d) __builtin_nontemporal_store(b, then);
+  } else {
+    if (c < d) *at = a;
+    if (c + Columns<float>::kSecond < d) *then = b;
+  }
+}
+template <bool PAST>
+__device__ __forceinline__ void store_columns(__bf16* row, int c, int d, const float (&v)[8]) {
+  bf16x8_t t;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = (__bf16)v[i];
+  if (c >= d) return;
+  if constexpr (PAST) __builtin_nontemporal_store(t, reinterpret_cast<bf16x8_t*>(row + c));
+  else *reinterpret_cast<bf16x8_t*>(row + c) = t;
+}
+
 // ---- lookup: out[t] = scale * table[tokens[t]], a block ROWS rows of a stripe of columns, all loads under way at once.
-template <typename S, typename O, int ROWS>
+template <typename S, typename O, int ROWS, bool PAST>
 __global__ __launch_bounds__(kThreads) void embedding_kernel(const EmbedArgs p) {
   const int64_t n = rows_of(p.T, p.count);
-  const int c = (int)blockIdx.y * kStripe + (int)threadIdx.x * 8;
+  const int c = Columns<O>::first((int)blockIdx.y);
   if (c >= p.d) return;
   for (int64_t t0 = (int64_t)blockIdx.x * ROWS; t0 < n; t0 += (int64_t)gridDim.x * ROWS) {
     int token[ROWS];
@@ -32,7 +83,7 @@ __global__ __launch_bounds__(kThreads) void embedding_kernel(const EmbedArgs p) 
     for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[r][i] = 0.f;
-      if ((uint32_t)token[r] < (uint32_t)p.V) load8(static_cast<const S*>(p.table) + (int64_t)token[r] * p.ld_table + c, v[r]);
+      if ((uint32_t)token[r] < (uint32_t)p.V) load_columns<O>(static_cast<const S*>(p.table) + (int64_t)token[r] * p.ld_table, c, p.d, v[r]);
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
@@ -41,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void embedding_kernel(const EmbedArgs p) 
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[r][i] *= p.scale;
       }
-      store8(static_cast<O*>(p.out) + (t0 + r) * p.ld_out + c, v[r]);
+      store_columns<PAST>(static_cast<O*>(p.out) + (t0 + r) * p.ld_out, c, p.d, v[r]);
     }
   }
 }
@@ -53,7 +104,8 @@ __global__ __launch_bounds__(kThreads) void embedding_kernel(const EmbedArgs p) 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMostDigitBits = 10, kMostBins = 1 << kMostDigitBits;
 constexpr int kMostSortBlocks = 64;
-constexpr int64_t kSortPiece = 4096;       // keys of a block, at least
+constexpr int kFillRows = 32;              // rows that a block fills
+constexpr int64_t kSortPiece = 2048;       // keys of a block, at least
 constexpr int64_t kOneBlockKeys = 8192;    // up to here one block sorts, in one launch
 
 struct SortArgs {
@@ -61,11 +113,10 @@ struct SortArgs {
   const int32_t* count;
   const int32_t *from_keys, *from_at;
   int32_t *to_keys, *to_at;
-  int32_t* counts;         // [bins, blocks]
-  uint32_t* present;
+  int32_t* counts;         // [blocks, kMostBins]
   int64_t n, piece;        // piece: keys of a block, a multiple of kSortThreads
   int32_t V, blocks, shift, bits;
-  int32_t first, last;     // whether this pass is the first, the last
+  int32_t first;           // whether this pass is the first
 };
 
 __device__ __forceinline__ int32_t key_at(const SortArgs& p, int64_t i, int64_t valid) {
@@ -74,21 +125,43 @@ __device__ __forceinline__ int32_t key_at(const SortArgs& p, int64_t i, int64_t 
   return (uint32_t)t < (uint32_t)p.V ? t : p.V;
 }
 
-__device__ __forceinline__ void clear_present(const SortArgs& p, int64_t first, int64_t stride) {
-  for (int64_t i = first; i < (p.V + 31) / 32; i += stride) p.present[i] = 0;
+// Part `part` of the memory that is to be filled, by block `block` of `blocks`: what sums go to is cleared while their tokens are
+// sorted, which takes a few blocks and little but waiting.
+struct FillPart { FillArgs fill; int64_t first, rows; };   // rows from `first` on
+__device__ __forceinline__ void fill_rows(const FillPart& p, int64_t block) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+  const uint32_t w = p.fill.word;
+  const u32x4_t v = {w, w, w, w};
+  const int64_t r0 = p.first + block * kFillRows, r1 = r0 + kFillRows < p.first + p.rows ? r0 + kFillRows : p.first + p.rows;
+  const int each = (int)(p.fill.row_bytes / 16);
+  int64_t r = r0 + (int)threadIdx.x / each;
+  int c = (int)threadIdx.x % each;
+  const int by_rows = kSortThreads / each, by_cols = kSortThreads % each;
+  while (r < r1) {
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(static_cast<char*>(p.fill.base) + r * p.fill.ld + (int64_t)c * 16));
+    r += by_rows;
+    c += by_cols;
+    if (c >= each) {
+      c -= each;
+      ++r;
+    }
+  }
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs p) {
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs p, const FillPart fill) {
   __shared__ int32_t bins[kMostBins];
+  if ((int)blockIdx.x >= p.blocks) {
+    fill_rows(fill, blockIdx.x - p.blocks);
+    return;
+  }
   const int n_bins = 1 << p.bits;
-  if (p.first) clear_present(p, (int64_t)blockIdx.x * kSortThreads + threadIdx.x, (int64_t)gridDim.x * kSortThreads);
   for (int b = threadIdx.x; b < n_bins; b += kSortThreads) bins[b] = 0;
   __syncthreads();
   const int64_t valid = rows_of(p.n, p.count), from = blockIdx.x * p.piece, end = from + p.piece < p.n ? from + p.piece : p.n;
   for (int64_t i = from + threadIdx.x; i < end; i += kSortThreads)
     atomicAdd(&bins[key_at(p, i, valid) >> p.shift & (n_bins - 1)], 1);
   __syncthreads();
-  for (int b = threadIdx.x; b < n_bins; b += kSortThreads) p.counts[(int64_t)b * p.blocks + blockIdx.x] = bins[b];
+  for (int b = threadIdx.x; b < n_bins; b += kSortThreads) p.counts[(int64_t)blockIdx.x * kMostBins + b] = bins[b];
 }
 
 struct SortLds {
@@ -96,31 +169,60 @@ struct SortLds {
   int32_t wave_sum[kSortWaves];
 };
 
-// One pass over block `block`'s piece.  `counts`: nullptr where it is the only block.
+// One pass over block `block`'s piece.  `counts`: nullptr where it is the only block.  A wave takes consecutive keys, 64 a round, and
+// holds those of up to kHeld rounds; beyond, it reads them again.
+constexpr int kHeld = 8;
 __device__ __forceinline__ void sort_piece(const SortArgs& p, SortLds& lds, int block, const int32_t* counts) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_bins = 1 << p.bits;
   const int64_t valid = rows_of(p.n, p.count);
-  // a wave takes consecutive keys, 64 a round
   const int64_t each = p.piece / kSortWaves, from = block * p.piece + wave * each;
   const int64_t end = from + each < p.n ? from + each : p.n;
-  for (int i = tid; i < kSortWaves * kMostBins; i += kSortThreads) (&lds.place[0][0])[i] = 0;
-  __syncthreads();
-  for (int64_t i = from + lane; i < end; i += 64) atomicAdd(&lds.place[wave][key_at(p, i, valid) >> p.shift & (n_bins - 1)], 1);
-  __syncthreads();
-  // a thread a digit (there are no more digits than threads)
-  int here = 0, ahead = 0, all = 0;
-  if (tid < n_bins) {
+  const bool held = each <= 64 * kHeld;
+  int32_t key_of[kHeld], at_of[kHeld];
 #pragma unroll
-    for (int w = 0; w < kSortWaves; ++w) here += lds.place[w][tid];
-    if (counts == nullptr) {
-      all = here;
-    } else {
-      for (int b = 0; b < p.blocks; ++b) {
-        const int c = counts[(int64_t)tid * p.blocks + b];
-        ahead += b < block ? c : 0;
-        all += c;
+  for (int r = 0; r < kHeld; ++r) {
+    const int64_t i = from + 64 * r + lane;
+    key_of[r] = 0;
+    at_of[r] = (int32_t)i;
+    if (held && i < end) {
+      key_of[r] = key_at(p, i, valid);
+      if (!p.first) at_of[r] = p.from_at[i];
+    }
+  }
+  // of a thread's digit (there are no more digits than threads): keys of other blocks that come ahead, and of all
+  int ahead = 0, all = 0;
+  if (counts != nullptr && tid < n_bins) {
+    constexpr int kAtOnce = 16;
+    for (int b0 = 0; b0 < p.blocks; b0 += kAtOnce) {
+      int c[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) c[i] = b0 + i < p.blocks ? counts[(int64_t)(b0 + i) * kMostBins + tid] : 0;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        ahead += b0 + i < block ? c[i] : 0;
+        all += c[i];
       }
     }
+  }
+  for (int b = lane; b < n_bins; b += 64) lds.place[wave][b] = 0;
+  __builtin_amdgcn_wave_barrier();
+  if (held) {
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r)
+      if (from + 64 * r + lane < end) atomicAdd(&lds.place[wave][key_of[r] >> p.shift & (n_bins - 1)], 1);
+  } else {
+    for (int64_t i = from + lane; i < end; i += 64) atomicAdd(&lds.place[wave][key_at(p, i, valid) >> p.shift & (n_bins - 1)], 1);
+  }
+  __syncthreads();
+  int here[kSortWaves];
+  if (tid < n_bins) {
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      here[w] = lds.place[w][tid];
+      sum += here[w];
+    }
+    if (counts == nullptr) all = sum;
   }
   int sum = all;   // inclusive, over the wave, then over the block
 #pragma unroll
@@ -135,18 +237,12 @@ __device__ __forceinline__ void sort_piece(const SortArgs& p, SortLds& lds, int 
     for (int w = 0; w < wave; ++w) at += lds.wave_sum[w];
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-      const int c = lds.place[w][tid];
       lds.place[w][tid] = at;
-      at += c;
+      at += here[w];
     }
   }
   __syncthreads();
-  for (int64_t i0 = from; i0 < end; i0 += 64) {
-    const int64_t i = i0 + lane;
-    const bool in = i < end;
-    const int32_t key = in ? key_at(p, i, valid) : 0;
-    const int32_t at = in ? (p.first ? (int32_t)i : p.from_at[i]) : 0;
-    const int32_t left = __shfl_up(key, 1, 64);
+  auto put = [&](bool in, int32_t key, int32_t at) __attribute__((always_inline)) {
     const int digit = key >> p.shift & (n_bins - 1);
     uint64_t same = __ballot(in);
     for (int b = 0; b < p.bits; ++b) {
@@ -162,24 +258,39 @@ __device__ __forceinline__ void sort_piece(const SortArgs& p, SortLds& lds, int 
     if (in) {
       p.to_keys[to + rank] = key;
       p.to_at[to + rank] = at;
-      // (positions of one token mostly lie side by side by then, and one of them says so)
-      if (p.last && key < p.V && (lane == 0 || key != left)) atomicOr(&p.present[key >> 5], 1u << (key & 31));
+    }
+  };
+  if (held) {
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r)
+      if (from + 64 * r < end) put(from + 64 * r + lane < end, key_of[r], at_of[r]);
+  } else {
+    for (int64_t i0 = from; i0 < end; i0 += 64) {
+      const bool in = i0 + lane < end;
+      put(in, in ? key_at(p, i0 + lane, valid) : 0, !in ? 0 : p.first ? (int32_t)(i0 + lane) : p.from_at[i0 + lane]);
     }
   }
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs p) {
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs p, const FillPart fill) {
   __shared__ SortLds lds;
+  if ((int)blockIdx.x >= p.blocks) {
+    fill_rows(fill, blockIdx.x - p.blocks);
+    return;
+  }
   sort_piece(p, lds, (int)blockIdx.x, p.counts);
 }
 
 // All passes in one block: keys and positions go to and fro between two buffers.
-__global__ __launch_bounds__(kSortThreads) void sort_one_block_kernel(SortArgs p, int32_t passes, int32_t* other_keys, int32_t* other_at) {
+__global__ __launch_bounds__(kSortThreads) void sort_one_block_kernel(SortArgs p, int32_t passes, int32_t* other_keys, int32_t* other_at,
+                                                                      const FillPart fill) {
   __shared__ SortLds lds;
-  clear_present(p, threadIdx.x, kSortThreads);
+  if (blockIdx.x > 0) {
+    fill_rows(fill, blockIdx.x - 1);
+    return;
+  }
   for (int pass = 0; pass < passes; ++pass) {
     p.first = pass == 0;
-    p.last = pass == passes - 1;
     sort_piece(p, lds, 0, nullptr);
     __threadfence_block();
     __syncthreads();
@@ -209,16 +320,14 @@ int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // ---- sums of rows by token.  A block takes kEach(n) sorted positions and a stripe of columns: 8 rows under way at once, added in
 // order; a token's sum goes out where the token ends.  A token whose positions reach over the end of a block's piece leaves a
-// partial sum there (0: it began ahead of the piece, 1: it goes on behind it), joined in order by a second kernel.  Blocks past
-// those of the sums clear the rows that no token names.
+// partial sum there (0: it began ahead of the piece, 1: it goes on behind it), joined in order by a second kernel.
 __host__ __device__ inline int each_of(int64_t n) { return n >= 32768 ? 64 : n >= 8192 ? 32 : n >= 2048 ? 16 : 8; }
 constexpr int kMostEach = 64;
-constexpr int kClearRows = 32;
 
 struct SumParams {
   TokenSumArgs a;
   int32_t each, stripes;
-  int64_t pieces, sum_blocks, blocks;   // blocks: those that sum, then those that clear
+  int64_t pieces, blocks;
 };
 constexpr int64_t kMostBlocks = 1 << 22;   // of a launch; further work is taken in turn
 
@@ -239,22 +348,11 @@ __device__ __forceinline__ void put_sum(const TokenSumArgs& a, int32_t key, int6
   store8(to, s);
 }
 
-// What one block does: piece and stripe `block`, or, past those, rows to clear.
+// Piece and stripe `block`.
 template <typename S, typename O>
-__device__ __forceinline__ void sum_or_clear(const SumParams& p, int64_t block, int32_t* keys, int32_t* ats, float* weights) {
+__device__ __forceinline__ void sum_piece(const SumParams& p, int64_t block, int32_t* keys, int32_t* ats, float* weights) {
   const TokenSumArgs& a = p.a;
   const int tid = threadIdx.x;
-  if (block >= p.sum_blocks) {
-    const int64_t r0 = (block - p.sum_blocks) * kClearRows;
-    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    static_assert(kClearRows == 32, "a word of bits");
-    const uint32_t present = a.sorted.present == nullptr ? 0u : a.sorted.present[r0 / 32];
-    for (int r = 0; r < kClearRows && r0 + r < a.V; ++r) {
-      if (present >> r & 1) continue;
-      for (int c = tid * 8; c < a.d; c += kStripe) store8(static_cast<O*>(a.sums) + (r0 + r) * a.ld_sums + c, zero);
-    }
-    return;
-  }
   const int64_t piece = block / p.stripes, e0 = piece * p.each;
   const int c = (int)(block % p.stripes) * kStripe + tid * 8;
   if (tid < p.each + 2) {
@@ -308,13 +406,44 @@ template <typename S, typename O>
 __global__ __launch_bounds__(kThreads) void token_sum_kernel(const SumParams p) {
   __shared__ int32_t keys[kMostEach + 2], ats[kMostEach];   // keys: with the ones before and behind the piece
   __shared__ float weights[kMostEach];
-  for (int64_t block = blockIdx.x; block < p.blocks; block += gridDim.x) sum_or_clear<S, O>(p, block, keys, ats, weights);
+  for (int64_t block = blockIdx.x; block < p.blocks; block += gridDim.x) sum_piece<S, O>(p, block, keys, ats, weights);
 }
 
 // Joins the partial sums of tokens that reach over pieces: a block looks through pieces (64 at once) for those at whose end a
-// token goes on that began in them; its 16 waves take a sixteenth of the token's partial sums each, in order, and the
-// sixteenths are added in order.  A lane has four columns.
-constexpr int kJoinWaves = 16;
+// token goes on that began in them.  A wave joins a token of few partial sums by itself, the block's waves taking such tokens in
+// turn; of one with more than kAlone the waves take a sixteenth each, in order, and the sixteenths are added in order.  A lane has
+// four columns.
+constexpr int kJoinWaves = 16, kAlone = 16;
+
+template <typename O>
+__device__ __forceinline__ void put_joined(const TokenSumArgs& a, int32_t key, int c, f32x4_t t) {
+  t *= a.scale;
+  const int64_t row = a.first != nullptr ? a.first[key] : key;
+  if constexpr (sizeof(O) == 4) {
+    f32x4_t* to = reinterpret_cast<f32x4_t*>(static_cast<float*>(a.sums) + row * a.ld_sums + c);
+    *to = a.accumulate ? *to + t : t;
+  } else {
+    *reinterpret_cast<bf16x4_t*>(static_cast<__bf16*>(a.sums) + row * a.ld_sums + c) =
+        bf16x4_t{(__bf16)t[0], (__bf16)t[1], (__bf16)t[2], (__bf16)t[3]};
+  }
+}
+// Partial sums m0 .. m1 - 1 of the token that goes on behind piece `from`, added in order, eight under way at once.
+__device__ __forceinline__ f32x4_t add_partials(const TokenSumArgs& a, int64_t from, int64_t m0, int64_t m1, int c, bool in) {
+  f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+  for (int64_t m = m0; m < m1; m += 8) {
+    f32x4_t v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const int64_t slot = m + i == 0 ? 2 * from + 1 : 2 * (from + m + i);
+      if (in && m + i < m1) v[i] = *reinterpret_cast<const f32x4_t*>(a.partials + slot * a.d + c);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += v[i];
+  }
+  return s;
+}
+
 template <typename O>
 __global__ __launch_bounds__(64 * kJoinWaves) void token_join_kernel(const SumParams p) {
   const TokenSumArgs& a = p.a;
@@ -322,62 +451,61 @@ __global__ __launch_bounds__(64 * kJoinWaves) void token_join_kernel(const SumPa
   const int c = ((int)blockIdx.x * 64 + lane) * 4;
   const bool in = c < a.d;
   __shared__ f32x4_t parts[kJoinWaves][64];
+  // How many partial sums the token has that goes on behind piece `from`: its own and those of pieces that begin inside of it, which
+  // are the first ones behind; the lanes probe 64 of them at once.
+  auto count_partials = [&](int64_t from, int32_t key) __attribute__((always_inline)) {
+    const int64_t past = (from + 1) * p.each;
+    int64_t more = 0, span = p.pieces - 1 - from;
+    for (bool near = true; span > 0; near = false) {
+      const int64_t step = near ? 1 : (span + 63) / 64, probe = more + (lane + 1) * step - 1, at = past + probe * p.each;
+      const uint64_t same = __ballot(probe < more + span && at < a.n && a.sorted.keys[at < a.n ? at : 0] == key);
+      const int64_t whole = ~same == 0 ? 64 : __builtin_ctzll(~same), rest = span - whole * step;
+      more += whole * step;
+      span = near ? (whole == 64 ? rest : 0) : step - 1 < rest ? step - 1 : rest;
+    }
+    return more + 1;
+  };
   for (int64_t base = (int64_t)blockIdx.y * 64; base < p.pieces; base += (int64_t)gridDim.y * 64) {
     const int64_t piece = base + lane, next = (piece + 1) * p.each;
     bool begins = false;
+    int32_t key_behind = a.V;
     if (next < a.n) {
-      const int32_t key = a.sorted.keys[next];
+      const int32_t key = key_behind = a.sorted.keys[next];
       // it reaches over the end, and the piece does not begin inside of it
       begins = key < a.V && a.sorted.keys[next - 1] == key && (piece == 0 || a.sorted.keys[piece * p.each - 1] != key);
     }
-    for (uint64_t left = __ballot(begins); left != 0; left &= left - 1) {
-      const int64_t from = base + __builtin_ctzll(left), past = (from + 1) * p.each;   // past: the first position behind the piece
-      const int32_t key = a.sorted.keys[past];
-      int64_t more = 0;   // pieces behind it that begin inside of the token
-      for (;;) {
-        const int64_t at = past + (more + lane) * p.each;
-        const uint64_t same = __ballot(at < a.n && a.sorted.keys[at < a.n ? at : 0] == key);
-        more += ~same == 0 ? 64 : __builtin_ctzll(~same);
-        if (~same != 0) break;
-      }
-      const int64_t all = more + 1, m0 = all * wave / kJoinWaves, m1 = all * (wave + 1) / kJoinWaves;
-      f32x4_t s = {0.f, 0.f, 0.f, 0.f};
-      for (int64_t m = m0; m < m1; m += 8) {
-        f32x4_t v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          v[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-          const int64_t slot = m + i == 0 ? 2 * from + 1 : 2 * (from + m + i);
-          if (in && m + i < m1) v[i] = *reinterpret_cast<const f32x4_t*>(a.partials + slot * a.d + c);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += v[i];
-      }
-      parts[wave][lane] = s;
+    const uint64_t found = __ballot(begins);
+    // A token of more partial sums than kAlone is that of the last piece found in 64, or the next one found lies as far behind.
+    int turn = 0;
+    for (uint64_t left = found; left != 0; left &= left - 1, ++turn) {
+      if (turn % kJoinWaves != wave) continue;
+      const int64_t from = base + __builtin_ctzll(left);
+      const int32_t key = __shfl(key_behind, __builtin_ctzll(left), 64);
+      const int64_t all = count_partials(from, key);
+      if (all > kAlone) continue;
+      const f32x4_t s = add_partials(a, from, 0, all, c, in);
+      if (in) put_joined<O>(a, key, c, s);
+    }
+    for (uint64_t left = found; left != 0; left &= left - 1) {
+      const int64_t from = base + __builtin_ctzll(left), behind = (left & (left - 1)) != 0 ? base + __builtin_ctzll(left & (left - 1)) : p.pieces;
+      if (behind - from < kAlone) continue;   // it has ended by then
+      const int32_t key = __shfl(key_behind, __builtin_ctzll(left), 64);
+      const int64_t all = count_partials(from, key);
+      if (all <= kAlone) continue;
+      parts[wave][lane] = add_partials(a, from, all * wave / kJoinWaves, all * (wave + 1) / kJoinWaves, c, in);
       __syncthreads();
       if (wave == 0 && in) {
         f32x4_t t = parts[0][lane];
 #pragma unroll
         for (int w = 1; w < kJoinWaves; ++w) t += parts[w][lane];
-        t *= a.scale;
-        int64_t row = key;
-        if (a.first != nullptr) row = a.first[key];
-        if constexpr (sizeof(O) == 4) {
-          f32x4_t* to = reinterpret_cast<f32x4_t*>(static_cast<float*>(a.sums) + row * a.ld_sums + c);
-          *to = a.accumulate ? *to + t : t;
-        } else {
-          *reinterpret_cast<bf16x4_t*>(static_cast<__bf16*>(a.sums) + row * a.ld_sums + c) =
-              bf16x4_t{(__bf16)t[0], (__bf16)t[1], (__bf16)t[2], (__bf16)t[3]};
-        }
+        put_joined<O>(a, key, c, t);
       }
       __syncthreads();
     }
   }
 }
 
-__global__ __launch_bounds__(kThreads) void fill_none_kernel(int32_t* first, int32_t V) {
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < V; i += (int64_t)gridDim.x * kThreads) first[i] = -1;
-}
+__global__ __launch_bounds__(kSortThreads) void fill_kernel(const FillPart p) { fill_rows(p, blockIdx.x); }
 
 // ---- dropout
 
@@ -396,9 +524,9 @@ __device__ __forceinline__ void philox(uint32_t (&c)[4], uint32_t k0, uint32_t k
   }
 }
 
-template <typename S, typename O, bool ADD, int ROWS>
+template <typename S, typename O, bool ADD, int ROWS, bool PAST>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(const DropoutArgs p) {
-  const int c = (int)blockIdx.y * kStripe + (int)threadIdx.x * 8;
+  const int c = (int)blockIdx.y * kStripe + (int)threadIdx.x * 8;   // eight columns share the generator's words
   if (c >= p.d) return;
   for (int64_t t0 = (int64_t)blockIdx.x * ROWS; t0 < p.T; t0 += (int64_t)gridDim.x * ROWS) {
     float v[ROWS][8], add[ADD ? ROWS : 1][8];
@@ -421,7 +549,9 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const DropoutArgs p) 
         v[r][i] = bits >= p.border ? v[r][i] * p.grow : 0.f;
         if constexpr (ADD) v[r][i] += add[r][i];
       }
-      store8(static_cast<O*>(p.out) + (t0 + r) * p.ld_out + c, v[r]);
+      O* const out = static_cast<O*>(p.out) + (t0 + r) * p.ld_out;
+      if constexpr (PAST && sizeof(O) == 2) store_columns<true>(out, c, p.d, v[r]);
+      else store8(out + c, v[r]);
     }
   }
 }
@@ -434,17 +564,22 @@ dim3 row_grid(int64_t T, int rows, int d) {
 // Rows of a block: several once there are blocks enough.
 bool many_rows(int64_t T, int32_t d) { return T * ((d + kStripe - 1) / kStripe) >= 8192; }
 constexpr int kManyRows = 4;
+constexpr int64_t kPastBytes = (int64_t)256 << 20;   // an output as large as the memory-side cache
 
 template <typename S, typename O>
 int launch_embedding(const EmbedArgs& a, hipStream_t stream) {
-  if (many_rows(a.T, a.d)) return launch_kernel(embedding_kernel<S, O, kManyRows>, row_grid(a.T, kManyRows, a.d), dim3(kThreads), stream, a);
-  return launch_kernel(embedding_kernel<S, O, 1>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
+  if (a.T * a.d * (int64_t)sizeof(O) >= kPastBytes)
+    return launch_kernel(embedding_kernel<S, O, kManyRows, true>, row_grid(a.T, kManyRows, a.d), dim3(kThreads), stream, a);
+  if (many_rows(a.T, a.d)) return launch_kernel(embedding_kernel<S, O, kManyRows, false>, row_grid(a.T, kManyRows, a.d), dim3(kThreads), stream, a);
+  return launch_kernel(embedding_kernel<S, O, 1, false>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
 }
 
 template <typename S, typename O, bool ADD>
 int launch_dropout_as(const DropoutArgs& a, hipStream_t stream) {
-  if (many_rows(a.T, a.d)) return launch_kernel(dropout_kernel<S, O, ADD, kManyRows>, row_grid(a.T, kManyRows, a.d), dim3(kThreads), stream, a);
-  return launch_kernel(dropout_kernel<S, O, ADD, 1>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
+  if (a.T * a.d * (int64_t)sizeof(O) >= kPastBytes)
+    return launch_kernel(dropout_kernel<S, O, ADD, kManyRows, true>, row_grid(a.T, kManyRows, a.d), dim3(kThreads), stream, a);
+  if (many_rows(a.T, a.d)) return launch_kernel(dropout_kernel<S, O, ADD, kManyRows, false>, row_grid(a.T, kManyRows, a.d), dim3(kThreads), stream, a);
+  return launch_kernel(dropout_kernel<S, O, ADD, 1, false>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
 }
 
 template <typename S, typename O>
@@ -466,12 +601,33 @@ int launch_embedding_forward(const EmbedArgs& a, bool table_f32, bool out_f32, h
   return out_f32 ? launch_embedding<__bf16, float>(a, stream) : launch_embedding<__bf16, __bf16>(a, stream);
 }
 
-// Two buffers of keys and positions, the digits' counts, the bits of what is present.
-int64_t sort_tokens_bytes(int64_t n, int32_t V) {
-  return 4 * padded(4 * n) + padded((int64_t)kMostBins * kMostSortBlocks * 4) + padded(((int64_t)V + 31) / 32 * 4);
+// Two buffers of keys and positions, the digits' counts.
+int64_t sort_tokens_bytes(int64_t n) { return 4 * padded(4 * n) + padded((int64_t)kMostBins * kMostSortBlocks * 4); }
+
+namespace {
+constexpr int64_t kMostFillBlocks = 1 << 20;   // of a launch (rows past them: a block fills more)
+// Part l of `of` of what is to be filled, and the blocks it takes.
+FillPart fill_part(const FillArgs& f, int l, int of, int64_t* blocks) {
+  const int64_t tiles = (f.rows + kFillRows - 1) / kFillRows, from = tiles * l / of, to = tiles * (l + 1) / of;
+  FillPart p = {f, from * kFillRows, 0};
+  p.rows = (to * kFillRows < f.rows ? to * kFillRows : f.rows) - p.first;
+  if (p.rows < 0) p.rows = 0;
+  *blocks = (p.rows + kFillRows - 1) / kFillRows;
+  return p;
+}
+}  // namespace
+
+int launch_fill(const FillArgs& f, hipStream_t stream) {
+  const int of = (int)((f.rows + kFillRows * kMostFillBlocks - 1) / (kFillRows * kMostFillBlocks));
+  for (int l = 0; l < of; ++l) {
+    int64_t blocks;
+    const FillPart p = fill_part(f, l, of, &blocks);
+    if (blocks > 0 && launch_kernel(fill_kernel, dim3((unsigned)blocks), dim3(kSortThreads), stream, p) != 0) return -1;
+  }
+  return 0;
 }
 
-int launch_sort_tokens(const int32_t* tokens, int64_t n, const int32_t* count, int32_t V, void* space, SortedTokens* out,
+int launch_sort_tokens(const int32_t* tokens, int64_t n, const int32_t* count, int32_t V, void* space, const FillArgs& fill, SortedTokens* out,
                        hipStream_t stream) {
   const SortPlan plan = plan_sort(n, V);
   char* at = static_cast<char*>(space);
@@ -486,29 +642,37 @@ int launch_sort_tokens(const int32_t* tokens, int64_t n, const int32_t* count, i
   a.tokens = tokens;
   a.count = count;
   a.counts = reinterpret_cast<int32_t*>(at);
-  a.present = reinterpret_cast<uint32_t*>(at + padded((int64_t)kMostBins * kMostSortBlocks * 4));
   a.n = n;
   a.piece = plan.piece;
   a.V = V;
   a.blocks = plan.blocks;
   a.bits = plan.bits;
   const int last = (plan.passes - 1) & 1;
-  *out = SortedTokens{keys[last], ats[last], a.present};
+  *out = SortedTokens{keys[last], ats[last]};
   a.to_keys = keys[0];
   a.to_at = ats[0];
-  if (plan.blocks == 1)
-    return launch_kernel(sort_one_block_kernel, dim3(1), dim3(kSortThreads), stream, a, plan.passes, keys[1], ats[1]);
+  const int launches = plan.blocks == 1 ? 1 : 2 * plan.passes;
+  FillArgs f = fill;
+  if (f.rows > kFillRows * kMostFillBlocks) {   // more than these launches have blocks for
+    if (launch_fill(f, stream) != 0) return -1;
+    f.rows = 0;
+  }
+  int64_t blocks;
+  if (plan.blocks == 1) {
+    const FillPart part = fill_part(f, 0, 1, &blocks);
+    return launch_kernel(sort_one_block_kernel, dim3((unsigned)(1 + blocks)), dim3(kSortThreads), stream, a, plan.passes, keys[1], ats[1], part);
+  }
   for (int pass = 0; pass < plan.passes; ++pass) {
     a.first = pass == 0;
-    a.last = pass == plan.passes - 1;
     a.shift = pass * plan.bits;
     a.from_keys = keys[(pass + 1) & 1];
     a.from_at = ats[(pass + 1) & 1];
     a.to_keys = keys[pass & 1];
     a.to_at = ats[pass & 1];
-    if (launch_kernel(sort_count_kernel, dim3((unsigned)plan.blocks), dim3(kSortThreads), stream, a) != 0 ||
-        launch_kernel(sort_place_kernel, dim3((unsigned)plan.blocks), dim3(kSortThreads), stream, a) != 0)
-      return -1;
+    FillPart part = fill_part(f, 2 * pass, launches, &blocks);
+    if (launch_kernel(sort_count_kernel, dim3((unsigned)(plan.blocks + blocks)), dim3(kSortThreads), stream, a, part) != 0) return -1;
+    part = fill_part(f, 2 * pass + 1, launches, &blocks);
+    if (launch_kernel(sort_place_kernel, dim3((unsigned)(plan.blocks + blocks)), dim3(kSortThreads), stream, a, part) != 0) return -1;
   }
   return 0;
 }
@@ -521,12 +685,7 @@ int launch_token_sums(const TokenSumArgs& a, bool rows_f32, bool sums_f32, hipSt
   p.each = each_of(a.n);
   p.stripes = (a.d + kStripe - 1) / kStripe;
   p.pieces = (a.n + p.each - 1) / p.each;
-  p.sum_blocks = p.pieces * p.stripes;
-  if (a.first != nullptr &&
-      launch_kernel(fill_none_kernel, dim3((unsigned)((a.V + kThreads - 1) / kThreads < 1024 ? (a.V + kThreads - 1) / kThreads : 1024)),
-                    dim3(kThreads), stream, a.first, a.V) != 0)
-    return -1;
-  p.blocks = p.sum_blocks + (a.accumulate || a.first != nullptr ? 0 : ((int64_t)a.V + kClearRows - 1) / kClearRows);
+  p.blocks = p.pieces * p.stripes;
   if (rows_f32) return sums_f32 ? launch_sums<float, float>(p, stream) : launch_sums<float, __bf16>(p, stream);
   return sums_f32 ? launch_sums<__bf16, float>(p, stream) : launch_sums<__bf16, __bf16>(p, stream);
 }

@@ -643,6 +643,8 @@ struct GradientSpace {
   int64_t dl_rows;
   int32_t splits;
 };
+constexpr int64_t kSlotBytes = 4096;   // the slots are filled in rows of so many bytes
+int64_t slot_rows(int32_t V) { return (4 * (int64_t)V + kSlotBytes - 1) / kSlotBytes; }
 GradientSpace gradient_space(int64_t max_rows, int32_t d, int32_t V) {
   GradientSpace s;
   const bool low = max_rows <= kLowRows;
@@ -651,10 +653,10 @@ GradientSpace gradient_space(int64_t max_rows, int32_t d, int32_t V) {
   s.rows = 0;
   s.coef = s.rows + padded(2 * max_rows * d);
   s.sort = s.coef + padded(4 * max_rows);
-  s.sums = s.sort + padded(sort_tokens_bytes(max_rows, V));
+  s.sums = s.sort + padded(sort_tokens_bytes(max_rows));
   s.extra = s.sums + padded(4 * token_sum_partials(max_rows) * d);
   s.slot = s.extra + padded(4 * max_rows * d);
-  s.parts = s.slot + padded(4 * (int64_t)V);
+  s.parts = s.slot + slot_rows(V) * kSlotBytes;
   s.dl = s.parts + padded(4 * s.splits * s.dl_rows * d);
   s.least = s.dl + 2 * s.dl_rows * kVocab;
   return s;
@@ -724,7 +726,8 @@ int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
     if (launch_kernel(target_terms_kernel, dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(256), stream, t) != 0) return -1;
     if (dw) {
       TokenSumArgs sum = {};
-      if (launch_sort_tokens(a.targets, a.max_rows, a.count, a.V, ws + at.sort, &sum.sorted, stream) != 0) return -1;
+      const FillArgs none = {slot, kSlotBytes, slot_rows(a.V), kSlotBytes, 0xffffffffu};   // no target names an id: -1
+      if (launch_sort_tokens(a.targets, a.max_rows, a.count, a.V, ws + at.sort, none, &sum.sorted, stream) != 0) return -1;
       sum.rows = rows;
       sum.weights = coef;
       sum.partials = reinterpret_cast<float*>(ws + at.sums);

@@ -25,11 +25,16 @@ bool bad_list(const int32_t* tokens, const int32_t* count) { return tokens == nu
 struct EmbeddingSpace {
   int64_t partials, total;   // offsets, bytes; the sort's space comes first
 };
-EmbeddingSpace embedding_space(int64_t T, int32_t d, int32_t V) {
+EmbeddingSpace embedding_space(int64_t T, int32_t d) {
   EmbeddingSpace s;
-  s.partials = mosaic::sort_tokens_bytes(T, V);
+  s.partials = mosaic::sort_tokens_bytes(T);
   s.total = s.partials + 4 * mosaic::token_sum_partials(T) * d;
   return s;
+}
+
+mosaic::FillArgs clear_matrix(void* base, int32_t type, int64_t ld, int64_t rows, int32_t d) {
+  const int64_t bytes = type == MOSAIC_F32 ? 4 : 2;
+  return mosaic::FillArgs{base, ld * bytes, rows, d * bytes, 0u};
 }
 
 int check_dropout(int32_t type, int64_t T, int32_t d, float p, int32_t site, int64_t first_row) {
@@ -90,7 +95,7 @@ int mosaic_embedding_forward(const int32_t* tokens, int64_t T, const int32_t* co
 
 int64_t mosaic_embedding_backward_workspace_bytes(int64_t T, int32_t d, int32_t V) {
   if (check_sizes(T, d, MOSAIC_MAX_ROW) != MOSAIC_OK || check_vocab(V) != MOSAIC_OK) return 0;
-  return embedding_space(T, d, V).total;
+  return embedding_space(T, d).total;
 }
 
 int mosaic_embedding_backward(const void* dout, int32_t dout_type, int64_t ld_dout, const int32_t* tokens, int64_t T,
@@ -111,10 +116,12 @@ int mosaic_embedding_backward(const void* dout, int32_t dout_type, int64_t ld_do
     return MOSAIC_OK;
   }
   hipStream_t on = static_cast<hipStream_t>(stream);
+  const mosaic::FillArgs fill = clear_matrix(dtable, dtable_type, ld_dtable, accumulate != 0 ? 0 : V, d);
+  if (T == 0) return launched(mosaic::launch_fill(fill, on));
   mosaic::TokenSumArgs a = {};
-  if (T > 0 && mosaic::launch_sort_tokens(tokens, T, count, V, workspace, &a.sorted, on) != 0) return MOSAIC_ERR_HIP;
+  if (mosaic::launch_sort_tokens(tokens, T, count, V, workspace, fill, &a.sorted, on) != 0) return MOSAIC_ERR_HIP;
   a.rows = dout;
-  a.partials = T > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + embedding_space(T, d, V).partials) : nullptr;
+  a.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + embedding_space(T, d).partials);
   a.sums = dtable;
   a.n = T;
   a.ld_rows = ld_dout;
@@ -235,12 +242,7 @@ int mosaic_masked_logprobs_backward(const void* hidden, int64_t ld_h, int64_t T,
   hipStream_t on = static_cast<hipStream_t>(stream);
   if (!some) {   // no rows: dw is cleared
     if (dw == nullptr || accumulate != 0) return MOSAIC_OK;
-    mosaic::TokenSumArgs none = {};
-    none.sums = dw;
-    none.ld_sums = ld_dw;
-    none.V = V;
-    none.d = d;
-    return launched(mosaic::launch_token_sums(none, false, dw_type == MOSAIC_F32, on));
+    return launched(mosaic::launch_fill(clear_matrix(dw, dw_type, ld_dw, V, d), on));
   }
   mosaic::LogprobBackwardArgs a = {};
   a.hidden = hidden;

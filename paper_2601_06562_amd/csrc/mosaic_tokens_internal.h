@@ -19,15 +19,22 @@ struct EmbedArgs {
 };
 int launch_embedding_forward(const EmbedArgs& a, bool table_f32, bool out_f32, hipStream_t stream);
 
+// Memory to be filled with a word: `rows` rows, `ld` bytes apart, of `row_bytes` bytes, a multiple of 16 as the base is.
+struct FillArgs {
+  void* base;
+  int64_t ld, rows, row_bytes;
+  uint32_t word;
+};
+int launch_fill(const FillArgs& f, hipStream_t stream);
+
 // Positions sorted by their tokens: keys ascending, positions of a key ascending; what is left out has the key V and comes last.
 struct SortedTokens {
   int32_t* keys;       // [n]
   int32_t* at;         // [n]
-  uint32_t* present;   // a bit for each of V ids: some token names it
 };
-// Bytes that sorting n tokens of V takes, and where in them the results are.
-int64_t sort_tokens_bytes(int64_t n, int32_t V);
-int launch_sort_tokens(const int32_t* tokens, int64_t n, const int32_t* count, int32_t V, void* space, SortedTokens* out,
+// Bytes that sorting n tokens takes.  `fill` (of no rows: nothing) is filled beside the sort.
+int64_t sort_tokens_bytes(int64_t n);
+int launch_sort_tokens(const int32_t* tokens, int64_t n, const int32_t* count, int32_t V, void* space, const FillArgs& fill, SortedTokens* out,
                        hipStream_t stream);
 
 // Sums of rows by token, over sorted positions.
@@ -36,8 +43,8 @@ struct TokenSumArgs {
   const void* rows;      // [n, ld_rows]
   const float* weights;  // a factor for each row, or nullptr
   float* partials;       // [token_sum_partials(n), d]
-  void* sums;            // of token v: row v; compact: row first[v], the place of its first position
-  int32_t* first;        // compact: [V], -1 where no token names v; else nullptr
+  void* sums;            // of token v: row v; compact: row first[v], the place of its first position.  Rows without tokens are not written
+  int32_t* first;        // compact: [V], written for tokens that there are; else nullptr
   int64_t n, ld_rows, ld_sums;
   int32_t V, d, accumulate;
   float scale;
