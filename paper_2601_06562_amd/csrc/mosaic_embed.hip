@@ -416,9 +416,8 @@ __global__ __launch_bounds__(kThreads) void token_sum_kernel(const SumParams p) 
 constexpr int kJoinWaves = 16, kAlone = 16;
 
 template <typename O>
-__device__ __forceinline__ void put_joined(const TokenSumArgs& a, int32_t key, int c, f32x4_t t) {
+__device__ __forceinline__ void put_joined(const TokenSumArgs& a, int64_t row, int c, f32x4_t t) {
   t *= a.scale;
-  const int64_t row = a.first != nullptr ? a.first[key] : key;
   if constexpr (sizeof(O) == 4) {
     f32x4_t* to = reinterpret_cast<f32x4_t*>(static_cast<float*>(a.sums) + row * a.ld_sums + c);
     *to = a.accumulate ? *to + t : t;
@@ -451,54 +450,64 @@ __global__ __launch_bounds__(64 * kJoinWaves) void token_join_kernel(const SumPa
   const int c = ((int)blockIdx.x * 64 + lane) * 4;
   const bool in = c < a.d;
   __shared__ f32x4_t parts[kJoinWaves][64];
-  // How many partial sums the token has that goes on behind piece `from`: its own and those of pieces that begin inside of it, which
-  // are the first ones behind; the lanes probe 64 of them at once.
-  auto count_partials = [&](int64_t from, int32_t key) __attribute__((always_inline)) {
+  // How many partial sums the token `key` has that goes on behind piece `from`, the one of lane `at`: its own and those of pieces that
+  // begin inside of it, which are the first ones behind.  `key_behind` tells it for the pieces from `at` on; where they all are in
+  // the token, the lanes probe 64 further ones at once.
+  auto count_partials = [&](int64_t from, int at, int32_t key, int32_t key_behind) __attribute__((always_inline)) {
     const int64_t past = (from + 1) * p.each;
-    int64_t more = 0, span = p.pieces - 1 - from;
-    for (bool near = true; span > 0; near = false) {
-      const int64_t step = near ? 1 : (span + 63) / 64, probe = more + (lane + 1) * step - 1, at = past + probe * p.each;
-      const uint64_t same = __ballot(probe < more + span && at < a.n && a.sorted.keys[at < a.n ? at : 0] == key);
+    const uint64_t others = ~(__ballot(key_behind == key) >> at);   // (what comes in from above counts as others)
+    const int near = others == 0 ? 64 : __builtin_ctzll(others);     // no bit at all: lane 0 and 64 pieces in one token
+    const bool ended = near < 64 - at;
+    int64_t more = near, span = ended ? 0 : p.pieces - 1 - from - near;
+    while (span > 0) {
+      const int64_t step = (span + 63) / 64, probe = more + (lane + 1) * step - 1, e = past + probe * p.each;
+      const uint64_t same = __ballot(probe < more + span && e < a.n && a.sorted.keys[e < a.n ? e : 0] == key);
       const int64_t whole = ~same == 0 ? 64 : __builtin_ctzll(~same), rest = span - whole * step;
       more += whole * step;
-      span = near ? (whole == 64 ? rest : 0) : step - 1 < rest ? step - 1 : rest;
+      span = step - 1 < rest ? step - 1 : rest;
     }
     return more + 1;
   };
   for (int64_t base = (int64_t)blockIdx.y * 64; base < p.pieces; base += (int64_t)gridDim.y * 64) {
+    // keys behind the piece, at its end, ahead of it: all asked for at once, since what another kernel wrote is far away
     const int64_t piece = base + lane, next = (piece + 1) * p.each;
-    bool begins = false;
-    int32_t key_behind = a.V;
+    int32_t key_behind = a.V, key_last = a.V, key_ahead = a.V;
     if (next < a.n) {
-      const int32_t key = key_behind = a.sorted.keys[next];
-      // it reaches over the end, and the piece does not begin inside of it
-      begins = key < a.V && a.sorted.keys[next - 1] == key && (piece == 0 || a.sorted.keys[piece * p.each - 1] != key);
+      key_behind = a.sorted.keys[next];
+      key_last = a.sorted.keys[next - 1];
+      if (piece > 0) key_ahead = a.sorted.keys[piece * p.each - 1];
     }
+    // a token reaches over the end, and the piece does not begin inside of it
+    const bool begins = key_behind < a.V && key_last == key_behind && key_ahead != key_behind;
     const uint64_t found = __ballot(begins);
     // A token of more partial sums than kAlone is that of the last piece found in 64, or the next one found lies as far behind.
     int turn = 0;
     for (uint64_t left = found; left != 0; left &= left - 1, ++turn) {
       if (turn % kJoinWaves != wave) continue;
-      const int64_t from = base + __builtin_ctzll(left);
-      const int32_t key = __shfl(key_behind, __builtin_ctzll(left), 64);
-      const int64_t all = count_partials(from, key);
+      const int at = __builtin_ctzll(left);
+      const int64_t from = base + at;
+      const int32_t key = __shfl(key_behind, at, 64);
+      const int64_t all = count_partials(from, at, key, key_behind);
       if (all > kAlone) continue;
+      const int64_t row = a.first != nullptr ? a.first[key] : key;
       const f32x4_t s = add_partials(a, from, 0, all, c, in);
-      if (in) put_joined<O>(a, key, c, s);
+      if (in) put_joined<O>(a, row, c, s);
     }
     for (uint64_t left = found; left != 0; left &= left - 1) {
-      const int64_t from = base + __builtin_ctzll(left), behind = (left & (left - 1)) != 0 ? base + __builtin_ctzll(left & (left - 1)) : p.pieces;
+      const int at = __builtin_ctzll(left);
+      const int64_t from = base + at, behind = (left & (left - 1)) != 0 ? base + __builtin_ctzll(left & (left - 1)) : p.pieces;
       if (behind - from < kAlone) continue;   // it has ended by then
-      const int32_t key = __shfl(key_behind, __builtin_ctzll(left), 64);
-      const int64_t all = count_partials(from, key);
+      const int32_t key = __shfl(key_behind, at, 64);
+      const int64_t all = count_partials(from, at, key, key_behind);
       if (all <= kAlone) continue;
+      const int64_t row = a.first != nullptr ? a.first[key] : key;
       parts[wave][lane] = add_partials(a, from, all * wave / kJoinWaves, all * (wave + 1) / kJoinWaves, c, in);
       __syncthreads();
       if (wave == 0 && in) {
         f32x4_t t = parts[0][lane];
 #pragma unroll
         for (int w = 1; w < kJoinWaves; ++w) t += parts[w][lane];
-        put_joined<O>(a, key, c, t);
+        put_joined<O>(a, row, c, t);
       }
       __syncthreads();
     }

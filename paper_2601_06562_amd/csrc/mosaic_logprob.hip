@@ -248,7 +248,9 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
       const int64_t v = (int64_t)done_vt * kVocab + wp * kHalf;
       const int q0 = done_row0 + wq * 16 * QB, g = lane >> 4;
       if constexpr (MODE == kGradients) {
-        gradient_tile<QB, false>(load, v, q0, found);
+        GradientRows<QB> of;
+        of.read(p, q0, found);
+        gradient_tile<QB, false>(load, of, v, q0, found);
       } else {
         if (done_tiles == 0) st.clear(q0, rows);
         const int own_row = q0 + 16 * g + (lane & 15);

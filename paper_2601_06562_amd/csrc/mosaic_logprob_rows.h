@@ -510,19 +510,41 @@ __device__ __forceinline__ bool sort_now(int tiles, int of) { return tiles == of
 //   dl[v] = - p[v] (g + h (log p[v] + H))      g, h: the gradients of the row's log probability and entropy H
 // with 0 at the target, whose one-hot term outweighs the others; the target's whole term goes past the 16 bits.
 // v0: the first id of the wave.
+template <int QB>
+struct GradientRows {   // what a lane holds of its own rows (as Rows)
+  static constexpr int kOwn = (QB + 3) / 4;
+  float lse[kOwn], g[kOwn], h[kOwn], entropy[kOwn];
+  int target[kOwn];
+
+  __device__ __forceinline__ void read(const LogitParams& p, int row0, int found) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      const int row = row0 + 64 * k + lane;
+      const bool listed = 4 * k + (lane >> 4) < QB && row < found;
+      lse[k] = listed ? in_memory(p.lse)[row] : 0.f;
+      target[k] = listed && p.targets != nullptr ? in_memory(p.targets)[row] : -1;
+      g[k] = (uint32_t)target[k] < (uint32_t)p.all_ids ? in_memory(p.dlogprob)[row] : 0.f;
+      h[k] = listed && p.dentropy != nullptr ? in_memory(p.dentropy)[row] : 0.f;
+      entropy[k] = listed && p.dentropy != nullptr ? in_memory(p.entropy)[row] : 0.f;
+    }
+  }
+};
 template <int QB, bool ROLLED, class Load>
-__device__ __forceinline__ void gradient_tile(Load load, int64_t v0, int row0, int found) {
+__device__ __forceinline__ void gradient_tile(Load load, const GradientRows<QB>& of, int64_t v0, int row0, int found) {
   const Arguments p = arguments_again();
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, run = first_of<4>(lane);
   const int there = p->V - v0 < kHalf ? (int)(p->V - v0) - 4 * g4 : kHalf;   // ids there are from this lane's first on
   each_column<ROLLED, QB>([&](int j) __attribute__((always_inline)) {
-    const int row = row0 + 16 * j + l16;
+    const int owner = 16 * (j & 3) + l16, row = row0 + 16 * j + l16;
     const bool in = row < p->max_rows, listed = row < found;
-    const float lse = listed ? in_memory(p->lse)[row] : 0.f;
-    const int target = listed && p->targets != nullptr ? in_memory(p->targets)[row] : -1;
-    const float g = (uint32_t)target < (uint32_t)p->all_ids ? in_memory(p->dlogprob)[row] : 0.f;
-    const float h = listed && p->dentropy != nullptr ? in_memory(p->dentropy)[row] : 0.f;
-    const float entropy = listed && p->dentropy != nullptr ? in_memory(p->entropy)[row] : 0.f;
+    const float lse = __shfl(pick(of.lse, j >> 2), owner, 64), g = __shfl(pick(of.g, j >> 2), owner, 64);
+    float h = 0.f, entropy = 0.f;
+    if (p->dentropy != nullptr) {
+      h = __shfl(pick(of.h, j >> 2), owner, 64);
+      entropy = __shfl(pick(of.entropy, j >> 2), owner, 64);
+    }
+    const int target = __shfl(pick(of.target, j >> 2), owner, 64);
     const int64_t from = (int64_t)target - p->first_id - v0;
     const int rel = target >= 0 && from >= 0 && from < kHalf ? (int)from - 4 * g4 : -kHalf;
     float x[32];

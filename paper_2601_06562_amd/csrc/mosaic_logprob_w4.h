@@ -203,8 +203,10 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
     uint32_t st_wk = (uint32_t)((kPairs && gw >= total_steps ? total_steps - 1 : gw) % nk), st_hk = (uint32_t)(gh % nk);
     uint32_t st_g = 0;
 
-    Rows<NB> st;
-    st.clear(first_row, rows);
+    [[maybe_unused]] Rows<NB> st;
+    [[maybe_unused]] GradientRows<NB> of;
+    if constexpr (MODE == kGradients) of.read(p, first_row, found);
+    else st.clear(first_row, rows);
     const int64_t of_half = (int64_t)(2 * sp + wv) * sched.stride;
     auto place = [&](int k, bool& in) __attribute__((always_inline)) {
       const int row = first_row + 16 * (4 * k + q) + l16;
@@ -241,7 +243,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
       };
       const int64_t v = first_id(vt0 + n) + wv * kHalf;
       if constexpr (MODE == kGradients) {
-        gradient_tile<NB, true>(load, v, first_row, found);
+        gradient_tile<NB, true>(load, of, v, first_row, found);
       } else {
         const int64_t from = vt0 + n == ragged_tile ? (int64_t)ragged_tile * kVocab : 0;
         reduce_tile<NB, true, MODE == kAlternatives>(load, st, v + 4 * q, from, p.V, target, first_row, lists, n == 0, sort_now(n + 1, ntile), place);

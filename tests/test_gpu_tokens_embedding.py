@@ -113,6 +113,18 @@ def test_gradient(T, d, V, kind):
     assert torch.equal(again, got)
 
 
+@pytest.mark.parametrize("lengths", [(511, 1), (512,), (513,), (520, 7), (8, 512, 8), (7, 513, 519, 8), (512, 512, 512), (1, 1023, 900),
+                                     (127, 129, 8, 8, 136, 1), (1600,)])
+def test_gradient_of_tokens_of_many_rows(lengths):
+    """Rows of one token that end at, just before and just behind multiples of what one wave adds (8 rows) and looks at (512)."""
+    gen = generator(sum(lengths) + len(lengths))
+    T, d, V = sum(lengths), 264, len(lengths) + 1
+    dout, _ = matrix(T, d, BF16, gen)
+    tokens = torch.repeat_interleave(torch.arange(len(lengths), dtype=torch.int32), torch.tensor(lengths))
+    tokens = tokens[torch.randperm(T, generator=torch.Generator().manual_seed(T))].to(DEV)
+    check_gradient(run_backward(dout, tokens, V, F32), dout, tokens, V, F32, 1.0)
+
+
 @pytest.mark.parametrize("kind", ["any", "mask", "one", "holes"])
 def test_gradient_added_to_what_is_there(kind):
     """What is added is the 32-bit sum: one more unit, of the result.  Rows that no token names keep every bit."""
