@@ -99,8 +99,9 @@ int mosaic_dropout_backward(const void *dout, int32_t stream_type, int64_t ld_do
  *   targets    dev int32[max_rows], of the listed rows in their order; needed for out_logprob alone
  *   out_*      dev float[max_rows], each may be NULL, not all of them with n_top = 0; entries from M on are left as they were
  *   n_top      0 .. MOSAIC_MAX_TOP;  top_id int32 and top_logprob float [max_rows, n_top], dense, NULL where it is 0
- *   workspace  dev, 16-byte aligned, mosaic_masked_logprobs_workspace_bytes bytes: sums of the vocabulary's parts, with
- *              alternatives their candidates (38 to 151 MB), and, where the hidden states pass 2 GiB, the listed rows side by side
+ *   workspace  dev, 16-byte aligned, mosaic_masked_logprobs_workspace_bytes bytes (one for more rows serves fewer): sums of the
+ *              vocabulary's parts, with alternatives lists of their candidates (67 MB) and the parts' best, and, where the
+ *              hidden states pass 2 GiB, the listed rows side by side
  * A NaN among a row's logits makes that row's log probabilities, entropy and log-sum-exp NaN and its alternatives unspecified
  * (ids in [-1, V)); other rows are not affected.
  * How the vocabulary is parted follows from the rows found: a row's last bits may depend on their number.

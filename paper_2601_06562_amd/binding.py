@@ -666,12 +666,12 @@ def mosaic_dropout_backward(dout, dx, p, seed, site=0, first_row=0, stream=None)
 def _list_args(hidden, w, idx, count, max_rows):
     """(hidden pointer, ld_h, T, d, w pointer, ld_w, V, idx pointer, count pointer) of a pass over listed rows."""
     (T, d), V = hidden.shape, w.shape[0]
-    p_h, ld_h = _rows(hidden, "hidden", T, d, torch.bfloat16)
-    p_w, ld_w = _rows(w, "w", V, d, torch.bfloat16)
     if (idx is None) != (count is None):
         raise ValueError("idx and count go together")
     if idx is not None and idx.numel() < max_rows:
         raise ValueError("idx holds fewer than max_rows entries")
+    p_h, ld_h = _rows(hidden, "hidden", T, d, torch.bfloat16)
+    p_w, ld_w = _rows(w, "w", V, d, torch.bfloat16)
     return p_h, ld_h, T, d, p_w, ld_w, V, _dev_ptr(idx, "idx", torch.int32), _count_ptr(count)
 
 

@@ -686,7 +686,15 @@ int launch_sort_tokens(const int32_t* tokens, int64_t n, const int32_t* count, i
   return 0;
 }
 
-int64_t token_sum_partials(int64_t n) { return 2 * ((n + each_of(n) - 1) / each_of(n)); }
+// Room for up to n positions: fewer of them can have more pieces where each_of() steps up.
+int64_t token_sum_partials(int64_t n) {
+  int64_t most = (n + each_of(n) - 1) / each_of(n);
+  for (const int64_t step : {2048, 8192, 32768}) {
+    const int64_t below = (step + each_of(step - 1) - 2) / each_of(step - 1);
+    if (n >= step && most < below) most = below;
+  }
+  return 2 * most;
+}
 
 int launch_token_sums(const TokenSumArgs& a, bool rows_f32, bool sums_f32, hipStream_t stream) {
   SumParams p = {};

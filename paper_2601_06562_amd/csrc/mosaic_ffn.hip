@@ -729,6 +729,10 @@ int launch_gated_ffn_forward(const FfnForwardArgs& f, hipStream_t stream) {
   return 0;
 }
 
+int64_t most_part_rows(int64_t rows) {
+  const int64_t parts = rows * kMostParts < kPartRows ? rows * kMostParts : kPartRows;
+  return parts > rows ? parts : rows;
+}
 ProductPlan plan_row_product(int64_t rows, int32_t cols, int64_t depth) {
   const int64_t steps = tiles(depth, kStepK);
   ProductPlan best = {1, 0.0};

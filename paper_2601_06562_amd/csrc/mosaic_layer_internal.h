@@ -91,6 +91,7 @@ struct ProductArgs {
 };
 struct ProductPlan { int32_t splits; double us; };
 ProductPlan plan_row_product(int64_t rows, int32_t cols, int64_t depth);
+int64_t most_part_rows(int64_t rows);   // parts x rows of any plan for up to so many rows
 int launch_row_product(const ProductArgs& a, hipStream_t stream);
 int launch_column_product(const ProductArgs& a, hipStream_t stream);
 

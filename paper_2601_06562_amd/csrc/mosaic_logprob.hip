@@ -553,9 +553,11 @@ Space space_of(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, 
   Space s;
   const int64_t tile = max_rows <= 64 ? 64 : max_rows <= 128 ? 128 : 256;
   int64_t lists;
-  if (w4_takes(d, V)) {   // as many parts as fill the chip at the bound; fewer rows have room for more
-    const int64_t row_tiles = (max_rows + 255) / 256;
-    s.slots = row_tiles * 256 * choose_vocab_splits(row_tiles, ((int64_t)V + kVocab - 1) / kVocab, kCus);
+  if (w4_takes(d, V)) {   // room for two rounds of units, and for four parts and a round more of many rows: grows with the bound
+    const int64_t row_tiles = (max_rows + 255) / 256, vocab_tiles = ((int64_t)V + kVocab - 1) / kVocab;
+    const int64_t most = vocab_tiles < MOSAIC_MAX_VOCAB_SPLITS ? vocab_tiles : MOSAIC_MAX_VOCAB_SPLITS;
+    const int64_t wide = 4 * row_tiles + kCus, units = wide > 2 * kCus ? wide : 2 * kCus;
+    s.slots = 256 * (units < row_tiles * most ? units : row_tiles * most);
     s.entries = 2 * s.slots;
     lists = w4_list_bytes();
   } else {
@@ -659,8 +661,9 @@ GradientSpace gradient_space(int64_t max_rows, int32_t d, int32_t V) {
   s.extra = s.sums + padded(4 * token_sum_partials(max_rows) * d);
   s.slot = s.extra + padded(4 * max_rows * d);
   s.parts = s.slot + slot_rows(V) * kSlotBytes;
-  s.dl = s.parts + padded(4 * s.splits * s.dl_rows * d);
-  s.least = s.dl + 2 * s.dl_rows * kVocab;
+  const int64_t most = max_rows <= kLowRows || max_rows > 2 * kLowRows ? s.dl_rows : 2 * kLowRows;   // so that fewer rows need no more
+  s.dl = s.parts + padded(4 * most_part_rows(most) * d);
+  s.least = s.dl + 2 * most * kVocab;
   return s;
 }
 // Ids at a time with so many bytes for dl, evenly, in whole tiles.
