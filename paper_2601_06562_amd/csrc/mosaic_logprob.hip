@@ -25,6 +25,10 @@ __host__ __device__ inline int tile_rows(int64_t rows) {
   return 92 * ((rows + 127) / 128) < 150 * ((rows + 255) / 256) ? 128 : 256;
 }
 
+// With alternatives a tile has 128 rows at most: beside the accumulators of 256 their state does not fit into registers (32003 x 1032,
+// five alternatives: 900 rows 382 us, of 128 rows 233; 3000 rows 1102 and 671).
+constexpr int kListedTile = 128;
+
 // Into how many parts the vocabulary's tiles go: the least time of the longest block, a unit costing about two tiles' steps of
 // 64 k more than its tiles.  One lane tries every 64th count.
 __device__ __forceinline__ int choose_parts(int row_tiles, int vocab_tiles, int steps) {
@@ -218,9 +222,13 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
   bool done_last = false, fresh = true;                                             // the last of its unit; fresh: a unit is to be begun
   auto load = [&](int j, float (&x)[32]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int c = 0; c < QB; ++c) {
+      if (c != j) continue;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[4 * i + r] = acc[i][j][r];
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[4 * i + r] = acc[i][c][r];
+    }
   };
   for (;;) {
     const bool more = unit < end;
@@ -262,7 +270,8 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
           return p.part_top + (of_half + (in ? row : 0)) * p.n_top;
         };
         ++done_tiles;
-        reduce_tile<QB, false, MODE == kAlternatives>(load, st, v + 4 * g, 0, p.V, target, q0, lists, done_tiles == 1, sort_now(done_tiles, unit_tiles), place);
+        // (with alternatives column by column in a loop: unrolled, 2129 registers are spilled and 900 rows take 1902 us)
+        reduce_tile<QB, MODE == kAlternatives, MODE == kAlternatives>(load, st, v + 4 * g, 0, p.V, target, q0, lists, done_tiles == 1, sort_now(done_tiles, unit_tiles), place);
         if (done_last) {
 #pragma unroll
           for (int k = 0; k < Rows<QB>::kOwn; ++k) {
@@ -358,8 +367,10 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(const LogitParams p) 
   const int rows = rows_found(p);
   if (rows <= 0) return;
   const int tile = tile_rows(rows);
-  if (tile == 256) run_units<MODE, 256, 3, 2>(p, smem, rows, rows);
-  else if (tile == 128) run_units<MODE, 128, 3, 3>(p, smem, rows, rows);
+  if constexpr (MODE != kAlternatives) {
+    if (tile == 256) return run_units<MODE, 256, 3, 2>(p, smem, rows, rows);
+  }
+  if (tile >= kListedTile) run_units<MODE, kListedTile, 3, 3>(p, smem, rows, rows);
   else run_units<MODE, 64, 4, 4>(p, smem, rows, rows);
 }
 template <int TQ, int SP, int SQ>
@@ -565,7 +576,7 @@ Space space_of(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32_t V, 
     const int64_t most = (int64_t)kMostSplits * max_rows < kMostUnits * tile ? (int64_t)kMostSplits * max_rows : kMostUnits * tile;
     s.slots = most > max_rows ? most : max_rows;
     s.entries = 2 * s.slots;
-    lists = (int64_t)kCus * 8 * tile * kListRoom * (int64_t)sizeof(Entry);
+    lists = (int64_t)kCus * 8 * (tile < kListedTile ? tile : kListedTile) * kListRoom * (int64_t)sizeof(Entry);
   }
   s.found = 0;
   s.lists = 256;
