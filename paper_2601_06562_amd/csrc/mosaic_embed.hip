@@ -426,19 +426,23 @@ __device__ __forceinline__ void put_joined(const TokenSumArgs& a, int64_t row, i
         bf16x4_t{(__bf16)t[0], (__bf16)t[1], (__bf16)t[2], (__bf16)t[3]};
   }
 }
-// Partial sums m0 .. m1 - 1 of the token that goes on behind piece `from`, added in order, eight under way at once.
+// Partial sums m0 .. m1 - 1 of the token that goes on behind piece `from`, added in order, eight under way at once: past the last
+// one it is read again and counts nothing, since loads behind a branch each would be waited for one by one.
 __device__ __forceinline__ f32x4_t add_partials(const TokenSumArgs& a, int64_t from, int64_t m0, int64_t m1, int c, bool in) {
   f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+  const float* base = a.partials + (in ? c : 0);
+#pragma unroll 1
   for (int64_t m = m0; m < m1; m += 8) {
     f32x4_t v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      v[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      const int64_t slot = m + i == 0 ? 2 * from + 1 : 2 * (from + m + i);
-      if (in && m + i < m1) v[i] = *reinterpret_cast<const f32x4_t*>(a.partials + slot * a.d + c);
+      const int64_t k = m + i < m1 ? m + i : m1 - 1;
+      v[i] = *reinterpret_cast<const f32x4_t*>(base + (k == 0 ? 2 * from + 1 : 2 * (from + k)) * a.d);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += v[i];
+    for (int i = 0; i < 8; ++i) {
+      if (m + i < m1) s += v[i];
+    }
   }
   return s;
 }
@@ -446,7 +450,7 @@ __device__ __forceinline__ f32x4_t add_partials(const TokenSumArgs& a, int64_t f
 template <typename O>
 __global__ __launch_bounds__(64 * kJoinWaves) void token_join_kernel(const SumParams p) {
   const TokenSumArgs& a = p.a;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int c = ((int)blockIdx.x * 64 + lane) * 4;
   const bool in = c < a.d;
   __shared__ f32x4_t parts[kJoinWaves][64];
