@@ -379,7 +379,8 @@ __global__ __launch_bounds__(kThreads) void logit_gradient_kernel(const LogitPar
   run_units<kGradients, TQ, SP, SQ>(p, smem, p.max_rows, rows_found(p));
 }
 
-// Joins a row's parts, a wave a row: a lane takes every 64th half.
+// Joins a row's parts, a wave a row: a lane takes every 64th half.  Bound by the time to memory, which another kernel wrote: the
+// loads of a row go out together.
 constexpr int kJoinWaves = 4;
 struct JoinParams {
   LogitParams l;
@@ -393,41 +394,47 @@ __device__ __forceinline__ T over_wave(T v, F f) {
   for (int x = 32; x >= 1; x >>= 1) v = f(v, __shfl_xor(v, x, 64));
   return v;
 }
-__global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(const JoinParams p) {
-  constexpr int kHeld = 2 * kMostSplits / 64;   // halves of a lane, at most
+// HELD: halves of a lane, at most.  Every lane loads as much, what lies past the halves counting nothing: loads behind a branch each
+// would be waited for one by one.
+template <int HELD>
+__device__ __forceinline__ void join_rows(const JoinParams& p, int rows, int halves, int stride) {
   const LogitParams& l = p.l;
-  const int rows = rows_found(l), lane = threadIdx.x & 63;
-  if (rows <= 0) return;
-  const int stride = l.found[1];
-  // (whatever another call on the same workspace left there, nobody is to be led beyond the arrays)
-  const int halves = stride >= rows && l.found[0] > 0 && l.found[0] <= 2 * kMostSplits && (int64_t)l.found[0] * stride <= p.entries ? l.found[0] : 0;
-  const int held = (halves + 63) / 64;
-  for (int64_t row = (int64_t)blockIdx.x * kJoinWaves + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * kJoinWaves) {
-    float pe[kHeld], ps[kHeld], pt[kHeld];
-    Candidate head[kHeld];
-    int taken[kHeld];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  for (int64_t row = (int64_t)blockIdx.x * kJoinWaves + wave; row < rows; row += (int64_t)gridDim.x * kJoinWaves) {
+    float pe[HELD], ps[HELD], pt[HELD];
+    Candidate head[HELD], second[HELD];
+    int taken[HELD];
     float e = kNegExponent;
+    const int target = p.out_logprob != nullptr ? l.targets[row] : -1;
+    const float target_logit = p.out_logprob != nullptr ? l.target_logit[row] : 0.f;   // (holds nothing where there is no target)
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-      const int h = lane + 64 * i;
-      pe[i] = kNegExponent;
-      ps[i] = pt[i] = 0.f;
-      head[i] = 0.0;
-      taken[i] = 0;
-      if (i < held && h < halves) {
-        const int64_t at = (int64_t)h * stride + row;
-        pe[i] = l.part_e[at];
-        ps[i] = l.part_s[at];
-        pt[i] = l.part_t[at];
-        if (l.n_top > 0) head[i] = l.part_top[at * l.n_top];
+    for (int i = 0; i < HELD; ++i) {
+      const int64_t at = (int64_t)(lane + 64 * i < halves ? lane + 64 * i : 0) * stride + row;
+      pe[i] = l.part_e[at];
+      ps[i] = l.part_s[at];
+      pt[i] = l.part_t[at];
+    }
+    if (l.n_top > 0) {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i) {
+        const Candidate* const best = l.part_top + ((int64_t)(lane + 64 * i < halves ? lane + 64 * i : 0) * stride + row) * l.n_top;
+        head[i] = best[0];
+        second[i] = best[l.n_top > 1 ? 1 : 0];
       }
     }
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) e = fmaxf(e, pe[i]);
+    for (int i = 0; i < HELD; ++i) {
+      const bool there = lane + 64 * i < halves;
+      pe[i] = there ? pe[i] : kNegExponent;
+      ps[i] = there ? ps[i] : 0.f;
+      pt[i] = there ? pt[i] : 0.f;
+      taken[i] = 0;
+      e = fmaxf(e, pe[i]);
+    }
     e = over_wave(e, [](float a, float b) { return fmaxf(a, b); });
     double s = 0.0, t = 0.0;
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
+    for (int i = 0; i < HELD; ++i) {
       const float by = pe[i] - e, scale = __builtin_amdgcn_exp2f(by);
       s += (double)(scale * ps[i]);
       t += (double)scale * ((double)pt[i] + (double)ps[i] * by);
@@ -442,23 +449,30 @@ __global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(const Joi
       const float entropy = (float)((log_s - t / s) / (double)kLog2e);
       if (p.out_entropy != nullptr) p.out_entropy[row] = entropy < 0.f ? 0.f : entropy;
       if (p.out_logprob != nullptr) {
-        const int target = l.targets[row];
-        const float logp = (uint32_t)target < (uint32_t)l.V ? (float)((double)l.target_logit[row] - lse) : 0.f;
+        const float logp = (uint32_t)target < (uint32_t)l.V ? (float)((double)target_logit - lse) : 0.f;
         p.out_logprob[row] = logp > 0.f ? 0.f : logp;
       }
     }
-    // The best n_top of the halves' best: a lane holds the first candidates of its halves and, each time the best of all is its own,
-    // looks at the next of that half.
+    if (l.n_top == 0) continue;
+    // The best n_top of the halves' best: a lane holds the first two candidates left of its halves and, each time the best of all is
+    // its own, fetches another of that half.
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const bool there = lane + 64 * i < halves;
+      head[i] = there ? head[i] : 0.0;
+      second[i] = there && l.n_top > 1 ? second[i] : 0.0;
+    }
     for (int k = 0; k < l.n_top; ++k) {
       Candidate best = 0.0;
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i) best = first_of_two(head[i], best);
+      for (int i = 0; i < HELD; ++i) best = first_of_two(head[i], best);
       best = over_wave(best, [](double a, double b) { return first_of_two(a, b); });
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i) {
+      for (int i = 0; i < HELD; ++i) {
         if (best != 0.0 && head[i] == best) {   // (ids differ, so it is one lane's)
           ++taken[i];
-          head[i] = taken[i] < l.n_top ? l.part_top[((int64_t)(lane + 64 * i) * stride + row) * l.n_top + taken[i]] : 0.0;
+          head[i] = second[i];
+          second[i] = taken[i] + 1 < l.n_top ? l.part_top[((int64_t)(lane + 64 * i) * stride + row) * l.n_top + taken[i] + 1] : 0.0;
         }
       }
       if (lane == 0) {
@@ -468,6 +482,16 @@ __global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(const Joi
       }
     }
   }
+}
+__global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(const JoinParams p) {
+  const LogitParams& l = p.l;
+  const int parts = l.found[0], stride = l.found[1], rows = rows_found(l);
+  if (rows <= 0) return;
+  // (whatever another call on the same workspace left there, nobody is to be led beyond the arrays)
+  const int halves = stride >= rows && parts > 0 && parts <= 2 * kMostSplits && (int64_t)parts * stride <= p.entries ? parts : 0;
+  if (halves <= 64) join_rows<1>(p, rows, halves, stride);
+  else if (halves <= 128) join_rows<2>(p, rows, halves, stride);
+  else join_rows<2 * kMostSplits / 64>(p, rows, halves, stride);
 }
 
 // Rows gathered side by side, zeros from the last listed one on.
