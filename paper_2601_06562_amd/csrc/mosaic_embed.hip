@@ -68,7 +68,8 @@ __device__ __forceinline__ void store_columns(__bf16* row, int c, int d, const f
   else *reinterpret_cast<bf16x8_t*>(row + c) = t;
 }
 
-// ---- lookup: out[t] = scale * table[tokens[t]], a block ROWS rows of a stripe of columns, all loads under way at once.
+// ---- lookup: out[t] = scale * table[tokens[t]], a block ROWS rows of a stripe of columns, all loads under way at once.  37 rows of
+// 3584 take 6 us, of which the kernel is 2.5.
 template <typename S, typename O, int ROWS, bool PAST>
 __global__ __launch_bounds__(kThreads) void embedding_kernel(const EmbedArgs p) {
   const int64_t n = rows_of(p.T, p.count);
@@ -105,8 +106,10 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMostDigitBits = 10, kMostBins = 1 << kMostDigitBits;
 constexpr int kMostSortBlocks = 64;
 constexpr int kFillRows = 32;              // rows that a block fills
-constexpr int64_t kSortPiece = 2048;       // keys of a block, at least
-constexpr int64_t kOneBlockKeys = 8192;    // up to here one block sorts, in one launch
+constexpr int64_t kSortPiece = 1024;       // keys of a block, at least (gradient of 12000 rows of 512: 51 us, with 4096 keys 61)
+// Up to here one block sorts, in one launch (gradient of 3000 rows of 512: 31 us, in launches of several blocks 36; 6000: 42 and 40;
+// 8000: 48 and 41).
+constexpr int64_t kOneBlockKeys = 6144;
 
 struct SortArgs {
   const int32_t* tokens;   // first pass: what keys and positions are made from
@@ -318,10 +321,18 @@ SortPlan plan_sort(int64_t n, int32_t V) {
 }
 int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// ---- sums of rows by token.  A block takes kEach(n) sorted positions and a stripe of columns: 8 rows under way at once, added in
+// ---- sums of rows by token.  A block takes each_of(n, d) sorted positions and a stripe of columns: 8 rows under way at once, added in
 // order; a token's sum goes out where the token ends.  A token whose positions reach over the end of a block's piece leaves a
 // partial sum there (0: it began ahead of the piece, 1: it goes on behind it), joined in order by a second kernel.
-__host__ __device__ inline int each_of(int64_t n) { return n >= 32768 ? 64 : n >= 8192 ? 32 : n >= 2048 ? 16 : 8; }
+//
+// Few positions a block keep more blocks busy and a lone row's chain short, many leave fewer partial sums to join: the choice goes by
+// what there is for all blocks.  Half of the tokens the same, us with 8, 16, 32 and 64: 3000 rows of 512 28, 31, 41 and 60; 12000 48,
+// 45, 55 and 72; 32768 of 1024 84, 75, 72 and 96; 131072 of 512 244, 192, 165 and 158; 32768 of 4096 with 32 and 64 275 and 269.
+int64_t stripes_of(int32_t d) { return (d + kStripe - 1) / kStripe; }
+int each_of(int64_t n, int32_t d) {
+  const int64_t m = n * stripes_of(d);
+  return m >= 65536 ? 64 : m >= 32768 ? 32 : m >= 8192 ? 16 : 8;
+}
 constexpr int kMostEach = 64;
 
 struct SumParams {
@@ -412,7 +423,8 @@ __global__ __launch_bounds__(kThreads) void token_sum_kernel(const SumParams p) 
 // Joins the partial sums of tokens that reach over pieces: a block looks through pieces (64 at once) for those at whose end a
 // token goes on that began in them.  A wave joins a token of few partial sums by itself, the block's waves taking such tokens in
 // turn; of one with more than kAlone the waves take a sixteenth each, in order, and the sixteenths are added in order.  A lane has
-// four columns.
+// four columns.  Bound by the time to memory, which other kernels wrote: the keys of 64 pieces are asked for at once, and a token's
+// partial sums eight at a time (1003 rows of 1024: 8 us; with a branch around each load, and registers spilled for it, 35).
 constexpr int kJoinWaves = 16, kAlone = 16;
 
 template <typename O>
@@ -537,35 +549,29 @@ __device__ __forceinline__ void philox(uint32_t (&c)[4], uint32_t k0, uint32_t k
   }
 }
 
-template <typename S, typename O, bool ADD, int ROWS, bool PAST>
+// A block takes a row of a stripe of columns (32768 x 4096 with a 32-bit residual 250 us, 5.4 TB/s, as the largest copies reach;
+// two and four rows, loaded at once, 251 and 258, in 16 bits 80 and 83 us where one takes 74).  Ten rounds of the generator for eight
+// columns hide behind the memory.
+template <typename S, typename O, bool ADD, bool PAST>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(const DropoutArgs p) {
   const int c = (int)blockIdx.y * kStripe + (int)threadIdx.x * 8;   // eight columns share the generator's words
   if (c >= p.d) return;
-  for (int64_t t0 = (int64_t)blockIdx.x * ROWS; t0 < p.T; t0 += (int64_t)gridDim.x * ROWS) {
-    float v[ROWS][8], add[ADD ? ROWS : 1][8];
+  for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
+    float v[8], add[8];
+    load8(static_cast<const S*>(p.x) + t * p.ld_x + c, v);
+    if constexpr (ADD) load8(static_cast<const O*>(p.residual) + t * p.ld_residual + c, add);
+    const uint64_t row = (uint64_t)(p.first_row + t);
+    uint32_t w[4] = {(uint32_t)c >> 3, (uint32_t)row, (uint32_t)(row >> 32), p.site};
+    philox(w, p.key_low, p.key_high);
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      if (t0 + r < p.T) {
-        load8(static_cast<const S*>(p.x) + (t0 + r) * p.ld_x + c, v[r]);
-        if constexpr (ADD) load8(static_cast<const O*>(p.residual) + (t0 + r) * p.ld_residual + c, add[r]);
-      }
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t bits = i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu;
+      v[i] = bits >= p.border ? v[i] * p.grow : 0.f;
+      if constexpr (ADD) v[i] += add[i];
     }
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      if (t0 + r >= p.T) break;
-      const uint64_t row = (uint64_t)(p.first_row + t0 + r);
-      uint32_t w[4] = {(uint32_t)c >> 3, (uint32_t)row, (uint32_t)(row >> 32), p.site};
-      philox(w, p.key_low, p.key_high);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t bits = i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu;
-        v[r][i] = bits >= p.border ? v[r][i] * p.grow : 0.f;
-        if constexpr (ADD) v[r][i] += add[r][i];
-      }
-      O* const out = static_cast<O*>(p.out) + (t0 + r) * p.ld_out;
-      if constexpr (PAST && sizeof(O) == 2) store_columns<true>(out, c, p.d, v[r]);
-      else store8(out + c, v[r]);
-    }
+    O* const out = static_cast<O*>(p.out) + t * p.ld_out;
+    if constexpr (PAST && sizeof(O) == 2) store_columns<true>(out, c, p.d, v);
+    else store8(out + c, v);
   }
 }
 
@@ -574,25 +580,24 @@ dim3 row_grid(int64_t T, int rows, int d) {
   const int64_t blocks = (T + rows - 1) / rows;
   return dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks), (unsigned)((d + kStripe - 1) / kStripe));
 }
-// Rows of a block: several once there are blocks enough.
-bool many_rows(int64_t T, int32_t d) { return T * ((d + kStripe - 1) / kStripe) >= 8192; }
-constexpr int kManyRows = 4;
-constexpr int64_t kPastBytes = (int64_t)256 << 20;   // an output as large as the memory-side cache
+// An output from half of the memory-side cache on is written past the caches, which keeps the rows that are read in them (into 32 bits
+// 32768 x 4096: 146 -> 115 us, 16000 x 4096, 262 MB: 75 -> 57; 16000 x 1024, 66 MB: 16.4 either way, and what comes next finds
+// it there).
+constexpr int64_t kPastBytes = (int64_t)128 << 20;
+constexpr int kPastRows = 2;   // rows of a block then: one 155 us, two 114, four 115; below, one takes what two and four do
 
 template <typename S, typename O>
 int launch_embedding(const EmbedArgs& a, hipStream_t stream) {
   if (a.T * a.d * (int64_t)sizeof(O) >= kPastBytes)
-    return launch_kernel(embedding_kernel<S, O, kManyRows, true>, row_grid(a.T, kManyRows, a.d), dim3(kThreads), stream, a);
-  if (many_rows(a.T, a.d)) return launch_kernel(embedding_kernel<S, O, kManyRows, false>, row_grid(a.T, kManyRows, a.d), dim3(kThreads), stream, a);
+    return launch_kernel(embedding_kernel<S, O, kPastRows, true>, row_grid(a.T, kPastRows, a.d), dim3(kThreads), stream, a);
   return launch_kernel(embedding_kernel<S, O, 1, false>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
 }
 
 template <typename S, typename O, bool ADD>
 int launch_dropout_as(const DropoutArgs& a, hipStream_t stream) {
   if (a.T * a.d * (int64_t)sizeof(O) >= kPastBytes)
-    return launch_kernel(dropout_kernel<S, O, ADD, kManyRows, true>, row_grid(a.T, kManyRows, a.d), dim3(kThreads), stream, a);
-  if (many_rows(a.T, a.d)) return launch_kernel(dropout_kernel<S, O, ADD, kManyRows, false>, row_grid(a.T, kManyRows, a.d), dim3(kThreads), stream, a);
-  return launch_kernel(dropout_kernel<S, O, ADD, 1, false>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
+    return launch_kernel(dropout_kernel<S, O, ADD, true>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
+  return launch_kernel(dropout_kernel<S, O, ADD, false>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
 }
 
 template <typename S, typename O>
@@ -691,11 +696,11 @@ int launch_sort_tokens(const int32_t* tokens, int64_t n, const int32_t* count, i
 }
 
 // Room for up to n positions: fewer of them can have more pieces where each_of() steps up.
-int64_t token_sum_partials(int64_t n) {
-  int64_t most = (n + each_of(n) - 1) / each_of(n);
-  for (const int64_t step : {2048, 8192, 32768}) {
-    const int64_t below = (step + each_of(step - 1) - 2) / each_of(step - 1);
-    if (n >= step && most < below) most = below;
+int64_t token_sum_partials(int64_t n, int32_t d) {
+  int64_t most = (n + each_of(n, d) - 1) / each_of(n, d);
+  for (const int64_t step : {8192, 32768, 65536}) {
+    const int64_t first = (step + stripes_of(d) - 1) / stripes_of(d), below = (first + each_of(first - 1, d) - 2) / each_of(first - 1, d);
+    if (n >= first && most < below) most = below;
   }
   return 2 * most;
 }
@@ -703,8 +708,8 @@ int64_t token_sum_partials(int64_t n) {
 int launch_token_sums(const TokenSumArgs& a, bool rows_f32, bool sums_f32, hipStream_t stream) {
   SumParams p = {};
   p.a = a;
-  p.each = each_of(a.n);
-  p.stripes = (a.d + kStripe - 1) / kStripe;
+  p.each = each_of(a.n, a.d);
+  p.stripes = (int32_t)stripes_of(a.d);
   p.pieces = (a.n + p.each - 1) / p.each;
   p.blocks = p.pieces * p.stripes;
   if (rows_f32) return sums_f32 ? launch_sums<float, float>(p, stream) : launch_sums<float, __bf16>(p, stream);

@@ -693,7 +693,7 @@ GradientSpace gradient_space(int64_t max_rows, int32_t d, int32_t V) {
   s.coef = s.rows + padded(2 * max_rows * d);
   s.sort = s.coef + padded(4 * max_rows);
   s.sums = s.sort + padded(sort_tokens_bytes(max_rows));
-  s.extra = s.sums + padded(4 * token_sum_partials(max_rows) * d);
+  s.extra = s.sums + padded(4 * token_sum_partials(max_rows, d) * d);
   s.slot = s.extra + padded(4 * max_rows * d);
   s.parts = s.slot + slot_rows(V) * kSlotBytes;
   const int64_t most = max_rows <= kLowRows || max_rows > 2 * kLowRows ? s.dl_rows : 2 * kLowRows;   // so that fewer rows need no more

@@ -28,7 +28,7 @@ struct EmbeddingSpace {
 EmbeddingSpace embedding_space(int64_t T, int32_t d) {
   EmbeddingSpace s;
   s.partials = mosaic::sort_tokens_bytes(T);
-  s.total = s.partials + 4 * mosaic::token_sum_partials(T) * d;
+  s.total = s.partials + 4 * mosaic::token_sum_partials(T, d) * d;
   return s;
 }
 

@@ -49,7 +49,7 @@ struct TokenSumArgs {
   int32_t V, d, accumulate;
   float scale;
 };
-int64_t token_sum_partials(int64_t n);
+int64_t token_sum_partials(int64_t n, int32_t d);
 int launch_token_sums(const TokenSumArgs& a, bool rows_f32, bool sums_f32, hipStream_t stream);
 
 // ---- dropout (mosaic_embed.hip)
