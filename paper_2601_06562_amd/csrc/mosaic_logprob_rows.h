@@ -4,7 +4,7 @@
 // In both kernels a wave holds 128 ids of a tile by 16 QB rows, in blocks of 16 x 16: lane l has ids 16 i + 4 (l / 16) + r, i < 8,
 // r < 4, of rows 16 j + l % 16, j < QB ("columns").  A row of a wave lies in four lanes, 16 apart; what is kept of it between tiles
 // one of them holds, its owner: of column j lane group j % 4.  `load(j, x)` gives a column's 32 elements, x[4 i + r].  ROLLED:
-// columns are taken in a loop, so that the code is there once; where the compiler holds the accumulators it needs them unrolled.
+// columns are taken in a loop, so that the code is there once; where the compiler holds the accumulators, unrolled costs less.
 #ifndef MOSAIC_LOGPROB_ROWS_H_
 #define MOSAIC_LOGPROB_ROWS_H_
 
