@@ -5,7 +5,7 @@
 // vocabulary ids ("P", the weights' rows) by 64, 128 or 256 listed rows ("Q", gathered as they are copied), K in
 // steps of 64 through rings of slots in LDS.  A unit is a tile of rows and a part of the vocabulary, whose tiles a block takes one
 // after another; the state of a row is held between them.  32003 x 1032: 900 rows 81 us, 3000 rows 218 (0.91 PFLOP/s), where the
-// hand-scheduled loop takes 71 and 176 for 32000 x 1024; five alternatives 233 and 671, there 130 and 305.
+// hand-scheduled loop takes 71 and 176 for 32000 x 1024; five alternatives 233 and 671, there 122 and 292.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>

@@ -238,6 +238,7 @@ template <int QB, class Place>
 __device__ __forceinline__ void sort_all_in(Rows<QB>& st, const Entry* lists, int n, Place place) {
   const int g = (threadIdx.x & 63) >> 4;
   __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // the lists' entries were stored by other lanes
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll 1
   for (int k = 0; k < Rows<QB>::kOwn; ++k) {
     bool in = 4 * k + g < QB;
@@ -365,6 +366,21 @@ __device__ __forceinline__ float reached_by(const float (&q)[8], int n) {
   return bound;
 }
 
+// A lane's list of a column, as a buffer that nothing goes beyond.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t list_buffer(Entry* list) {
+  return __builtin_amdgcn_make_buffer_rsrc(list, 0, kListRoom * 64 * (int)sizeof(Entry), 0x00020000);
+}
+// Puts x and its id at `to` of a lane's list and moves on, where x is above `pass`; elsewhere it goes past the buffer, which drops it: a
+// branch around each store, which some lane nearly always takes, is two jumps (900 rows of 32000 x 1024, five alternatives: 128 us, so
+// 122; a column's stores are a microsecond of the 2.5 that it takes then).
+__device__ __forceinline__ void append_above(float x, float pass, int32_t id, __amdgpu_buffer_rsrc_t list, uint32_t& to) {
+  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+  static_assert(sizeof(Entry) == 8, "an entry is two words");
+  const bool in = x > pass;
+  __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{__float_as_uint(x), (uint32_t)id}, list, (int)(in ? to : kOutside), 0, 0);
+  to = in ? to + 64 * (uint32_t)sizeof(Entry) : to;
+}
+
 // Works a finished tile into the rows' states.  v0: the id of this lane's first element; ids below `from` and from `end` on are
 // not counted; target: of the own rows, less than 0: none.  begins: the first tile of its unit.  now: whether the candidates so far
 // are sorted in at the end.  place(k, in): where the candidates of own row k go.
@@ -451,7 +467,7 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
         // on there once all have been sorted in.
         int done = (int)(pick(next, k) >> at & 255), n = (int)(pick(st.listed, k) >> at & 255);
         bool stopped = false;
-        char* const list = reinterpret_cast<char*>(lists) + j * (kListRoom * 64 * (int)sizeof(Entry));
+        const __amdgpu_buffer_rsrc_t list = list_buffer(lists + j * (kListRoom * 64));
         uint32_t to = (uint32_t)(n * 64 + lane) * (uint32_t)sizeof(Entry);
         constexpr uint32_t kFull = (kListRoom - 4) * 64 * (uint32_t)sizeof(Entry);
         const int id0 = (int)v0;
@@ -462,15 +478,9 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
             const bool fits = to < kFull + 64 * (uint32_t)sizeof(Entry);
             stopped = stopped | (want & !fits);
             done = (want & !fits) ? i : done;
-            if (want & fits) {
+            const float above = want & fits ? pass : __builtin_inff();
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                if (x[4 * i + r] > pass) {
-                  *reinterpret_cast<Entry*>(list + to) = Entry{x[4 * i + r], id0 + 16 * i + r};
-                  to += 64 * (uint32_t)sizeof(Entry);
-                }
-              }
-            }
+            for (int r = 0; r < 4; ++r) append_above(x[4 * i + r], above, id0 + 16 * i + r, list, to);
           }
         }
         n = (int)(to / (64 * (uint32_t)sizeof(Entry)));
