@@ -103,7 +103,8 @@ int mosaic_dropout_backward(const void *dout, int32_t stream_type, int64_t ld_do
  *              vocabulary's parts, with alternatives lists of their candidates (67 MB) and the parts' best, and, where the
  *              hidden states pass 2 GiB, the listed rows side by side
  * A NaN among a row's logits makes that row's log probabilities, entropy and log-sum-exp NaN and its alternatives unspecified
- * (ids in [-1, V)), an infinite one (of infinite weights or states) at least its entropy NaN; other rows are not affected.
+ * (ids in [-1, V)), an infinite one (of infinite weights or states; 2^100 and more counts as one) at least its entropy; other rows
+ * are not affected.
  * How the vocabulary is parted follows from the rows found: a row's last bits may depend on their number.
  */
 #define MOSAIC_MAX_TOP 16
