@@ -5,7 +5,7 @@
 // vocabulary ids ("P", the weights' rows) by 64, 128 or 256 listed rows ("Q", gathered as they are copied), K in
 // steps of 64 through rings of slots in LDS.  A unit is a tile of rows and a part of the vocabulary, whose tiles a block takes one
 // after another; the state of a row is held between them.  32003 x 1032: 900 rows 81 us, 3000 rows 218 (0.91 PFLOP/s), where the
-// hand-scheduled loop takes 71 and 176 for 32000 x 1024; five alternatives 233 and 671, there 122 and 292.
+// hand-scheduled loop takes 71 and 176 for 32000 x 1024; five alternatives 191 and 548, there 120 and 288.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -28,7 +28,7 @@ __host__ __device__ inline int tile_rows(int64_t rows) {
 }
 
 // With alternatives a tile has 128 rows at most: beside the accumulators of 256 their state does not fit into registers (32003 x 1032,
-// five alternatives: 900 rows 382 us, of 128 rows 233; 3000 rows 1102 and 671).
+// five alternatives, a store for every id: 900 rows 382 us, of 128 rows 233; 3000 rows 1102 and 671).
 constexpr int kListedTile = 128;
 
 // Into how many parts the vocabulary's tiles go: the least time of the longest block, a unit costing about two tiles' steps of
@@ -273,7 +273,7 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
         };
         ++done_tiles;
         // (with alternatives column by column in a loop: unrolled, 2129 registers are spilled and 900 rows take 1902 us)
-        reduce_tile<QB, MODE == kAlternatives, MODE == kAlternatives>(load, st, v + 4 * g, 0, p.V, target, q0, lists, done_tiles == 1, sort_now(done_tiles, unit_tiles), place);
+        reduce_tile<QB, MODE == kAlternatives, MODE == kAlternatives, true>(load, st, v + 4 * g, 0, p.V, target, q0, lists, done_tiles == 1, sort_now(done_tiles, unit_tiles), place);
         if (done_last) {
 #pragma unroll
           for (int k = 0; k < Rows<QB>::kOwn; ++k) {

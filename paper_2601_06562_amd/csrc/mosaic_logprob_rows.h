@@ -384,7 +384,7 @@ __device__ __forceinline__ void append_above(float x, float pass, int32_t id, __
 // Works a finished tile into the rows' states.  v0: the id of this lane's first element; ids below `from` and from `end` on are
 // not counted; target: of the own rows, less than 0: none.  begins: the first tile of its unit.  now: whether the candidates so far
 // are sorted in at the end.  place(k, in): where the candidates of own row k go.
-template <int QB, bool ROLLED, bool TOP, class Load, class Place>
+template <int QB, bool ROLLED, bool TOP, bool EIGHT, class Load, class Place>
 __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0, int64_t from, int64_t end,
                                             const int (&target)[Rows<QB>::kOwn], int row0, Entry* lists, bool begins, bool now,
                                             Place place) {
@@ -433,11 +433,19 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
         const float lane_m = fmaxf(fmaxf(fmaxf(fmaxf(most[0], most[1]), most[2]), fmaxf(fmaxf(most[3], most[4]), most[5])), fmaxf(most[6], most[7]));
         const float e = __builtin_ceilf(fmaxf(row_max(lane_m), kNeg) * kLog2e);
         float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};
+        // an exponential at a time, with the next but one's argument and the last one's sums beside it: their unit takes four times as long
+        float u[32], z[32];
+        u[0] = __builtin_fmaf(x[0], kLog2e, -e);
+        u[1] = __builtin_fmaf(x[1], kLog2e, -e);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const float u = __builtin_fmaf(x[i], kLog2e, -e), z = __builtin_amdgcn_exp2f(u);
-          s[i & 3] += z;
-          t[i & 3] = __builtin_fmaf(u, z, t[i & 3]);
+        for (int i = 0; i <= 32; ++i) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (i < 32) z[i] = __builtin_amdgcn_exp2f(u[i]);
+          if (i + 2 < 32) u[i + 2] = __builtin_fmaf(x[i + 2], kLog2e, -e);
+          if (i > 0) {
+            s[(i - 1) & 3] += z[i - 1];
+            t[(i - 1) & 3] = __builtin_fmaf(u[i - 1], z[i - 1], t[(i - 1) & 3]);
+          }
         }
         put(tile_e, k, own, e);
         put(tile_s, k, own, row_sum((s[0] + s[1]) + (s[2] + s[3])));
@@ -478,9 +486,22 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
             const bool fits = to < kFull + 64 * (uint32_t)sizeof(Entry);
             stopped = stopped | (want & !fits);
             done = (want & !fits) ? i : done;
-            const float above = want & fits ? pass : __builtin_inff();
+            // Most lanes put down one of a quad or none.  With EIGHT waves a compute unit, whose stores take turns, all four of a quad are
+            // only gone through where some lane has a second one (900 rows of 32003 x 1032, five alternatives: 236 us, so 191); with
+            // four waves telling that takes longer (32000 x 1024: 125 us, so 129).
+            const float above = want & fits ? pass : __builtin_inff(), *const v = x + 4 * i;
+            bool each = true;
+            if constexpr (EIGHT) {
+              const float second = fmaxf(fminf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fminf(v[0], v[1]), fminf(v[2], v[3])));
+              each = __any(second > above);
+            }
+            if (each) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) append_above(x[4 * i + r], above, id0 + 16 * i + r, list, to);
+              for (int r = 0; r < 4; ++r) append_above(v[r], above, id0 + 16 * i + r, list, to);
+            } else {
+              const int r = v[0] == most[i] ? 0 : v[1] == most[i] ? 1 : v[2] == most[i] ? 2 : 3;
+              append_above(most[i], above, id0 + 16 * i + r, list, to);
+            }
           }
         }
         n = (int)(to / (64 * (uint32_t)sizeof(Entry)));

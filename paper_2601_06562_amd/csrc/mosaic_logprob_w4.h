@@ -6,7 +6,7 @@
 // Bound by the power of the matrix cores for many rows, by memory for few: 126464 x 4096, 4096 rows 2.70 to 2.81 ms (1.51 to 1.57
 // PFLOP/s; the mask-only pass, which keeps no entropy, 2.56 to 2.59 beside it), with eight alternatives 4 to 5% more, one row 167 us
 // (6.2 TB/s); gradients at the logits, 2048 rows by 63232 ids, 764 us (1.39 PFLOP/s).  Alternatives cost small tiles of work most (900
-// rows of 32000 x 1024: 71 us, with five 122): a unit's first tiles bring the most candidates, and code that runs once a unit is
+// rows of 32000 x 1024: 68 us, with five 120): a unit's first tiles bring the most candidates, and code that runs once a unit is
 // fetched anew.  They are sorted in after 1, 2, 4, 8, ... tiles (every other schedule tried 2 to 8% slower at 4096 rows).
 //
 // It takes d that is a multiple of 64 and whole tiles of 256 ids, or a last tile over the vocabulary's last 256 ids, of which
@@ -252,7 +252,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
         gradient_tile<NB, true>(load, of, v, first_row, found);
       } else {
         const int64_t from = vt0 + n == ragged_tile ? (int64_t)ragged_tile * kVocab : 0;
-        reduce_tile<NB, true, MODE == kAlternatives>(load, st, v + 4 * q, from, p.V, target, first_row, lists, n == 0, sort_now(n + 1, ntile), place);
+        reduce_tile<NB, true, MODE == kAlternatives, false>(load, st, v + 4 * q, from, p.V, target, first_row, lists, n == 0, sort_now(n + 1, ntile), place);
       }
     }
     if constexpr (MODE != kGradients) {
