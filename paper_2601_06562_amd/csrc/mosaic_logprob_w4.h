@@ -3,8 +3,8 @@
 // column of 16 rows at a time.  Row tiles of 32 NB rows and parts of the vocabulary are chosen on the device from the rows found
 // (mosaic_schedule.h), as there.
 //
-// Bound by the power of the matrix cores for many rows, by memory for few: 126464 x 4096, 4096 rows 2.70 to 2.81 ms (1.51 to 1.57
-// PFLOP/s; the mask-only pass, which keeps no entropy, 2.56 to 2.59 beside it), with eight alternatives 4 to 5% more, one row 167 us
+// Bound by the power of the matrix cores for many rows, by memory for few: 126464 x 4096, 4096 rows 2.61 to 2.81 ms (1.51 to 1.63
+// PFLOP/s; the mask-only pass, which keeps no entropy, 2.55 to 2.59 beside it), with eight alternatives 4 to 5% more, one row 167 us
 // (6.2 TB/s); gradients at the logits, 2048 rows by 63232 ids, 764 us (1.39 PFLOP/s).  Alternatives cost small tiles of work most (900
 // rows of 32000 x 1024: 68 us, with five 120): a unit's first tiles bring the most candidates, and code that runs once a unit is
 // fetched anew.  They are sorted in after 1, 2, 4, 8, ... tiles (every other schedule tried 2 to 8% slower at 4096 rows).
