@@ -745,7 +745,8 @@ int launch_dl(LogitParams p, int64_t v, int64_t n, hipStream_t stream) {
 int64_t logprob_backward_workspace_bytes(int64_t max_rows, int32_t d, int32_t V, int64_t budget_bytes) {
   const GradientSpace at = gradient_space(max_rows, d, V);
   const int64_t room = budget_bytes > 0 ? budget_bytes - at.dl : kDlBytes;
-  return at.dl + 2 * at.dl_rows * ids_at_once(at.dl_rows, V, room);
+  const int64_t need = at.dl + 2 * at.dl_rows * ids_at_once(at.dl_rows, V, room);
+  return need > at.least ? need : at.least;   // (from 33 to 63 rows the least is that of 64, which 32 of two numbers each need)
 }
 int64_t logprob_backward_least_bytes(int64_t max_rows, int32_t d, int32_t V) { return gradient_space(max_rows, d, V).least; }
 
