@@ -95,7 +95,7 @@ int mosaic_dropout_backward(const void *dout, int32_t stream_type, int64_t ld_do
  *   hidden     bf16 [T, d];  w: bf16 [V, d]
  *   idx, count dev int32, as mosaic_mask_compact makes them, or both NULL for all rows (then max_rows = T).  Rows may be listed
  *              in any order and more than once; an entry outside [0, T) is clamped to it
- *   max_rows   bound on *count, at most 2^31 - 1.  What the call takes follows from the rows found; its workspace from the bound
+ *   max_rows   bound on *count, at most 2^31 - 256.  What the call takes follows from the rows found; its workspace from the bound
  *   targets    dev int32[max_rows], of the listed rows in their order; needed for out_logprob alone
  *   out_*      dev float[max_rows], each may be NULL, not all of them with n_top = 0; entries from M on are left as they were
  *   n_top      0 .. MOSAIC_MAX_TOP;  top_id int32 and top_logprob float [max_rows, n_top], dense, NULL where it is 0

@@ -13,6 +13,8 @@ namespace {
 using namespace mosaic::arguments;
 
 constexpr int32_t kMostVocab = INT32_MAX - 256;
+// Listed rows: the kernels number them in 32 bits, in tiles of up to 256, the last of which ends below 2^31 as well.
+constexpr int64_t kMostListed = ((int64_t)1 << 31) - 256;
 
 int check_vocab(int32_t V) {
   if (V <= 0) return MOSAIC_ERR_INVALID_ARG;
@@ -61,7 +63,7 @@ int check_list_sizes(int64_t T, int64_t ld_h, int64_t max_rows, int32_t d, int32
   MOSAIC_RETURN_IF(check_sizes(T, d, MOSAIC_MAX_ROW));
   MOSAIC_RETURN_IF(check_vocab(V));
   if (max_rows < 0) return MOSAIC_ERR_INVALID_ARG;
-  if (max_rows >= kMaxRows || ld_h < d || ld_h % 8 != 0 || ld_h > kMaxStride) return MOSAIC_ERR_UNSUPPORTED_SHAPE;
+  if (max_rows > kMostListed || ld_h < d || ld_h % 8 != 0 || ld_h > kMaxStride) return MOSAIC_ERR_UNSUPPORTED_SHAPE;
   return MOSAIC_OK;
 }
 
