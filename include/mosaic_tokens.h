@@ -120,8 +120,9 @@ int mosaic_masked_logprobs(const void *hidden, int64_t ld_h, int64_t T, int32_t 
  *   dl[j, v] = g[j] ([v == targets[j]] - p[j, v]) - h[j] p[j, v] (log p[j, v] + H[j])       (g[j] = 0 without a target)
  *   dx[j]    = sum_v dl[j, v] w[v]                              the gradient at the listed row hidden[idx[j]]
  *   dw[v]    = sum_j dl[j, v] hidden[idx[j]]                    [+ what dw holds, if accumulate]
- * dl is rounded to bf16 for the matrix cores (up to 2^-8 relative per term; up to 32 rows with what that leaves over in a
- * second number each), but for the target's entries, which outweigh the others: those go into both sums in 32 bits.
+ * dl is rounded to bf16 for the matrix cores (up to 2^-8 relative per term), with what that leaves over in a second number
+ * each (2^-16 then) where dw has 32 bits, for dw, and up to 32 rows, for both results.  The target's entries, which outweigh the
+ * others, go into both sums in 32 bits.
  *   hidden .. targets   as for the forward pass
  *   logprob, entropy, lse   dev float[max_rows], what the forward pass gave: lse always, logprob with dlogprob, entropy with dentropy
  *   dlogprob   dev float[max_rows], or NULL (then targets and logprob are not looked at);  dentropy: the same, or NULL; not both NULL
@@ -129,10 +130,10 @@ int mosaic_masked_logprobs(const void *hidden, int64_t ld_h, int64_t T, int32_t 
  *              scatters them itself; mosaic_embedding_backward with idx as the tokens does it also where they are not
  *   dw         [V, d] by `dw_type`, row stride ld_dw, or NULL; not both NULL.  Every row is written
  *   accumulate nonzero: dw is added to (32-bit only), so that a batch can be taken in parts
- *   workspace  dev, 16-byte aligned: the listed rows, 32-bit sums of dx, the targets' terms of dw (6 and 4 max_rows d bytes and
- *              more for few rows), and dl of as many ids as the rest holds, 2 max_rows bytes each, at least 256.  The query answers for
- *              at most budget_bytes where that is enough, 0 or less: dl of up to 256 MiB; one for more rows serves fewer.  The sums'
- *              last bits follow from the size
+ *   workspace  dev, 16-byte aligned: the listed rows twice, 32-bit sums of dx, the targets' terms of dw (4 max_rows d bytes each and
+ *              more for few rows), and dl of as many ids as the rest holds, 2 max_rows bytes each, with second numbers 4, of these at
+ *              least 256.  The query answers for at most budget_bytes where that is enough, 0 or less: dl of up to 256 MiB; one for more
+ *              rows serves fewer.  The sums' last bits follow from the size
  * Every row of the bound costs what a listed one does: a close max_rows is worth its while.
  */
 int64_t mosaic_masked_logprobs_backward_workspace_bytes(int64_t max_rows, int32_t d, int32_t V, int64_t budget_bytes);

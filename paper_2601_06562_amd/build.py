@@ -14,7 +14,7 @@ LIB = os.path.join(PKG, "libmosaic.so")
 SOURCES = ["mosaic_api.hip", "mosaic_compact.hip", "mosaic_logits.hip", "mosaic_unmask.hip", "mosaic_probe.hip", "mosaic_vmm.hip",
            "mosaic_plan.cpp", "mosaic_graph.cpp", "mosaic_layer_api.hip", "mosaic_norm.hip", "mosaic_ffn.hip", "mosaic_tokens_api.hip",
            "mosaic_embed.hip", "mosaic_logprob.hip", "mosaic_logprob_w4_stats.hip", "mosaic_logprob_w4_top.hip",
-           "mosaic_logprob_w4_grad.hip"]
+           "mosaic_logprob_w4_grad.hip", "mosaic_logprob_w4_grad_low.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -130,7 +130,7 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
       p_base1 = MODE == kDx ? a.p1 + (int64_t)p_row * 2 : p_base0;
     }
     q_base = kRowQ ? a.q + q_row * 2 : a.q + q_row * a.ld_q;
-    cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, kStepK, kIsDw ? a.repeat : 0);
+    cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, kStepK, MODE == kDw ? a.repeat : 0);
     cq.place(wave, lane, a.ld_q, a.rows_q - q_row, kStepK);
     placed_p = placed_q = kStepK;
     step0 = (int)((int64_t)all_steps * split / a.splits);
@@ -175,7 +175,7 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int blo
       placed_p = left;
       cp.place(wave_p, lane, a.ld_p, a.rows_p - p_row, left);
     }
-    const int rows = kIsDw && a.repeat != 0 && left != 0 ? a.repeat : left;   // across K: there are behind the base
+    const int rows = MODE == kDw && a.repeat != 0 && left != 0 ? a.repeat : left;   // across K: there are behind the base
     walk_p.from = buffer_from((seg ? p_base1 : p_base0) + (kRowP ? k * a.ld_p : k * 2),
                               kRowP ? rows * (uint32_t)a.ld_p : left == 0 ? 0 : kOutside);
   };
@@ -758,7 +758,6 @@ GemmArgs product_args(const ProductArgs& f) {
   a.accumulate = f.accumulate;
   a.out0 = static_cast<char*>(f.out);
   a.ld_out0 = f.ld_out * (f.f32 ? 4 : 2);
-  a.repeat = f.repeat;
   a.slot = f.slot;
   a.extra = f.extra;
   a.ld_extra = f.ld_extra;

@@ -87,7 +87,6 @@ struct ProductArgs {
   int64_t ld_p, ld_q, ld_out, ld_extra;   // elements
   int64_t rows, depth;
   int32_t cols, splits, f32, accumulate;
-  int32_t repeat;        // column product: rows of p that there are where K, at most 64 then, takes them twice; else 0
 };
 struct ProductPlan { int32_t splits; double us; };
 ProductPlan plan_row_product(int64_t rows, int32_t cols, int64_t depth);

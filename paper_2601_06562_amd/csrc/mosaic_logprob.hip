@@ -215,7 +215,7 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
     slot_q = to_q;
   };
 
-  if (MODE != kGradients && blockIdx.x == 0 && threadIdx.x == 0) {
+  if (!gradient_mode(MODE) && blockIdx.x == 0 && threadIdx.x == 0) {
     p.found[0] = 2 * parts;
     p.found[1] = rows;
   }
@@ -257,10 +257,10 @@ __device__ __forceinline__ void run_units(const LogitParams& p, char* smem, int 
     if (done_vt >= 0) {
       const int64_t v = (int64_t)done_vt * kVocab + wp * kHalf;
       const int q0 = done_row0 + wq * 16 * QB, g = lane >> 4;
-      if constexpr (MODE == kGradients) {
+      if constexpr (gradient_mode(MODE)) {
         GradientRows<QB> of;
         of.read(p, q0, found);
-        gradient_tile<QB, false>(load, of, v, q0, found);
+        gradient_tile<QB, false, MODE == kGradientsLow>(load, of, v, q0, found);
       } else {
         if (done_tiles == 0) st.clear(q0, rows);
         const int own_row = q0 + 16 * g + (lane & 15);
@@ -375,10 +375,10 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(const LogitParams p) 
   if (tile >= kListedTile) run_units<MODE, kListedTile, 3, 3>(p, smem, rows, rows);
   else run_units<MODE, 64, 4, 4>(p, smem, rows, rows);
 }
-template <int TQ, int SP, int SQ>
+template <int MODE, int TQ, int SP, int SQ>
 __global__ __launch_bounds__(kThreads) void logit_gradient_kernel(const LogitParams p) {
   __shared__ __attribute__((aligned(1024))) char smem[ring_bytes(kVocab, TQ, SP, SQ)];
-  run_units<kGradients, TQ, SP, SQ>(p, smem, p.max_rows, rows_found(p));
+  run_units<MODE, TQ, SP, SQ>(p, smem, p.max_rows, rows_found(p));
 }
 
 // Joins a row's parts, a wave a row: a lane takes every 64th half.  Bound by the time to memory, which another kernel wrote: the
@@ -496,9 +496,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(const Joi
   else join_rows<2 * kMostSplits / 64>(p, rows, halves, stride);
 }
 
-// Rows gathered side by side, zeros from the last listed one on.
+// Rows gathered side by side, zeros from the last listed one on; `twice`: and again behind them.
 __global__ __launch_bounds__(256) void gather_rows_kernel(const __bf16* x, int64_t ld_x, const int32_t* idx, const int32_t* count, int T,
-                                                          int max_rows, int d, __bf16* out) {
+                                                          int max_rows, int d, __bf16* out, int twice) {
   const int n = count == nullptr ? max_rows : *count;
   const int per_row = d / 8;
   const int64_t all = (int64_t)max_rows * per_row;
@@ -512,6 +512,7 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const __bf16* x, int64
       v = *reinterpret_cast<const bf16x8_t*>(x + t * ld_x + c);
     }
     *reinterpret_cast<bf16x8_t*>(out + j * d + c) = v;
+    if (twice) *reinterpret_cast<bf16x8_t*>(out + (max_rows + j) * d + c) = v;
   }
 }
 
@@ -649,7 +650,7 @@ int launch_logprobs(const LogprobArgs& a, hipStream_t stream) {
     __bf16* rows = reinterpret_cast<__bf16*>(ws + at.rows);
     const int64_t pieces = a.max_rows * (a.d / 8);
     if (launch_kernel(gather_rows_kernel, dim3((unsigned)((pieces + 255) / 256 < 65536 ? (pieces + 255) / 256 : 65536)), dim3(256),
-                      stream, static_cast<const __bf16*>(a.hidden), a.ld_h, a.idx, a.count, (int)a.T, (int)a.max_rows, a.d, rows) != 0)
+                      stream, static_cast<const __bf16*>(a.hidden), a.ld_h, a.idx, a.count, (int)a.T, (int)a.max_rows, a.d, rows, 0) != 0)
       return -1;
     p.x = reinterpret_cast<const char*>(rows);
     p.ld_x = (int64_t)a.d * 2;
@@ -679,30 +680,32 @@ namespace {
 // Of dl, where the caller sets no other bound: what is written for a part of the vocabulary and read twice fits the memory-side cache,
 // and a part has enough ids to fill the chip (2048 rows of 126464 ids: two parts).
 constexpr int64_t kDlBytes = (int64_t)256 << 20;
-constexpr int64_t kLowRows = 32;                   // up to here dl carries what its rounding leaves over, as the feed-forward block's
+// Up to here dl carries what its rounding leaves over into both results, as the feed-forward block's; beyond, into dw of 32 bits alone:
+// results of 16 bits are rounded by more than it adds (2048 rows of 126464 x 4096: in the 2-norm 0.00172 off with it, 0.00166 without).
+// The products of dw are then twice as many: 2048 rows of 126464 x 4096 6.6 ms, in 16 bits 4.8.
+constexpr int64_t kLowRows = 32;
 
 struct GradientSpace {
   int64_t rows, coef, sort, sums, extra, slot, parts, dl, least;   // offsets; least: bytes for one tile of ids
-  int64_t dl_rows;
+  int64_t dx_rows;   // of dl in dx's product
   int32_t splits;
 };
 constexpr int64_t kSlotBytes = 4096;   // the slots are filled in rows of so many bytes
 int64_t slot_rows(int32_t V) { return (4 * (int64_t)V + kSlotBytes - 1) / kSlotBytes; }
 GradientSpace gradient_space(int64_t max_rows, int32_t d, int32_t V) {
   GradientSpace s;
-  const bool low = max_rows <= kLowRows;
-  s.dl_rows = low ? 2 * max_rows : max_rows;
-  s.splits = plan_row_product(s.dl_rows, d, V < 65536 ? V : 65536).splits;
+  s.dx_rows = max_rows <= kLowRows ? 2 * max_rows : max_rows;
+  s.splits = plan_row_product(s.dx_rows, d, V < 65536 ? V : 65536).splits;
   s.rows = 0;
-  s.coef = s.rows + padded(2 * max_rows * d);
+  s.coef = s.rows + padded(4 * max_rows * d);   // twice: K of dw where dl has two numbers an entry
   s.sort = s.coef + padded(4 * max_rows);
   s.sums = s.sort + padded(sort_tokens_bytes(max_rows));
   s.extra = s.sums + padded(4 * token_sum_partials(max_rows, d) * d);
   s.slot = s.extra + padded(4 * max_rows * d);
   s.parts = s.slot + slot_rows(V) * kSlotBytes;
-  const int64_t most = max_rows <= kLowRows || max_rows > 2 * kLowRows ? s.dl_rows : 2 * kLowRows;   // so that fewer rows need no more
+  const int64_t most = max_rows <= kLowRows || max_rows > 2 * kLowRows ? s.dx_rows : 2 * kLowRows;   // so that fewer rows need no more
   s.dl = s.parts + padded(4 * most_part_rows(most) * d);
-  s.least = s.dl + 2 * most * kVocab;
+  s.least = s.dl + 4 * max_rows * kVocab;
   return s;
 }
 // Ids at a time with so many bytes for dl, evenly, in whole tiles.
@@ -715,11 +718,12 @@ int64_t ids_at_once(int64_t dl_rows, int32_t V, int64_t bytes) {
   return (((int64_t)V + parts - 1) / parts + kVocab - 1) / kVocab * kVocab;
 }
 
+template <int MODE>
 int launch_gradient_tiles(const LogitParams& p, hipStream_t stream) {
   const int tile = tile_rows(p.max_rows);
-  if (tile == 256) return launch_kernel(logit_gradient_kernel<256, 3, 2>, dim3(kCus), dim3(kThreads), stream, p);
-  if (tile == 128) return launch_kernel(logit_gradient_kernel<128, 3, 3>, dim3(kCus), dim3(kThreads), stream, p);
-  return launch_kernel(logit_gradient_kernel<64, 4, 4>, dim3(kCus), dim3(kThreads), stream, p);
+  if (tile == 256) return launch_kernel(logit_gradient_kernel<MODE, 256, 3, 2>, dim3(kCus), dim3(kThreads), stream, p);
+  if (tile == 128) return launch_kernel(logit_gradient_kernel<MODE, 128, 3, 3>, dim3(kCus), dim3(kThreads), stream, p);
+  return launch_kernel(logit_gradient_kernel<MODE, 64, 4, 4>, dim3(kCus), dim3(kThreads), stream, p);
 }
 
 // dl of `n` ids from v on: whole tiles of ids on the 4-wave kernel where it takes them.
@@ -735,7 +739,9 @@ int launch_dl(LogitParams p, int64_t v, int64_t n, hipStream_t stream) {
     p.V = (int32_t)parts[k][1];
     p.dl_ids = (p.V + 7) / 8 * 8;
     p.first_id = (int32_t)(v + parts[k][0]);
-    if ((k == 0 ? launch_gradients_w4(p, stream) : launch_gradient_tiles(p, stream)) != 0) return -1;
+    const auto launch = p.low != 0 ? (k == 0 ? launch_gradients_low_w4 : launch_gradient_tiles<kGradientsLow>)
+                                   : (k == 0 ? launch_gradients_w4 : launch_gradient_tiles<kGradients>);
+    if (launch(p, stream) != 0) return -1;
   }
   return 0;
 }
@@ -745,13 +751,14 @@ int launch_dl(LogitParams p, int64_t v, int64_t n, hipStream_t stream) {
 int64_t logprob_backward_workspace_bytes(int64_t max_rows, int32_t d, int32_t V, int64_t budget_bytes) {
   const GradientSpace at = gradient_space(max_rows, d, V);
   const int64_t room = budget_bytes > 0 ? budget_bytes - at.dl : kDlBytes;
-  const int64_t need = at.dl + 2 * at.dl_rows * ids_at_once(at.dl_rows, V, room);
-  return need > at.least ? need : at.least;   // (from 33 to 63 rows the least is that of 64, which 32 of two numbers each need)
+  return at.dl + 4 * max_rows * ids_at_once(2 * max_rows, V, room);   // with two numbers an entry
 }
 int64_t logprob_backward_least_bytes(int64_t max_rows, int32_t d, int32_t V) { return gradient_space(max_rows, d, V).least; }
 
 int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
   const GradientSpace at = gradient_space(a.max_rows, a.d, a.V);
+  const bool dw = a.dw != nullptr, low = a.max_rows <= kLowRows || (dw && a.dw_f32 != 0);   // whether dl has two numbers an entry
+  const int64_t dl_rows = low ? 2 * a.max_rows : a.max_rows;
   char* ws = static_cast<char*>(a.workspace);
   __bf16* rows = reinterpret_cast<__bf16*>(ws + at.rows);
   float* coef = reinterpret_cast<float*>(ws + at.coef);
@@ -761,10 +768,9 @@ int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
   const int64_t pieces = (a.max_rows * (a.d / 8) + 255) / 256;
   const dim3 grid((unsigned)(pieces < 65536 ? pieces : 65536));
   if (launch_kernel(gather_rows_kernel, grid, dim3(256), stream, static_cast<const __bf16*>(a.hidden), a.ld_h, a.idx, a.count, (int)a.T,
-                    (int)a.max_rows, a.d, rows) != 0)
+                    (int)a.max_rows, a.d, rows, low ? 1 : 0) != 0)
     return -1;
   // the targets' own terms: for dw summed by target
-  const bool dw = a.dw != nullptr;
   if (a.targets != nullptr) {
     TermParams t = {a.targets, a.count, a.logprob, a.entropy, a.dlogprob, a.dentropy, coef, (int32_t)a.max_rows, a.V};
     const int64_t blocks = (a.max_rows + 255) / 256;
@@ -786,8 +792,7 @@ int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
       if (launch_token_sums(sum, false, true, stream) != 0) return -1;
     }
   }
-  const int64_t each = ids_at_once(at.dl_rows, a.V, a.workspace_bytes - at.dl);
-  const bool low = a.max_rows <= kLowRows;
+  const int64_t each = ids_at_once(dl_rows, a.V, a.workspace_bytes - at.dl);
   LogitParams p = {};
   p.w = static_cast<const char*>(a.w);
   p.x = reinterpret_cast<const char*>(rows);
@@ -817,7 +822,7 @@ int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
       x.ld_p = a.ld_w;
       x.ld_q = each;
       x.ld_out = a.d;
-      x.rows = at.dl_rows;
+      x.rows = at.dx_rows;
       x.depth = n;
       x.cols = a.d;
       x.splits = at.splits;
@@ -836,12 +841,11 @@ int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
       w.ld_q = each;
       w.ld_out = a.ld_dw;
       w.rows = n;
-      w.depth = at.dl_rows;
+      w.depth = dl_rows;
       w.cols = a.d;
       w.splits = 1;
       w.f32 = a.dw_f32;
       w.accumulate = a.accumulate;
-      w.repeat = low ? (int32_t)a.max_rows : 0;
       if (launch_column_product(w, stream) != 0) return -1;
     }
   }
@@ -855,7 +859,7 @@ int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
   o.dx = static_cast<__bf16*>(a.dx);
   o.ld_w = a.ld_w;
   o.ld_dx = a.ld_dx;
-  o.n_parts = at.splits * (low ? 2 : 1);
+  o.n_parts = at.splits * (int32_t)(at.dx_rows / a.max_rows);
   o.max_rows = (int32_t)a.max_rows;
   o.d = a.d;
   o.V = a.V;

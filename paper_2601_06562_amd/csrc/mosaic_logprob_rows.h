@@ -79,8 +79,10 @@ struct LogitParams {
   int32_t first_id, all_ids;
   int32_t dl_ids;            // ids that dl holds, a multiple of 8
 };
-// Alternatives are a kernel's own: without them its code is a quarter, and most of a short call's time goes to fetching code.
-enum { kStatistics, kAlternatives, kGradients };
+// Alternatives are a kernel's own: without them its code is a quarter, and most of a short call's time goes to fetching code.  So are
+// gradients with low halves: asked for at each tile, they took 1% of a call without.
+enum { kStatistics, kAlternatives, kGradients, kGradientsLow };
+constexpr bool gradient_mode(int mode) { return mode == kGradients || mode == kGradientsLow; }
 
 // A kernel's arguments, read where they are used: what is made of a tile uses many, and kept from one tile to the next they would
 // take the scalar registers that the products need.
@@ -539,7 +541,8 @@ __device__ __forceinline__ bool sort_now(int tiles, int of) { return tiles == of
 
 // The gradient at a finished tile's logits, in 16 bits, as the matrix products behind take it:
 //   dl[v] = - p[v] (g + h (log p[v] + H))      g, h: the gradients of the row's log probability and entropy H
-// with 0 at the target, whose one-hot term outweighs the others; the target's whole term goes past the 16 bits.
+// with 0 at the target, whose one-hot term outweighs the others; the target's whole term goes past the 16 bits.  What the rounding
+// leaves over is a second number of 16 bits where the sums show it (LOW): for results in 32 bits, and in the sums of few rows.
 // v0: the first id of the wave.
 template <int QB>
 struct GradientRows {   // what a lane holds of its own rows (as Rows)
@@ -561,7 +564,7 @@ struct GradientRows {   // what a lane holds of its own rows (as Rows)
     }
   }
 };
-template <int QB, bool ROLLED, class Load>
+template <int QB, bool ROLLED, bool LOW, class Load>
 __device__ __forceinline__ void gradient_tile(Load load, const GradientRows<QB>& of, int64_t v0, int row0, int found) {
   const Arguments p = arguments_again();
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, run = first_of<4>(lane);
@@ -595,16 +598,14 @@ __device__ __forceinline__ void gradient_tile(Load load, const GradientRows<QB>&
           v[r] = listed && rel != at && at < there ? d : 0.f;
         }
         pack(o[k], v);
-        if constexpr (QB == 1) pack_low(low[k], o[k], v);
+        if constexpr (LOW) pack_low(low[k], o[k], v);
       }
       gather(o);
       const int c = (int)(v0 + 16 * b) + run;
       if (in) store_quads(p->dl + row * p->ld_dl, c, p->dl_ids, o);
-      if constexpr (QB == 1) {   // the tiles that few rows take
-        if (p->low != 0) {
-          gather(low);
-          if (in) store_quads(p->dl + p->low + row * p->ld_dl, c, p->dl_ids, low);
-        }
+      if constexpr (LOW) {
+        gather(low);
+        if (in) store_quads(p->dl + p->low + row * p->ld_dl, c, p->dl_ids, low);
       }
     }
   });
@@ -614,7 +615,8 @@ __device__ __forceinline__ void gradient_tile(Load load, const GradientRows<QB>&
 bool w4_takes(int32_t d, int32_t V);
 int launch_statistics_w4(const LogitParams& p, hipStream_t stream);
 int launch_alternatives_w4(const LogitParams& p, hipStream_t stream);
-int launch_gradients_w4(const LogitParams& p, hipStream_t stream);
+int launch_gradients_w4(const LogitParams& p, hipStream_t stream);        // without low halves
+int launch_gradients_low_w4(const LogitParams& p, hipStream_t stream);    // with them
 int64_t w4_list_bytes();
 
 }  // namespace logprob

@@ -10,7 +10,7 @@
 // fetched anew.  They are sorted in after 1, 2, 4, 8, ... tiles (every other schedule tried 2 to 8% slower at 4096 rows).
 //
 // It takes d that is a multiple of 64 and whole tiles of 256 ids, or a last tile over the vocabulary's last 256 ids, of which
-// those of the tile before it are not counted again; mosaic_logprob.hip has the kernel for the rest.  Each of the three kernels is
+// those of the tile before it are not counted again; mosaic_logprob.hip has the kernel for the rest.  Each of the four kernels is
 // compiled by itself (mosaic_logprob_w4_*.hip), since one takes about a minute.
 #ifndef MOSAIC_LOGPROB_W4_H_
 #define MOSAIC_LOGPROB_W4_H_
@@ -129,7 +129,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
     const int first_row = tt * kTokens + wt * (kTokens / 2);   // this wave's rows
     int trow[NB];
     [[maybe_unused]] int target[Rows<NB>::kOwn];
-    if constexpr (MODE != kGradients) {
+    if constexpr (!gradient_mode(MODE)) {
 #pragma unroll
       for (int k = 0; k < Rows<NB>::kOwn; ++k) {
         const int row = first_row + 16 * (4 * k + q) + l16;
@@ -211,7 +211,7 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
 
     [[maybe_unused]] Rows<NB> st;
     [[maybe_unused]] GradientRows<NB> of;
-    if constexpr (MODE == kGradients) of.read(p, first_row, found);
+    if constexpr (gradient_mode(MODE)) of.read(p, first_row, found);
     else st.clear(first_row, rows);
     const int64_t of_half = (int64_t)(2 * sp + wv) * sched.stride;
     auto place = [&](int k, bool& in) __attribute__((always_inline)) {
@@ -248,14 +248,14 @@ __device__ __forceinline__ void w4_units(const LogitParams& p, const Schedule& s
 #include "mosaic_w4_columns.inc"
       };
       const int64_t v = first_id(vt0 + n) + wv * kHalf;
-      if constexpr (MODE == kGradients) {
-        gradient_tile<NB, true>(load, of, v, first_row, found);
+      if constexpr (gradient_mode(MODE)) {
+        gradient_tile<NB, true, MODE == kGradientsLow>(load, of, v, first_row, found);
       } else {
         const int64_t from = vt0 + n == ragged_tile ? (int64_t)ragged_tile * kVocab : 0;
         reduce_tile<NB, true, MODE == kAlternatives, false>(load, st, v + 4 * q, from, p.V, target, first_row, lists, n == 0, sort_now(n + 1, ntile), place);
       }
     }
-    if constexpr (MODE != kGradients) {
+    if constexpr (!gradient_mode(MODE)) {
 #pragma unroll
       for (int k = 0; k < Rows<NB>::kOwn; ++k) {
         const int row = first_row + 16 * (4 * k + q) + l16;
@@ -288,16 +288,16 @@ __device__ __forceinline__ void w4_units_of(const LogitParams& p, const Schedule
 template <int MODE>
 __global__ __launch_bounds__(kW4Threads) void logprob_kernel_w4(const LogitParams p, int stream_w) {
   __shared__ __attribute__((aligned(1024))) char smem[kLdsBytes];
-  const int found = rows_found(p), rows = MODE == kGradients ? p.max_rows : found;
+  const int found = rows_found(p), rows = gradient_mode(MODE) ? p.max_rows : found;
   if (rows <= 0) return;
   const Schedule sched = choose_schedule_wave(p.sched, rows);
-  if (MODE != kGradients && blockIdx.x == 0 && threadIdx.x == 0) {
+  if (!gradient_mode(MODE) && blockIdx.x == 0 && threadIdx.x == 0) {
     p.found[0] = 2 * sched.splits;
     p.found[1] = sched.stride;
   }
   const int units = sched.row_tiles * sched.splits, first = first_unit((int)blockIdx.x, (int)p.sched.grid, units);
   if (first >= units) return;
-  if constexpr (MODE != kGradients) {
+  if constexpr (!gradient_mode(MODE)) {
     if (stream_w != 0 && sched.row_tiles == 1) {
       w4_units_of<MODE, true>(p, sched, rows, found, first, smem);
       return;
