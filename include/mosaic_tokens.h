@@ -101,7 +101,7 @@ int mosaic_dropout_backward(const void *dout, int32_t stream_type, int64_t ld_do
  *   n_top      0 .. MOSAIC_MAX_TOP;  top_id int32 and top_logprob float [max_rows, n_top], dense, NULL where it is 0
  *   workspace  dev, 16-byte aligned, mosaic_masked_logprobs_workspace_bytes bytes (one for more rows serves fewer): sums of the
  *              vocabulary's parts, with alternatives lists of their candidates (67 MB) and the parts' best, and, where the
- *              hidden states pass 2 GiB, the listed rows side by side
+ *              hidden states pass 2 GiB, the listed rows side by side (counted without a list, too, and not used then)
  * A NaN among a row's logits makes that row's log probabilities, entropy and log-sum-exp NaN and its alternatives unspecified
  * (ids in [-1, V)), an infinite one (of infinite weights or states; 2^100 and more counts as one) at least its entropy; other rows
  * are not affected.

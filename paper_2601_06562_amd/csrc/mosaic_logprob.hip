@@ -496,12 +496,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(const Joi
   else join_rows<2 * kMostSplits / 64>(p, rows, halves, stride);
 }
 
-// Rows gathered side by side, zeros from the last listed one on; `twice`: and again behind them.
+// Rows gathered side by side.  copies: 0, the listed ones alone; 1 or 2, with zeros from the last listed one on, and so often, one
+// behind the other.
 __global__ __launch_bounds__(256) void gather_rows_kernel(const __bf16* x, int64_t ld_x, const int32_t* idx, const int32_t* count, int T,
-                                                          int max_rows, int d, __bf16* out, int twice) {
+                                                          int max_rows, int d, __bf16* out, int copies) {
   const int n = count == nullptr ? max_rows : *count;
   const int per_row = d / 8;
-  const int64_t all = (int64_t)max_rows * per_row;
+  const int64_t all = (int64_t)(copies == 0 && n < max_rows ? n : max_rows) * per_row;
   for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
     const int64_t j = e / per_row;
     const int c = (int)(e - j * per_row) * 8;
@@ -512,7 +513,7 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const __bf16* x, int64
       v = *reinterpret_cast<const bf16x8_t*>(x + t * ld_x + c);
     }
     *reinterpret_cast<bf16x8_t*>(out + j * d + c) = v;
-    if (twice) *reinterpret_cast<bf16x8_t*>(out + (max_rows + j) * d + c) = v;
+    if (copies == 2) *reinterpret_cast<bf16x8_t*>(out + (max_rows + j) * d + c) = v;
   }
 }
 
@@ -768,7 +769,7 @@ int launch_logprobs_backward(const LogprobBackwardArgs& a, hipStream_t stream) {
   const int64_t pieces = (a.max_rows * (a.d / 8) + 255) / 256;
   const dim3 grid((unsigned)(pieces < 65536 ? pieces : 65536));
   if (launch_kernel(gather_rows_kernel, grid, dim3(256), stream, static_cast<const __bf16*>(a.hidden), a.ld_h, a.idx, a.count, (int)a.T,
-                    (int)a.max_rows, a.d, rows, low ? 1 : 0) != 0)
+                    (int)a.max_rows, a.d, rows, low ? 2 : 1) != 0)
     return -1;
   // the targets' own terms: for dw summed by target
   if (a.targets != nullptr) {
