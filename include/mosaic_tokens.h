@@ -127,7 +127,8 @@ int mosaic_masked_logprobs(const void *hidden, int64_t ld_h, int64_t T, int32_t 
  *   logprob, entropy, lse   dev float[max_rows], what the forward pass gave: lse always, logprob with dlogprob, entropy with dentropy
  *   dlogprob   dev float[max_rows], or NULL (then targets and logprob are not looked at);  dentropy: the same, or NULL; not both NULL
  *   dx         bf16 [max_rows, d] or NULL; rows from M on are left as they were.  A program whose listed rows are all different
- *              scatters them itself; mosaic_embedding_backward with idx as the tokens does it also where they are not
+ *              scatters them itself; mosaic_embedding_backward with idx as the tokens does it also where they are not.  Of an entry
+ *              outside [0, T), clamped here as in the forward pass, it takes no gradient: such a list is clamped by the caller
  *   dw         [V, d] by `dw_type`, row stride ld_dw, or NULL; not both NULL.  Every row is written
  *   accumulate nonzero: dw is added to (32-bit only), so that a batch can be taken in parts
  *   workspace  dev, 16-byte aligned: the listed rows twice, 32-bit sums of dx, the targets' terms of dw (4 max_rows d bytes each and
