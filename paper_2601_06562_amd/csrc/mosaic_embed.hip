@@ -571,7 +571,7 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const DropoutArgs p) 
       if constexpr (ADD) v[i] += add[i];
     }
     O* const out = static_cast<O*>(p.out) + t * p.ld_out;
-    if constexpr (PAST && sizeof(O) == 2) store_columns<true>(out, c, p.d, v);
+    if constexpr (PAST) store_columns<true>(out, c, p.d, v);   // (a lane's columns side by side: of 16 bits)
     else store8(out + c, v);
   }
 }
@@ -581,9 +581,9 @@ dim3 row_grid(int64_t T, int rows, int d) {
   const int64_t blocks = (T + rows - 1) / rows;
   return dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks), (unsigned)((d + kStripe - 1) / kStripe));
 }
-// An output from half of the memory-side cache on is written past the caches, which keeps the rows that are read in them (into 32 bits
-// 32768 x 4096: 146 -> 115 us, 16000 x 4096, 262 MB: 75 -> 57; 16000 x 1024, 66 MB: 16.4 either way, and what comes next finds
-// it there).
+// A lookup's output from half of the memory-side cache on is written past the caches, which keeps the rows that are read in them (into 32
+// bits 32768 x 4096: 146 -> 115 us, 16000 x 4096, 262 MB: 75 -> 57; 16000 x 1024, 66 MB: 16.4 either way, and what comes next
+// finds it there); so is a dropout's of 16 bits, which reads as much as it writes, each once.
 constexpr int64_t kPastBytes = (int64_t)128 << 20;
 constexpr int kPastRows = 2;   // rows of a block then: one 155 us, two 114, four 115; below, one takes what two and four do
 
@@ -596,8 +596,10 @@ int launch_embedding(const EmbedArgs& a, hipStream_t stream) {
 
 template <typename S, typename O, bool ADD>
 int launch_dropout_as(const DropoutArgs& a, hipStream_t stream) {
-  if (a.T * a.d * (int64_t)sizeof(O) >= kPastBytes)
-    return launch_kernel(dropout_kernel<S, O, ADD, true>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
+  if constexpr (sizeof(O) == 2) {
+    if (a.T * a.d * (int64_t)sizeof(O) >= kPastBytes)
+      return launch_kernel(dropout_kernel<S, O, ADD, true>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
+  }
   return launch_kernel(dropout_kernel<S, O, ADD, false>, row_grid(a.T, 1, a.d), dim3(kThreads), stream, a);
 }
 
