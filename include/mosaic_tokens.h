@@ -121,8 +121,8 @@ int mosaic_masked_logprobs(const void *hidden, int64_t ld_h, int64_t T, int32_t 
  *   dx[j]    = sum_v dl[j, v] w[v]                              the gradient at the listed row hidden[idx[j]]
  *   dw[v]    = sum_j dl[j, v] hidden[idx[j]]                    [+ what dw holds, if accumulate]
  * dl is rounded to bf16 for the matrix cores (up to 2^-8 relative per term), with what that leaves over in a second number
- * each (2^-16 then) where dw has 32 bits, for dw, and up to 32 rows, for both results.  The target's entries, which outweigh the
- * others, go into both sums in 32 bits.
+ * each (2^-16 then) where dw has 32 bits, for dw, and where max_rows is 32 or less, for both results.  The target's entries,
+ * which outweigh the others, go into both sums in 32 bits.
  *   hidden .. targets   as for the forward pass
  *   logprob, entropy, lse   dev float[max_rows], what the forward pass gave: lse always, logprob with dlogprob, entropy with dentropy
  *   dlogprob   dev float[max_rows], or NULL (then targets and logprob are not looked at);  dentropy: the same, or NULL; not both NULL
