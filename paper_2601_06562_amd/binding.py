@@ -639,28 +639,36 @@ def mosaic_embedding_backward(dout, tokens, dtable, workspace, scale=1.0, count=
         _stream_ptr(stream)), "mosaic_embedding_backward")
 
 
+def _mask_args(p, seed, site, first_row):
+    """What a dropout's mask follows from.  Numbers past the library's would arrive there as others, and make their mask."""
+    site, first_row = int(site), int(first_row)
+    if not 0 <= site < 2 ** 31 - 1 or not 0 <= first_row < 2 ** 63:
+        raise ValueError("site must lie in [0, 2^31 - 1), first_row in [0, 2^63)")
+    return float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, site, first_row
+
+
 def mosaic_dropout_forward(x, residual, out, p, seed, site=0, first_row=0, stream=None):
     """out = x with a share p of its elements dropped and the others grown [+ residual]: x bf16 [T, d], residual (or None) and
     out bf16 or float32, both of one type.  The mask follows from seed, site, first_row + row, and column."""
+    mask = _mask_args(p, seed, site, first_row)
     T, d = x.shape
     if residual is not None and residual.dtype != out.dtype:
         raise TypeError("out must have the residual's type")
     p_x, ld_x = _rows(x, "x", T, d, torch.bfloat16)
     p_r, ld_r = _rows(residual, "residual", T, d)
     p_o, ld_o = _rows(out, "out", T, d)
-    _check(_tokens().mosaic_dropout_forward(p_x, ld_x, p_r, _type_of(out, "out"), ld_r, T, d, float(p),
-                                            int(seed) & 0xFFFFFFFFFFFFFFFF, int(site), int(first_row), p_o, ld_o,
+    _check(_tokens().mosaic_dropout_forward(p_x, ld_x, p_r, _type_of(out, "out"), ld_r, T, d, *mask, p_o, ld_o,
                                             _stream_ptr(stream)), "mosaic_dropout_forward")
 
 
 def mosaic_dropout_backward(dout, dx, p, seed, site=0, first_row=0, stream=None):
     """dx (bf16 [T, d]) from dout (bf16 or float32) by the mask that mosaic_dropout_forward makes of the same arguments."""
+    mask = _mask_args(p, seed, site, first_row)
     T, d = dout.shape
     p_g, ld_g = _rows(dout, "dout", T, d)
     p_x, ld_x = _rows(dx, "dx", T, d, torch.bfloat16)
-    _check(_tokens().mosaic_dropout_backward(p_g, _type_of(dout, "dout"), ld_g, T, d, float(p),
-                                             int(seed) & 0xFFFFFFFFFFFFFFFF, int(site), int(first_row), p_x, ld_x,
-                                             _stream_ptr(stream)), "mosaic_dropout_backward")
+    _check(_tokens().mosaic_dropout_backward(p_g, _type_of(dout, "dout"), ld_g, T, d, *mask, p_x, ld_x, _stream_ptr(stream)),
+           "mosaic_dropout_backward")
 
 
 def _list_args(hidden, w, idx, count, max_rows):
