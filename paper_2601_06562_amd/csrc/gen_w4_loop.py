@@ -2,7 +2,7 @@
 """Generates mosaic_w4_tile.inc (greedy) and mosaic_w4_tile_sample.inc (sampling): one vocabulary tile of the 4-wave
 fused kernel as one inline-asm statement, the hand-scheduled K-loop followed by the tile's vocabulary reduction, for
 each width of the row tile (32*NB tokens, NB = 1..8, chosen by `if constexpr`); mosaic_w4_products.inc, the K-loop alone, and
-mosaic_w4_columns.inc, the logits it leaves in the accumulators (log probabilities of given tokens, mosaic_logprob_w4.hip).
+mosaic_w4_columns.inc, the logits it leaves in the accumulators (log probabilities of given tokens, mosaic_logprob_w4.h).
 
 The K-loop covers the nk K-tiles of the vocabulary tile.  Per K-tile (step g) a wave issues 16*nb
 v_mfma_f32_16x16x32_bf16: its 128 vocabulary ids (8 blocks) against its half of the tokens (nb blocks), both K-halves of

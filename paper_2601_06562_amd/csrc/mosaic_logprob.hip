@@ -4,8 +4,8 @@
 // The kernels here take any sizes; where the hand-scheduled K-loop takes them too (mosaic_logprob_w4.h) that one runs.  A tile is 256
 // vocabulary ids ("P", the weights' rows) by 64, 128 or 256 listed rows ("Q", gathered as they are copied), K in
 // steps of 64 through rings of slots in LDS.  A unit is a tile of rows and a part of the vocabulary, whose tiles a block takes one
-// after another; the state of a row is held between them.  32003 x 1032: 900 rows 81 us, 3000 rows 218 (0.91 PFLOP/s), where the
-// hand-scheduled loop takes 71 and 176 for 32000 x 1024; five alternatives 191 and 548, there 120 and 288.
+// after another; the state of a row is held between them.  32003 x 1032: 900 rows 83 us, 3000 rows 200 (0.99 PFLOP/s), where the
+// hand-scheduled loop takes 64 and 164 for 32000 x 1024; five alternatives 187 and 551, there 117 and 276.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -682,8 +682,9 @@ namespace {
 // and a part has enough ids to fill the chip (2048 rows of 126464 ids: two parts).
 constexpr int64_t kDlBytes = (int64_t)256 << 20;
 // Up to here dl carries what its rounding leaves over into both results, as the feed-forward block's; beyond, into dw of 32 bits alone:
-// results of 16 bits are rounded by more than it adds (2048 rows of 126464 x 4096: in the 2-norm 0.00172 off with it, 0.00166 without).
-// The products of dw are then twice as many: 2048 rows of 126464 x 4096 6.6 ms, in 16 bits 4.8.
+// results of 16 bits are rounded by more than it adds (dw and dx of 2048 rows of 126464 x 4096 are 0.00170 and 0.00171 off in the 2-norm,
+// rounded alone 0.00165 and 0.00166; 900 of 32000 x 1024 0.00175 and 0.00176 for 0.00166 and 0.00167).  dw of 32 bits is 6e-7 off, with
+// terms of 16 bits 4e-4; its products are twice as many: 2048 rows of 126464 x 4096 6.6 ms, with terms of 16 bits 5.0, dw of 16 bits 4.8.
 constexpr int64_t kLowRows = 32;
 
 struct GradientSpace {

@@ -1,4 +1,4 @@
-// What the kernels that make logits tile by tile do with them (mosaic_logprob.hip, mosaic_logprob_w4.hip): statistics of rows,
+// What the kernels that make logits tile by tile do with them (mosaic_logprob.hip, mosaic_logprob_w4.h): statistics of rows,
 // candidates for their most probable ids, gradients at the logits.  Device code.
 //
 // In both kernels a wave holds 128 ids of a tile by 16 QB rows, in blocks of 16 x 16: lane l has ids 16 i + 4 (l / 16) + r, i < 8,
@@ -71,7 +71,7 @@ struct LogitParams {
   float* target_logit;       // [max_rows]
   Entry* lists;              // of every block's waves: kListRoom x columns x 64 lanes
   int32_t* found;
-  ScheduleInput sched;       // mosaic_logprob_w4.hip
+  ScheduleInput sched;       // mosaic_logprob_w4.h
   // gradients: of V ids from `first_id` on, for max_rows rows (zeros from the last listed one on)
   const float *lse, *entropy, *dlogprob, *dentropy;   // the last three each with what needs them, else nullptr
   char* dl;                  // bf16 [max_rows, ld_dl]
@@ -489,9 +489,9 @@ __device__ __forceinline__ void reduce_tile(Load load, Rows<QB>& st, int64_t v0,
             stopped = stopped | (want & !fits);
             done = (want & !fits) ? i : done;
             // Most lanes put down one of a quad or none.  With EIGHT waves a compute unit, whose stores take turns, all four of a quad are
-            // only gone through where some lane has a second one (900 rows of 32003 x 1032, five alternatives: 236 us, so 191); with
+            // only gone through where some lane has a second one (900 rows of 32003 x 1032, five alternatives: 236 us, so 187); with
             // four waves telling that takes longer (32000 x 1024: 125 us, so 129).
-            const float above = want & fits ? pass : __builtin_inff(), *const v = x + 4 * i;
+            const float above = (want & fits) ? pass : __builtin_inff(), *const v = x + 4 * i;
             bool each = true;
             if constexpr (EIGHT) {
               const float second = fmaxf(fminf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fminf(v[0], v[1]), fminf(v[2], v[3])));

@@ -6,7 +6,7 @@
 // Bound by the power of the matrix cores for many rows, by memory for few: 126464 x 4096, 4096 rows 2.61 to 2.81 ms (1.51 to 1.63
 // PFLOP/s; the mask-only pass, which keeps no entropy, 2.55 to 2.59 beside it), with eight alternatives 4 to 5% more, one row 167 us
 // (6.2 TB/s); gradients at the logits, 2048 rows by 63232 ids, 764 us (1.39 PFLOP/s).  Alternatives cost small tiles of work most (900
-// rows of 32000 x 1024: 68 us, with five 120): a unit's first tiles bring the most candidates, and code that runs once a unit is
+// rows of 32000 x 1024: 64 us, with five 117): a unit's first tiles bring the most candidates, and code that runs once a unit is
 // fetched anew.  They are sorted in after 1, 2, 4, 8, ... tiles (every other schedule tried 2 to 8% slower at 4096 rows).
 //
 // It takes d that is a multiple of 64 and whole tiles of 256 ids, or a last tile over the vocabulary's last 256 ids, of which
@@ -311,6 +311,10 @@ int launch(LogitParams p, hipStream_t stream) {
   p.sched.vocab_tiles = (uint32_t)(((int64_t)p.V + kVocab - 1) / kVocab);
   p.sched.k_tiles = (uint32_t)(p.d / kTileK);
   p.sched.widths = 0xff;
+  // The mask-only pass's own rule, by its greedy reduction.  Each width forced in turn, 20 to 3000 rows of 8192 x 512, 32000 x 1024, 50257
+  // x 704, 65536 x 2048, 126464 x 4096 and 152064 x 3584, 60 sizes: without alternatives its choice is 1.2% off the best width in the
+  // mean and at most 13% (40 rows of 65536 x 2048, 57 us for 50); with one 1.9% and 18% (500 of 32000 x 1024, 71 for 60), five 1.8%
+  // and 18% (79 for 67), 16 3.8% and 32% (500 of 50257 x 704, 160 for 122): candidates cost a wide tile more than the rule counts.
   p.sched.sampling = 0;
   p.sched.extra = 0;
   p.sched.grid = kCus;
