@@ -19,6 +19,8 @@ SIZES = [  # rows, d, V, whether dw has 32 bits
     (101, 128, 67328, False), (196, 64, 48128, False), (185, 8, 72801, True), (145, 8, 93010, False), (100, 128, 72680, True),
     (137, 64, 81920, False), (1133, 64, 11008, False), (708, 64, 18452, True), (487, 64, 33756, False), (13586, 64, 1280, False),
     (13642, 64, 1280, True), (14718, 64, 1487, False),
+    # more rows than dx takes in one launch
+    (140003, 64, 300, True), (140003, 72, 257, False), (262145, 64, 512, False),
     # K of many steps in every product
     (1500, 1032, 9003, False), (1500, 1024, 9003, True),
 ]

@@ -21,9 +21,11 @@ SIZES = [  # rows, d, V
     # a lone row tile under weights past the memory-side cache
     (1, 1408, 107264), (33, 1536, 98560), (65, 1536, 98561), (97, 1536, 98560), (129, 1536, 98700), (161, 1472, 102656),
     (193, 1472, 102656), (225, 1536, 98560), (225, 1536, 98815),
+    # more rows than any but the widest tile is offered for
+    (1048577, 64, 512), (1050001, 320, 270),
     # the kernel of eight waves
     (2, 16, 218), (1, 8, 97792), (80, 40, 201), (77, 16, 71424), (156, 8, 37632), (139, 32, 251), (130, 64, 66945), (8815, 136, 3314),
-    (8544, 144, 1792), (1534, 248, 21760), (7281, 176, 8704),
+    (8544, 144, 1792), (1534, 248, 21760), (7281, 176, 8704), (1050001, 8, 300),
 ]
 TOPS = (0, 2, 16)
 
