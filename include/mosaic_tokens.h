@@ -134,7 +134,7 @@ int mosaic_masked_logprobs(const void *hidden, int64_t ld_h, int64_t T, int32_t 
  *   workspace  dev, 16-byte aligned: the listed rows twice, 32-bit sums of dx, the targets' terms of dw (4 max_rows d bytes each and
  *              more for few rows), and dl of as many ids as the rest holds, 2 max_rows bytes each, with second numbers 4, of these at
  *              least 256.  The query answers for at most budget_bytes where that is enough, 0 or less: dl of up to 256 MiB; one for more
- *              rows serves fewer.  The sums' last bits follow from the size
+ *              rows serves fewer.  The sums' last bits follow from the size, and from whether there are second numbers
  * Every row of the bound costs what a listed one does: a close max_rows is worth its while.
  */
 int64_t mosaic_masked_logprobs_backward_workspace_bytes(int64_t max_rows, int32_t d, int32_t V, int64_t budget_bytes);
